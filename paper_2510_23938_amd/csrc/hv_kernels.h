@@ -217,4 +217,41 @@ hipError_t launch_verify_root_dev(const uint8_t* root, const uint8_t* expected, 
 hipError_t launch_compare_roots(const uint8_t* roots, const uint8_t* expected, uint32_t n, uint32_t nbytes,
                                 uint32_t* mismatch, hipStream_t s);
 
+// 8-bit operators (fp8_quantize.hip, fp8_matmul.hip); arguments as in hv_fp8.h,
+// checked, with at least one element to write.
+enum : int { kTypeBf16 = 0, kTypeF16 = 1, kTypeF32 = 2 };  // hv_type
+struct NormArgs {
+    const void* x;
+    uint64_t ld_x;
+    const void* residual;  // NULL: none
+    uint64_t ld_residual;
+    const void* weight;
+    float eps;
+    uint64_t rows, cols;
+    void* residual_out;
+    uint64_t ld_out;
+    uint8_t* codes;
+    uint64_t ld_codes;
+    float* scales;
+};
+struct MatmulArgs {
+    const uint8_t* a;
+    uint64_t ld_a;
+    const float* a_scales;
+    const uint8_t* b;
+    uint64_t ld_b;
+    const float* b_scales;
+    uint64_t m, n, k;
+    void* c;
+    uint64_t ld_c;
+    void* workspace;
+};
+hipError_t launch_fp8_quantize(int type, const void* x, uint64_t ld_x, uint64_t rows, uint64_t cols, bool blocks,
+                               uint8_t* codes, uint64_t ld_codes, float* scales, hipStream_t s);
+hipError_t launch_fp8_rms_norm(int type, const NormArgs& a, hipStream_t s);
+hipError_t launch_fp8_gated(int type, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
+                            uint64_t rows, uint64_t cols, uint8_t* codes, uint64_t ld_codes, float* scales,
+                            hipStream_t s);
+hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
+
 }  // namespace hv

@@ -41,6 +41,10 @@ HV_SHA256, HV_SHA384 = 0, 1
 HV_NOALLOC_SCRATCH_BYTES = 64 << 20  # the static scratch of hv_hash_chunks_noalloc, per GPU
 # hash name -> (hv_alg code, digest bytes)
 ALGS = {"sha256": (HV_SHA256, 32), "sha384": (HV_SHA384, 48)}
+HV_BF16, HV_F16, HV_F32 = 0, 1, 2
+# element type -> its hv_type code
+TYPES = {torch.bfloat16: HV_BF16, torch.float16: HV_F16, torch.float32: HV_F32}
+HV_FP8_GROUP = 128  # columns (and, for weights, rows) of an 8-bit matrix that share a scale
 _STATUS = {1: "HV_ERR_INVALID_ARG", 2: "HV_ERR_WORKSPACE", 3: "HV_ERR_HIP"}
 
 # exported symbols, in the order include/hv.h declares them
@@ -62,6 +66,8 @@ EXPORTS = (
     "hv_stream_destroy",  # include/hv_monitor.h
     "hv_plan_bytes", "hv_plan_init", "hv_plan_run", "hv_verify_model_workspace_bytes",
     "hv_verify_model",  # include/hv_plan.h
+    "hv_fp8_quantize", "hv_fp8_rms_norm", "hv_fp8_gated", "hv_fp8_matmul_workspace_bytes",
+    "hv_fp8_matmul",  # include/hv_fp8.h
 )
 
 
@@ -163,6 +169,13 @@ def _load():
         "hv_stream_create_cu_masked": ([vp, u32, vp], ctypes.c_int),
         "hv_stream_cu_mask": ([vp, vp, u32], ctypes.c_int),
         "hv_stream_destroy": ([vp], ctypes.c_int),
+        "hv_fp8_quantize": ([ctypes.c_int32, vp, u64, u64, u64, u32, vp, u64, vp, vp], ctypes.c_int),
+        "hv_fp8_rms_norm": ([ctypes.c_int32, vp, u64, vp, u64, vp, ctypes.c_float, u64, u64, vp, u64, vp, u64, vp,
+                             vp], ctypes.c_int),
+        "hv_fp8_gated": ([ctypes.c_int32, vp, u64, vp, u64, u64, u64, vp, u64, vp, vp], ctypes.c_int),
+        "hv_fp8_matmul_workspace_bytes": ([u64, u64, u64], sz),
+        "hv_fp8_matmul": ([ctypes.c_int32, vp, u64, vp, vp, u64, vp, u64, u64, u64, vp, u64, vp, sz, vp],
+                          ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -1091,3 +1104,156 @@ def verify(named_tensors, expected: bytes, chunk_bytes: int, alg: str = "sha256"
     root = v.manifest_root([t for _, t in items], chunk_bytes)
     if not v.verify_root(root, expected):
         raise VerificationError("model root does not match the expected root")
+
+
+# --------------------------------------------------------------------------
+# 8-bit operators (include/hv_fp8.h): codes are torch.float8_e4m3fn tensors
+# [..., cols], scales contiguous float32, one for every 128 columns of a row
+# ([..., ceil(cols / 128)]) or for every block of 128 x 128
+# ([ceil(rows / 128), ceil(cols / 128)]).
+
+def _device_of(t, what: str):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    return t.device
+
+
+def _matrix(t, dtypes, what: str, device, shape=None) -> tuple:
+    """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
+    lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
+    what it is given, so anything it would overrun or misread is refused here."""
+    if _device_of(t, what) != device:
+        raise ValueError(f"{what} is on {t.device}, but the call runs on {device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
+    if shape is not None and t.shape != torch.Size(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}; the call needs {tuple(shape)}")
+    if t.dim() == 0:
+        raise ValueError(f"{what} has no dimensions")
+    cols = t.shape[-1]
+    rows = t.numel() // cols if cols else 0
+    ld = cols
+    if t.dim() == 2:
+        if cols > 1 and t.stride(1) != 1:
+            raise ValueError(f"{what}: the elements of a row must be adjacent")
+        if rows > 1:
+            ld = t.stride(0)
+        if ld < cols:
+            raise ValueError(f"{what}: rows overlap (stride {ld}, {cols} columns)")
+    elif not t.is_contiguous():
+        raise ValueError(f"{what} must be two-dimensional or contiguous")
+    return t.data_ptr(), ld, rows, cols
+
+
+def _groups(n: int) -> int:
+    return (n + HV_FP8_GROUP - 1) // HV_FP8_GROUP
+
+
+_CODES = (torch.float8_e4m3fn,)
+_SCALES = (torch.float32,)
+
+
+def _scales(t, what: str, device, shape) -> int:
+    ptr, ld, rows, cols = _matrix(t, _SCALES, what, device, shape)
+    if rows > 1 and ld != cols:
+        raise ValueError(f"{what} must be contiguous")
+    return ptr
+
+
+def _coded(shape, scales_shape, device, out, scales) -> tuple:
+    """(codes, scales, codes pointer, codes' leading dimension, scales pointer), allocated where not given."""
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
+        ptr, ld = out.data_ptr(), max(shape[-1], 1)
+    else:
+        ptr, ld, _, _ = _matrix(out, _CODES, "out", device, shape)
+    if scales is None:
+        scales = torch.empty(scales_shape, dtype=torch.float32, device=device)
+        scales_ptr = scales.data_ptr()
+    else:
+        scales_ptr = _scales(scales, "scales", device, scales_shape)
+    return out, scales, ptr, ld, scales_ptr
+
+
+def hv_fp8_quantize(x: torch.Tensor, tile: str = "rows", out=None, scales=None):
+    """(codes, scales) of ``x`` (bfloat16, float16 or float32): a scale for every 128 columns of a
+    row (``tile="rows"``, activations) or for every block of 128 x 128 of a two-dimensional ``x``
+    (``tile="blocks"``, weights)."""
+    if tile not in ("rows", "blocks"):
+        raise ValueError(f"unknown tile {tile!r}; expected 'rows' or 'blocks'")
+    dev = _device_of(x, "x")
+    ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
+    if tile == "blocks":
+        if x.dim() != 2:
+            raise ValueError("quantisation by blocks takes a two-dimensional x")
+        scales_shape = (_groups(x.shape[0]), _groups(cols))
+    else:
+        scales_shape = (*x.shape[:-1], _groups(cols))
+    out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x.shape, scales_shape, dev, out, scales)
+    _check(lib.hv_fp8_quantize(TYPES[x.dtype], ptr, ld, rows, cols, 1 if tile == "rows" else HV_FP8_GROUP, codes_ptr,
+                               ld_codes, scales_ptr, _stream(dev)))
+    return out, scales
+
+
+def hv_fp8_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual=None, out=None, scales=None,
+                    residual_out=None):
+    """(codes, scales, h): h = x + residual, its root-mean-square norm over the last dimension times
+    ``weight``, quantised by rows.  h comes back in x's type, for the next layer (``residual_out``
+    may be ``x`` or ``residual``, for the addition in place); without a residual it is None."""
+    dev = _device_of(x, "x")
+    ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
+    same = (x.dtype,)
+    weight_ptr = _matrix(weight, same, "weight", dev, (cols,))[0]
+    res_ptr, ld_res, h_ptr, ld_h = None, 0, None, 0
+    if residual is not None:
+        res_ptr, ld_res, _, _ = _matrix(residual, same, "residual", dev, x.shape)
+        if residual_out is None:
+            residual_out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        h_ptr, ld_h, _, _ = _matrix(residual_out, same, "residual_out", dev, x.shape)
+    elif residual_out is not None:
+        raise ValueError("residual_out without a residual")
+    out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x.shape, (*x.shape[:-1], _groups(cols)), dev, out, scales)
+    _check(lib.hv_fp8_rms_norm(TYPES[x.dtype], ptr, ld, res_ptr, ld_res, weight_ptr, eps, rows, cols, h_ptr, ld_h,
+                               codes_ptr, ld_codes, scales_ptr, _stream(dev)))
+    return out, scales, residual_out
+
+
+def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
+    """(codes, scales) of silu(gate) * up, quantised by rows.  ``gate`` and ``up`` may be the halves
+    of one product's columns."""
+    dev = _device_of(gate, "gate")
+    ptr, ld, rows, cols = _matrix(gate, TYPES, "gate", dev)
+    up_ptr, ld_up, _, _ = _matrix(up, (gate.dtype,), "up", dev, gate.shape)
+    out, scales, codes_ptr, ld_codes, scales_ptr = _coded(gate.shape, (*gate.shape[:-1], _groups(cols)), dev, out,
+                                                          scales)
+    _check(lib.hv_fp8_gated(TYPES[gate.dtype], ptr, ld, up_ptr, ld_up, rows, cols, codes_ptr, ld_codes, scales_ptr,
+                            _stream(dev)))
+    return out, scales
+
+
+def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+                  dtype=torch.bfloat16, out=None, workspace: Workspace | None = None):
+    """a [..., k] times the transpose of b [n, k], both in codes, in ``dtype``: ``a_scales`` by rows
+    ([..., ceil(k / 128)]), ``b_scales`` by blocks ([ceil(n / 128), ceil(k / 128)])."""
+    if dtype not in TYPES:
+        raise ValueError(f"dtype is {dtype}; expected one of {[str(d) for d in TYPES]}")
+    dev = _device_of(a, "a")
+    a_ptr, ld_a, _, k = _matrix(a, _CODES, "a", dev)
+    b_ptr, ld_b, _, _ = _matrix(b, _CODES, "b", dev)
+    if b.dim() != 2 or b.shape[1] != k:
+        raise ValueError(f"b has shape {tuple(b.shape)}; the call needs [n, {k}]")
+    n = b.shape[0]
+    lead = a.shape[:-1]
+    m = lead.numel()
+    sa_ptr = _scales(a_scales, "a_scales", dev, (*lead, _groups(k)))
+    sb_ptr = _scales(b_scales, "b_scales", dev, (_groups(n), _groups(k)))
+    if out is None:
+        out = torch.empty((*lead, n), dtype=dtype, device=dev)
+        out_ptr, ld_out = out.data_ptr(), n
+    else:
+        out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", dev, (*lead, n))
+    need = lib.hv_fp8_matmul_workspace_bytes(m, n, k)
+    ws = (workspace or Workspace(dev)).get(need) if need else None
+    _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
+                             ws.data_ptr() if need else None, ws.numel() if need else 0, _stream(dev)))
+    return out
