@@ -17,6 +17,7 @@ namespace {
 using int8x = __attribute__((ext_vector_type(8))) int;
 using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using int4x = __attribute__((ext_vector_type(4))) int;
 using float4x = __attribute__((ext_vector_type(4))) float;
 
 // The matrix unit adds the 16 products of a lane's 16 bytes in fixed point and
@@ -48,28 +49,25 @@ __device__ __forceinline__ float4x group_product<float>(int8x rows, int8x cols) 
     return sum;
 }
 
-// A lane's part of a 16-row fragment over a group: 16 bytes from p and 16 from
-// p + 64 (which columns a lane holds does not matter, as long as both
-// operands go by the same rule).  left: bytes of the row from p on, the rest
-// reads as zeros.
-__device__ __forceinline__ int8x load_fragment(const uint8_t* p, int left) {
-    int8x f = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (left >= 80) {
+// 16 bytes of a row that has `left` bytes from p on; zeros beyond them.
+__device__ __forceinline__ int4x load_16(const uint8_t* p, int left) {
+    int4x f = {0, 0, 0, 0};
+    if (left >= 16) {
         __builtin_memcpy(&f, p, 16);
-        __builtin_memcpy((char*)&f + 16, p + 64, 16);
     } else {
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            uint32_t v = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int at = (w >= 4 ? 64 - 16 : 0) + 4 * w + b;
-                if (at < left) v |= (uint32_t)p[at] << (8 * b);
-            }
-            f[w] = (int)v;
-        }
+        for (int b = 0; b < 15; ++b)
+            if (b < left) f[b / 4] |= (int)p[b] << (8 * (b % 4));
     }
     return f;
+}
+
+// A lane's part of a 16-row fragment over a group: 16 bytes from p and 16 from
+// p + 64 (which columns a lane holds does not matter, as long as both
+// operands go by the same rule).
+__device__ __forceinline__ int8x load_fragment(const uint8_t* p, int left) {
+    const int4x lo = load_16(p, left), hi = load_16(p + 64, left - 64);
+    return int8x{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 
 template <typename T>
@@ -121,11 +119,241 @@ __global__ void __launch_bounds__(256) stream_kernel(const uint8_t* __restrict__
     }
 }
 
+// ---------------------------------------------------------------------------
+// tiles in LDS
+
+constexpr uint64_t kMaxTileLd = (1 << 23) - 1;  // offsets within a tile's 256 rows stay below 2^31
+
+// A buffer that starts at p; its loads' offsets are in bounds by construction.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000);
+}
+
+// kBytes per lane from the buffer to consecutive places in LDS.
+template <int kBytes>
+__device__ __forceinline__ void buffer_to_lds(__amdgpu_buffer_rsrc_t from, void* lds, uint32_t lane_offset,
+                                              uint32_t offset) {
+#ifdef __HIP_DEVICE_COMPILE__  // the host pass does not know this builtin, and would drop the kernel for it
+    if constexpr (kBytes == 16)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, lane_offset, offset, 0, 0);
+    else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, lane_offset, offset, 0, 0);
+#endif
+}
+
+// A workgroup makes TM x TN outputs, WM x WN waves a part each.  While one
+// group's rows of A and B (128 bytes each) are multiplied, the next group's go
+// from memory to the other half of the LDS.
+template <typename T, int TM, int TN, int WM, int WN, bool kDirect>
+__global__ void __launch_bounds__(WM* WN * 64)
+    tile_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
+                const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
+                uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m, uint32_t tiles) {
+    constexpr int kThreads = WM * WN * 64;
+    constexpr int MT = TM / WM / 16, NT = TN / WN / 16;
+    constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte loads of a lane
+    static_assert(TN / WN <= kFp8Group && kFp8Group % (TN / WN) == 0, "a wave's columns share a scale");
+    constexpr int kScales = TM + 64;  // A's, then B's
+    static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
+    __shared__ alignas(1024) uint8_t a0[TM * 128], b0[TN * 128], a1[TM * 128], b1[TN * 128];
+    __shared__ alignas(256) float s0[kScales], s1[kScales];
+
+    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles
+    // that share rows of B, and its L2 serves those once.
+    const uint32_t per_xcd = gridDim.x / 8;
+    const uint32_t tile = blockIdx.x % 8 * per_xcd + blockIdx.x / 8;
+    if (tile >= tiles) return;
+    const uint32_t i0 = tile % tiles_m * TM, j0 = tile / tiles_m * TN;
+
+    const uint32_t lane = threadIdx.x % 64;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t wave_i = wave / WN * (TM / WM), wave_j = wave % WN * (TN / WN);
+    const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;
+
+    // The row of LDS that a lane of load instruction l fills is 8 * (l * waves + wave) + lane / 8; its
+    // 16-byte places hold the row's chunks in the order place ^ (row % 8), so that
+    // the lanes of a fragment read from different banks.
+    const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+    const uint8_t* const tile_a = a + i0 * ld_a;
+    const uint8_t* const tile_b = b + j0 * ld_b;
+    uint32_t from_a[kLoadsA], from_b[kLoadsB];
+#pragma unroll
+    for (int l = 0; l < kLoadsA; ++l)
+        from_a[l] = min(8 * (l * WM * WN + wave) + lane / 8, m - 1 - i0) * (uint32_t)ld_a + chunk;
+#pragma unroll
+    for (int l = 0; l < kLoadsB; ++l)
+        from_b[l] = min(8 * (l * WM * WN + wave) + lane / 8, n - 1 - j0) * (uint32_t)ld_b + chunk;
+    const uint32_t part_s = wave % (kScales / 64);  // waves beyond them load a part again
+    const bool scales_of_a = part_s < TM / 64;
+    const float* const tile_s = scales_of_a ? sa + (uint64_t)i0 * groups : sb + (uint64_t)(j0 / kFp8Group) * groups;
+    const uint32_t from_s = (scales_of_a ? min(part_s * 64 + lane, m - 1 - i0)
+                                         : min(lane, (n - 1) / kFp8Group - j0 / kFp8Group)) * groups * 4;
+
+    // Buffer loads: a lane's offset stays, the group's is a scalar.
+    const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b), all_s = rows_at(tile_s);
+    auto load = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
+#pragma unroll
+        for (int l = 0; l < kLoadsA; ++l)
+            buffer_to_lds<16>(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l)
+            buffer_to_lds<16>(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
+        buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4);
+    };
+    // The columns beyond the last whole group, with zeros after them.
+    auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
+        const uint32_t at = g * kFp8Group;
+        const int left = (int)(k - at) - (int)chunk;
+#pragma unroll
+        for (int l = 0; l < kLoadsA; ++l)
+            *(int4x*)(la + 1024 * (l * WM * WN + wave) + 16 * lane) = load_16(tile_a + at + from_a[l], left);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l)
+            *(int4x*)(lb + 1024 * (l * WM * WN + wave) + 16 * lane) = load_16(tile_b + at + from_b[l], left);
+        ls[64 * part_s + lane] = tile_s[from_s / 4 + g];
+    };
+
+    float4x sum[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sum[i][j] = float4x{0, 0, 0, 0};
+    // Where the lane reads its fragments: 16 bytes at *_lo and 16 at *_hi, from the
+    // first row of the wave's part on.  The empty asm keeps them whole, so that a read's
+    // row is an offset in its instruction and takes no register.
+    const uint32_t row16 = lane % 16, quarter = lane / 16;
+    const uint32_t place = row16 * 128 + (quarter ^ row16 % 8) * 16;
+    uint32_t a_lo = wave_i * 128 + place, a_hi = wave_i * 128 + (place ^ 64);
+    uint32_t b_lo = wave_j * 128 + place, b_hi = wave_j * 128 + (place ^ 64);
+    uint32_t a_scale = wave_i + row16;
+    asm("" : "+v"(a_lo), "+v"(a_hi), "+v"(b_lo), "+v"(b_hi), "+v"(a_scale));
+    auto fragment = [&](const uint8_t* rows, uint32_t at_lo, uint32_t at_hi) {
+        const int4x lo = *(const int4x*)(rows + at_lo), hi = *(const int4x*)(rows + at_hi);
+        return int8x{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    auto fragment_a = [&](const uint8_t* la, int i) { return fragment(la + 2048 * i, a_lo, a_hi); };
+    auto fragment_b = [&](const uint8_t* lb, int j) { return fragment(lb + 2048 * j, b_lo, b_hi); };
+    auto arrived = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's loads are in LDS
+        __syncthreads();
+    };
+
+    // One group.  The fragments of A's next 16 rows come from LDS while these are
+    // multiplied, and the next group's first ones while this group's last are.  By
+    // then every wave has read all it needs of this half of the LDS, so the group
+    // after the next may be loaded into it (past the last one, the last one again:
+    // nobody reads it).  A product is added to its sum two instructions later, when
+    // the matrix unit has it.
+    const uint32_t whole = k / kFp8Group;
+    int8x fb[NT], fa;
+    float scale_a, scale_b;
+    auto first = [&](const uint8_t* la, const uint8_t* lb, const float* ls) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = fragment_b(lb, j);
+        fa = fragment_a(la, 0);
+        scale_a = ls[a_scale];
+        scale_b = ls[TM + wave_j / kFp8Group];
+    };
+    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls, const uint8_t* next_a, const uint8_t* next_b,
+                        const float* next_s) {
+        const float in_b = scale_b;
+        float4x p[3];
+        float s[2];
+        auto add = [&](int t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum[t / NT][t % NT][e] = fmaf(p[t % 3][e], s[t / NT % 2], sum[t / NT][t % NT][e]);
+        };
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const bool last = i == MT - 1;
+            if (last) {
+                arrived();
+                load(min(g + 2, whole - 1), la, lb, ls);
+                scale_b = next_s[TM + wave_j / kFp8Group];
+            }
+            const int8x next_fa = last ? fragment_a(next_a, 0) : fragment_a(la, i + 1);
+            const float next_scale = last ? next_s[a_scale] : ls[a_scale + 16 * (i + 1)];
+            s[i % 2] = scale_a * in_b;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int t = i * NT + j;
+                p[t % 3] = group_product<T>(fb[j], fa);
+                if (last) fb[j] = fragment_b(next_b, j);
+                if (t >= 2) add(t - 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            fa = next_fa;
+            scale_a = next_scale;
+        }
+        add(MT * NT - 2);
+        add(MT * NT - 1);
+    };
+
+    if (whole > 0) {
+        load(0, a0, b0, s0);
+        arrived();
+        load(min(1u, whole - 1), a1, b1, s1);
+        first(a0, b0, s0);
+        for (uint32_t g = 0; g + 1 < whole; g += 2) {
+            multiply(g, a0, b0, s0, a1, b1, s1);
+            multiply(g + 1, a1, b1, s1, a0, b0, s0);
+        }
+        if (whole % 2 != 0) multiply(whole - 1, a0, b0, s0, a1, b1, s1);
+        arrived();
+    }
+    if (whole < groups) {
+        load_rest(whole, a0, b0, s0);
+        __syncthreads();
+        first(a0, b0, s0);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int8x rest = fragment_a(a0, i);
+            const float s = s0[a_scale + 16 * i] * scale_b;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const float4x p = group_product<T>(fb[j], rest);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
+            }
+        }
+    }
+    const bool inside = i0 + TM <= m && j0 + TN <= n;
+    T* const out = c + (uint64_t)(i0 + wave_i + row16) * ld_c + j0 + wave_j + quarter * 4;
+    const int rows_left = (int)(m - i0 - wave_i - row16), cols_left = (int)(n - j0 - wave_j - quarter * 4);
+    if (inside) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) store_four(out + 16 * i * ld_c + 16 * j, 4, sum[i][j]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (16 * i < rows_left && 16 * j + e < cols_left)
+                        out[16 * i * ld_c + 16 * j + e] = (T)sum[i][j][e];
+    }
+}
+
 }  // namespace
 
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s) {
     auto run = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
+        const bool direct = a.ld_a % 16 == 0 && a.ld_b % 16 == 0 && (uintptr_t)a.a % 16 == 0 && (uintptr_t)a.b % 16 == 0 &&
+                            a.ld_a <= kMaxTileLd && a.ld_b <= kMaxTileLd;
+        if (direct && a.m > 64 && a.k > 0) {
+            constexpr int TM = sizeof(T) == 4 ? 128 : 256, TN = TM;
+            const uint32_t tiles_m = (uint32_t)((a.m + TM - 1) / TM);
+            const uint32_t tiles = tiles_m * (uint32_t)((a.n + TN - 1) / TN);
+            tile_kernel<T, TM, TN, 2, TN / 64, true><<<(tiles + 7) / 8 * 8, TN / 64 * 128, 0, s>>>(
+                a.a, a.ld_a, a.a_scales, a.b, a.ld_b, a.b_scales, (uint32_t)a.m, (uint32_t)a.n, (uint32_t)a.k, (T*)a.c,
+                a.ld_c, tiles_m, tiles);
+            return hipGetLastError();
+        }
         const dim3 grid((uint32_t)((a.n + 15) / 16), (uint32_t)((a.m + 15) / 16));
         stream_kernel<T><<<grid, 256, 0, s>>>(a.a, a.ld_a, a.a_scales, a.b, a.ld_b, a.b_scales, (uint32_t)a.m,
                                               (uint32_t)a.n, (uint32_t)a.k, (T*)a.c, a.ld_c);
