@@ -191,14 +191,14 @@ __global__ void __launch_bounds__(WM* WN * 64)
 
     // Buffer loads: a lane's offset stays, the group's is a scalar.
     const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b), all_s = rows_at(tile_s);
-    auto load = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
-#pragma unroll
-        for (int l = 0; l < kLoadsA; ++l)
+    constexpr int kLoads = kLoadsA + kLoadsB + 1;
+    auto load = [&](int l, uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
+        if (l < kLoadsA)
             buffer_to_lds<16>(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l)
-            buffer_to_lds<16>(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
-        buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4);
+        else if (l < kLoadsA + kLoadsB)
+            buffer_to_lds<16>(all_b, lb + 1024 * ((l - kLoadsA) * WM * WN + wave), from_b[l - kLoadsA], g * kFp8Group);
+        else
+            buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4);
     };
     // The columns beyond the last whole group, with zeros after them.
     auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
@@ -242,8 +242,9 @@ __global__ void __launch_bounds__(WM* WN * 64)
     // multiplied, and the next group's first ones while this group's last are.  By
     // then every wave has read all it needs of this half of the LDS, so the group
     // after the next may be loaded into it (past the last one, the last one again:
-    // nobody reads it).  A product is added to its sum two instructions later, when
-    // the matrix unit has it.
+    // nobody reads it), a load after each product so that no wave stands in line to
+    // issue them.  A product is added to its sum two instructions later, when the
+    // matrix unit has it.
     const uint32_t whole = k / kFp8Group;
     int8x fb[NT], fa;
     float scale_a, scale_b;
@@ -254,8 +255,8 @@ __global__ void __launch_bounds__(WM* WN * 64)
         scale_a = ls[a_scale];
         scale_b = ls[TM + wave_j / kFp8Group];
     };
-    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls, const uint8_t* next_a, const uint8_t* next_b,
-                        const float* next_s) {
+    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls, uint8_t* next_a, uint8_t* next_b,
+                        float* next_s) {
         const float in_b = scale_b;
         float4x p[3];
         float s[2];
@@ -269,7 +270,6 @@ __global__ void __launch_bounds__(WM* WN * 64)
             const bool last = i == MT - 1;
             if (last) {
                 arrived();
-                load(min(g + 2, whole - 1), la, lb, ls);
                 scale_b = next_s[TM + wave_j / kFp8Group];
             }
             const int8x next_fa = last ? fragment_a(next_a, 0) : fragment_a(la, i + 1);
@@ -279,7 +279,12 @@ __global__ void __launch_bounds__(WM* WN * 64)
             for (int j = 0; j < NT; ++j) {
                 const int t = i * NT + j;
                 p[t % 3] = group_product<T>(fb[j], fa);
-                if (last) fb[j] = fragment_b(next_b, j);
+                if (last) {
+                    fb[j] = fragment_b(next_b, j);
+                    load(j, min(g + 2, whole - 1), la, lb, ls);
+                } else if (t + NT < kLoads) {
+                    load(t + NT, min(g + 1, whole - 1), next_a, next_b, next_s);
+                }
                 if (t >= 2) add(t - 2);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -291,9 +296,11 @@ __global__ void __launch_bounds__(WM* WN * 64)
     };
 
     if (whole > 0) {
-        load(0, a0, b0, s0);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) load(l, 0, a0, b0, s0);
         arrived();
-        load(min(1u, whole - 1), a1, b1, s1);
+#pragma unroll
+        for (int l = 0; l < NT; ++l) load(l, min(1u, whole - 1), a1, b1, s1);
         first(a0, b0, s0);
         for (uint32_t g = 0; g + 1 < whole; g += 2) {
             multiply(g, a0, b0, s0, a1, b1, s1);
