@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(WM* WN * 64)
     static_assert(TN / WN <= kFp8Group && kFp8Group % (TN / WN) == 0, "a wave's columns share a scale");
     constexpr int kScales = TM + 64;  // A's, then B's
     static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
+    static_assert(MT >= 3 && kLoadsA <= NT && kLoadsB <= (MT - 2) * NT, "a group's loads fit between its products");
     __shared__ alignas(1024) uint8_t a0[TM * 128], b0[TN * 128], a1[TM * 128], b1[TN * 128];
     __shared__ alignas(256) float s0[kScales], s1[kScales];
 
@@ -191,15 +192,13 @@ __global__ void __launch_bounds__(WM* WN * 64)
 
     // Buffer loads: a lane's offset stays, the group's is a scalar.
     const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b), all_s = rows_at(tile_s);
-    constexpr int kLoads = kLoadsA + kLoadsB + 1;
-    auto load = [&](int l, uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
-        if (l < kLoadsA)
-            buffer_to_lds<16>(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
-        else if (l < kLoadsA + kLoadsB)
-            buffer_to_lds<16>(all_b, lb + 1024 * ((l - kLoadsA) * WM * WN + wave), from_b[l - kLoadsA], g * kFp8Group);
-        else
-            buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4);
+    auto load_a = [&](int l, uint32_t g, uint8_t* la) {
+        buffer_to_lds<16>(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
     };
+    auto load_b = [&](int l, uint32_t g, uint8_t* lb) {
+        buffer_to_lds<16>(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
+    };
+    auto load_s = [&](uint32_t g, float* ls) { buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4); };
     // The columns beyond the last whole group, with zeros after them.
     auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
         const uint32_t at = g * kFp8Group;
@@ -233,18 +232,25 @@ __global__ void __launch_bounds__(WM* WN * 64)
     };
     auto fragment_a = [&](const uint8_t* la, int i) { return fragment(la + 2048 * i, a_lo, a_hi); };
     auto fragment_b = [&](const uint8_t* lb, int j) { return fragment(lb + 2048 * j, b_lo, b_hi); };
-    auto arrived = [&]() {
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's loads are in LDS
-        __syncthreads();
+    // Every wave's loads but its last kLater are in LDS, and no wave reads what it read before.
+    auto meet = [&](auto later) {
+        constexpr int kLater = decltype(later)::value;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((kLater & 15) | (kLater >> 4) << 14 | 7 << 4);  // vmcnt(kLater), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
+    constexpr std::integral_constant<int, 0> kNone;
+    constexpr std::integral_constant<int, kLoadsB> kOfB;
 
     // One group.  The fragments of A's next 16 rows come from LDS while these are
     // multiplied, and the next group's first ones while this group's last are.  By
-    // then every wave has read all it needs of this half of the LDS, so the group
-    // after the next may be loaded into it (past the last one, the last one again:
-    // nobody reads it), a load after each product so that no wave stands in line to
-    // issue them.  A product is added to its sum two instructions later, when the
-    // matrix unit has it.
+    // then every wave has read all it needs of this half's A, so the group after
+    // the next may be loaded there; of B every wave holds all it needs from the
+    // start, so the group after the next is loaded over it as soon as they have met.
+    // (Past the last group the last one is loaded again: nobody reads it.)  Loads are
+    // issued one after each product, so that no wave stands in line for them.  A
+    // product is added to its sum two instructions later, when the matrix unit has it.
     const uint32_t whole = k / kFp8Group;
     int8x fb[NT], fa;
     float scale_a, scale_b;
@@ -268,8 +274,9 @@ __global__ void __launch_bounds__(WM* WN * 64)
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const bool last = i == MT - 1;
+            if (i == 1) meet(std::integral_constant<int, 63>{});
             if (last) {
-                arrived();
+                meet(kOfB);
                 scale_b = next_s[TM + wave_j / kFp8Group];
             }
             const int8x next_fa = last ? fragment_a(next_a, 0) : fragment_a(la, i + 1);
@@ -279,11 +286,14 @@ __global__ void __launch_bounds__(WM* WN * 64)
             for (int j = 0; j < NT; ++j) {
                 const int t = i * NT + j;
                 p[t % 3] = group_product<T>(fb[j], fa);
+                __builtin_amdgcn_sched_barrier(0);
                 if (last) {
                     fb[j] = fragment_b(next_b, j);
-                    load(j, min(g + 2, whole - 1), la, lb, ls);
-                } else if (t + NT < kLoads) {
-                    load(t + NT, min(g + 1, whole - 1), next_a, next_b, next_s);
+                    if (j < kLoadsA) load_a(j, min(g + 2, whole - 1), la);
+                } else if (t == 0) {
+                    load_s(min(g + 1, whole - 1), next_s);
+                } else if (i >= 1 && t - NT < kLoadsB) {
+                    load_b(t - NT, min(g + 2, whole - 1), lb);
                 }
                 if (t >= 2) add(t - 2);
                 __builtin_amdgcn_sched_barrier(0);
@@ -296,18 +306,24 @@ __global__ void __launch_bounds__(WM* WN * 64)
     };
 
     if (whole > 0) {
+        const uint32_t second = min(1u, whole - 1);
 #pragma unroll
-        for (int l = 0; l < kLoads; ++l) load(l, 0, a0, b0, s0);
-        arrived();
+        for (int l = 0; l < kLoadsA; ++l) load_a(l, 0, a0);
 #pragma unroll
-        for (int l = 0; l < NT; ++l) load(l, min(1u, whole - 1), a1, b1, s1);
+        for (int l = 0; l < kLoadsB; ++l) load_b(l, 0, b0);
+        load_s(0, s0);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l) load_b(l, second, b1);
+        meet(kOfB);
+#pragma unroll
+        for (int l = 0; l < kLoadsA; ++l) load_a(l, second, a1);
         first(a0, b0, s0);
         for (uint32_t g = 0; g + 1 < whole; g += 2) {
             multiply(g, a0, b0, s0, a1, b1, s1);
             multiply(g + 1, a1, b1, s1, a0, b0, s0);
         }
         if (whole % 2 != 0) multiply(whole - 1, a0, b0, s0, a1, b1, s1);
-        arrived();
+        meet(kNone);
     }
     if (whole < groups) {
         load_rest(whole, a0, b0, s0);
