@@ -55,9 +55,13 @@ __device__ __forceinline__ int4x load_16(const uint8_t* p, int left) {
     if (left >= 16) {
         __builtin_memcpy(&f, p, 16);
     } else {
-#pragma unroll
-        for (int b = 0; b < 15; ++b)
-            if (b < left) f[b / 4] |= (int)p[b] << (8 * (b % 4));
+        uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+        for (int b = left - 1; b >= 0; --b) {
+            hi = hi << 8 | lo >> 56;
+            lo = lo << 8 | p[b];
+        }
+        f = int4x{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
     }
     return f;
 }
@@ -129,15 +133,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000);
 }
 
-// kBytes per lane from the buffer to consecutive places in LDS.
-template <int kBytes>
+// 16 bytes a lane from the buffer to consecutive places in LDS.
 __device__ __forceinline__ void buffer_to_lds(__amdgpu_buffer_rsrc_t from, void* lds, uint32_t lane_offset,
                                               uint32_t offset) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host pass does not know this builtin, and would drop the kernel for it
-    if constexpr (kBytes == 16)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, lane_offset, offset, 0, 0);
-    else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, lane_offset, offset, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, lane_offset, offset, 0, 0);
 #endif
 }
 
@@ -157,14 +157,18 @@ __global__ void __launch_bounds__(WM* WN * 64)
     static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
     static_assert(MT >= 3 && kLoadsA <= NT && kLoadsB <= (MT - 2) * NT, "a group's loads fit between its products");
     __shared__ alignas(1024) uint8_t a0[TM * 128], b0[TN * 128], a1[TM * 128], b1[TN * 128];
-    __shared__ alignas(256) float s0[kScales], s1[kScales];
+    __shared__ alignas(256) float4x scales[2][kScales];  // of four groups, and of the next four
 
-    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles
-    // that share rows of B, and its L2 serves those once.
+    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, in
+    // panels of 8 tiles' rows, so that the 32 it has at a time are 8 x 4 and its L2
+    // serves each row of A and B several times.
     const uint32_t per_xcd = gridDim.x / 8;
     const uint32_t tile = blockIdx.x % 8 * per_xcd + blockIdx.x / 8;
     if (tile >= tiles) return;
-    const uint32_t i0 = tile % tiles_m * TM, j0 = tile / tiles_m * TN;
+    const uint32_t tiles_n = tiles / tiles_m;
+    const uint32_t panel = tile / (8 * tiles_n), in_panel = tile - panel * 8 * tiles_n;
+    const uint32_t panel_rows = min(8u, tiles_m - panel * 8);
+    const uint32_t i0 = (panel * 8 + in_panel % panel_rows) * TM, j0 = in_panel / panel_rows * TN;
 
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -188,19 +192,29 @@ __global__ void __launch_bounds__(WM* WN * 64)
     const bool scales_of_a = part_s < TM / 64;
     const float* const tile_s = scales_of_a ? sa + (uint64_t)i0 * groups : sb + (uint64_t)(j0 / kFp8Group) * groups;
     const uint32_t from_s = (scales_of_a ? min(part_s * 64 + lane, m - 1 - i0)
-                                         : min(lane, (n - 1) / kFp8Group - j0 / kFp8Group)) * groups * 4;
+                                         : min(lane, (n - 1) / kFp8Group - j0 / kFp8Group)) * groups;
 
     // Buffer loads: a lane's offset stays, the group's is a scalar.
-    const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b), all_s = rows_at(tile_s);
+    const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b);
     auto load_a = [&](int l, uint32_t g, uint8_t* la) {
-        buffer_to_lds<16>(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
+        buffer_to_lds(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
     };
     auto load_b = [&](int l, uint32_t g, uint8_t* lb) {
-        buffer_to_lds<16>(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
+        buffer_to_lds(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
     };
-    auto load_s = [&](uint32_t g, float* ls) { buffer_to_lds<4>(all_s, ls + 64 * part_s, from_s, g * 4); };
+    // Scales come four groups at a time (a load of one group's takes as many
+    // requests as a load of a tile's 128-byte rows), the last four of a row where
+    // there are fewer left, and are kept in LDS as [row][4].
+    const uint32_t last_four = max(groups, 4u) - 4;
+    float4x four;
+    auto load_four = [&](uint32_t q) { __builtin_memcpy(&four, tile_s + from_s + min(4 * q, last_four), 16); };
+    auto keep_four = [&](uint32_t q) { scales[q % 2][64 * part_s + lane] = four; };
+    // where group g's scales stand, from a row's first one on
+    auto scales_at = [&](uint32_t g) {
+        return (const float*)scales + (g / 4 % 2 * kScales * 4 + g - min(g / 4 * 4, last_four));
+    };
     // The columns beyond the last whole group, with zeros after them.
-    auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls) {
+    auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb) {
         const uint32_t at = g * kFp8Group;
         const int left = (int)(k - at) - (int)chunk;
 #pragma unroll
@@ -209,7 +223,6 @@ __global__ void __launch_bounds__(WM* WN * 64)
 #pragma unroll
         for (int l = 0; l < kLoadsB; ++l)
             *(int4x*)(lb + 1024 * (l * WM * WN + wave) + 16 * lane) = load_16(tile_b + at + from_b[l], left);
-        ls[64 * part_s + lane] = tile_s[from_s / 4 + g];
     };
 
     float4x sum[MT][NT];
@@ -224,7 +237,7 @@ __global__ void __launch_bounds__(WM* WN * 64)
     const uint32_t place = row16 * 128 + (quarter ^ row16 % 8) * 16;
     uint32_t a_lo = wave_i * 128 + place, a_hi = wave_i * 128 + (place ^ 64);
     uint32_t b_lo = wave_j * 128 + place, b_hi = wave_j * 128 + (place ^ 64);
-    uint32_t a_scale = wave_i + row16;
+    uint32_t a_scale = 4 * (wave_i + row16);
     asm("" : "+v"(a_lo), "+v"(a_hi), "+v"(b_lo), "+v"(b_hi), "+v"(a_scale));
     auto fragment = [&](const uint8_t* rows, uint32_t at_lo, uint32_t at_hi) {
         const int4x lo = *(const int4x*)(rows + at_lo), hi = *(const int4x*)(rows + at_hi);
@@ -254,15 +267,19 @@ __global__ void __launch_bounds__(WM* WN * 64)
     const uint32_t whole = k / kFp8Group;
     int8x fb[NT], fa;
     float scale_a, scale_b;
-    auto first = [&](const uint8_t* la, const uint8_t* lb, const float* ls) {
+    const uint32_t b_scale = 4 * (TM + wave_j / kFp8Group);
+    auto first = [&](const uint8_t* la, const uint8_t* lb, uint32_t g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) fb[j] = fragment_b(lb, j);
         fa = fragment_a(la, 0);
-        scale_a = ls[a_scale];
-        scale_b = ls[TM + wave_j / kFp8Group];
+        scale_a = scales_at(g)[a_scale];
+        scale_b = scales_at(g)[b_scale];
     };
-    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, float* ls, uint8_t* next_a, uint8_t* next_b,
-                        float* next_s) {
+    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, const uint8_t* next_a, const uint8_t* next_b) {
+        const bool new_four = g % 4 == 1 && g / 4 * 4 + 4 < groups;
+        const float* const now = scales_at(g);
+        const float* const next = scales_at(g + 1);
+        if (new_four) load_four(g / 4 + 1);
         const float in_b = scale_b;
         float4x p[3];
         float s[2];
@@ -270,6 +287,7 @@ __global__ void __launch_bounds__(WM* WN * 64)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 sum[t / NT][t % NT][e] = fmaf(p[t % 3][e], s[t / NT % 2], sum[t / NT][t % NT][e]);
+            asm volatile("" : "+v"(sum[t / NT][t % NT]));  // here, not after a later branch
         };
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -277,10 +295,11 @@ __global__ void __launch_bounds__(WM* WN * 64)
             if (i == 1) meet(std::integral_constant<int, 63>{});
             if (last) {
                 meet(kOfB);
-                scale_b = next_s[TM + wave_j / kFp8Group];
+                if (new_four) keep_four(g / 4 + 1);
+                scale_b = next[b_scale];
             }
             const int8x next_fa = last ? fragment_a(next_a, 0) : fragment_a(la, i + 1);
-            const float next_scale = last ? next_s[a_scale] : ls[a_scale + 16 * (i + 1)];
+            const float next_scale = last ? next[a_scale] : now[a_scale + 64 * (i + 1)];
             s[i % 2] = scale_a * in_b;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -290,8 +309,6 @@ __global__ void __launch_bounds__(WM* WN * 64)
                 if (last) {
                     fb[j] = fragment_b(next_b, j);
                     if (j < kLoadsA) load_a(j, min(g + 2, whole - 1), la);
-                } else if (t == 0) {
-                    load_s(min(g + 1, whole - 1), next_s);
                 } else if (i >= 1 && t - NT < kLoadsB) {
                     load_b(t - NT, min(g + 2, whole - 1), lb);
                 }
@@ -305,34 +322,35 @@ __global__ void __launch_bounds__(WM* WN * 64)
         add(MT * NT - 1);
     };
 
+    for (uint32_t e = 0; e < 4; ++e) four[e] = e < groups ? tile_s[from_s + e] : 0.0f;
+    keep_four(0);
     if (whole > 0) {
         const uint32_t second = min(1u, whole - 1);
 #pragma unroll
         for (int l = 0; l < kLoadsA; ++l) load_a(l, 0, a0);
 #pragma unroll
         for (int l = 0; l < kLoadsB; ++l) load_b(l, 0, b0);
-        load_s(0, s0);
 #pragma unroll
         for (int l = 0; l < kLoadsB; ++l) load_b(l, second, b1);
         meet(kOfB);
 #pragma unroll
         for (int l = 0; l < kLoadsA; ++l) load_a(l, second, a1);
-        first(a0, b0, s0);
+        first(a0, b0, 0);
         for (uint32_t g = 0; g + 1 < whole; g += 2) {
-            multiply(g, a0, b0, s0, a1, b1, s1);
-            multiply(g + 1, a1, b1, s1, a0, b0, s0);
+            multiply(g, a0, b0, a1, b1);
+            multiply(g + 1, a1, b1, a0, b0);
         }
-        if (whole % 2 != 0) multiply(whole - 1, a0, b0, s0, a1, b1, s1);
+        if (whole % 2 != 0) multiply(whole - 1, a0, b0, a1, b1);
         meet(kNone);
     }
     if (whole < groups) {
-        load_rest(whole, a0, b0, s0);
+        load_rest(whole, a0, b0);
         __syncthreads();
-        first(a0, b0, s0);
+        first(a0, b0, whole);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int8x rest = fragment_a(a0, i);
-            const float s = s0[a_scale + 16 * i] * scale_b;
+            const float s = scales_at(whole)[a_scale + 64 * i] * scale_b;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const float4x p = group_product<T>(fb[j], rest);
