@@ -74,6 +74,13 @@ __device__ __forceinline__ int8x load_fragment(const uint8_t* p, int left) {
     return int8x{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 
+__device__ __forceinline__ int8x load_whole(const uint8_t* p) {
+    int8x f;
+    __builtin_memcpy(&f, p, 16);
+    __builtin_memcpy((char*)&f + 16, p + 64, 16);
+    return f;
+}
+
 template <typename T>
 __device__ __forceinline__ void store_four(T* p, int valid, float4x v) {
     T o[4];
@@ -88,38 +95,110 @@ __device__ __forceinline__ void store_four(T* p, int valid, float4x v) {
     }
 }
 
-// A workgroup makes 16 x 16 outputs; its four waves take every fourth group of
-// columns, straight from memory, and join their sums through LDS.
-template <typename T>
-__global__ void __launch_bounds__(256) stream_kernel(const uint8_t* __restrict__ a, uint64_t ld_a,
-                                                     const float* __restrict__ sa, const uint8_t* __restrict__ b,
-                                                     uint64_t ld_b, const float* __restrict__ sb, uint32_t m,
-                                                     uint32_t n, uint32_t k, T* __restrict__ c, uint64_t ld_c) {
-    __shared__ float4x part[4][64];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t i0 = blockIdx.y * 16, j0 = blockIdx.x * 16;
-    const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;
-    const uint32_t i = min(i0 + lane % 16, m - 1), j = min(j0 + lane % 16, n - 1);
+// ---------------------------------------------------------------------------
+// few rows: B straight from memory
+
+// A workgroup makes MT x NT fragments of 16 x 16 outputs; its waves take the
+// groups of columns in turn and join their sums through LDS.  Nothing is
+// shared between waves but A, which the caches hold, so B goes to registers with
+// kAhead groups on their way per wave.
+constexpr int kStreamWaves = 8;
+
+template <typename T, int MT, int NT, int kAhead>
+__global__ void __launch_bounds__(kStreamWaves * 64)
+    stream_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
+                  const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
+                  uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m) {
+    __shared__ float4x part[kStreamWaves][MT * NT][64];
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t i0 = blockIdx.x % tiles_m * 16 * MT, j0 = blockIdx.x / tiles_m * 16 * NT;
+    const uint32_t groups = (k + kFp8Group - 1) / kFp8Group, whole = k / kFp8Group;
     const uint32_t at = lane / 16 * 16;
-    const uint8_t* pa = a + i * ld_a + at;
-    const uint8_t* pb = b + j * ld_b + at;
-    const float* psa = sa + (uint64_t)i * groups;
-    const float* psb = sb + (uint64_t)(j0 / kFp8Group) * groups;
-    float4x sum = {0, 0, 0, 0};
-    for (uint32_t g = wave; g < groups; g += 4) {
-        const int left = (int)(k - g * kFp8Group) - (int)at;
-        const float4x p = group_product<T>(load_fragment(pb + g * kFp8Group, left),
-                                           load_fragment(pa + g * kFp8Group, left));
-        const float s = psa[g] * psb[g];
+    const uint8_t *row_a[MT], *row_b[NT];
+    const float* scale_a[MT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = fmaf(p[e], s, sum[e]);
+    for (int i = 0; i < MT; ++i) {
+        const uint32_t row = min(i0 + 16 * i + lane % 16, m - 1);
+        row_a[i] = a + row * ld_a + at;
+        scale_a[i] = sa + (uint64_t)row * groups;
     }
-    part[wave][lane] = sum;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) row_b[j] = b + min(j0 + 16 * j + lane % 16, n - 1) * ld_b + at;
+    const float* scale_b[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) scale_b[j] = sb + (uint64_t)(min(j0 + 16 * j, n - 1) / kFp8Group) * groups;
+
+    float4x sum[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sum[i][j] = float4x{0, 0, 0, 0};
+    int8x fa[kAhead][MT], fb[kAhead][NT];
+    float in_a[kAhead][MT], in_b[kAhead][NT];
+    auto load = [&](int slot, uint32_t g) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            fb[slot][j] = load_whole(row_b[j] + g * kFp8Group);
+            in_b[slot][j] = scale_b[j][g];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            fa[slot][i] = load_whole(row_a[i] + g * kFp8Group);
+            in_a[slot][i] = scale_a[i][g];
+        }
+    };
+    auto multiply = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const float4x p = group_product<T>(fb[slot][j], fa[slot][i]);
+                const float s = in_a[slot][i] * in_b[slot][j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
+            }
+    };
+    // The wave's groups are wave, wave + kStreamWaves, ...; count of the whole ones among them.
+    const uint32_t count = whole > wave ? (whole - wave + kStreamWaves - 1) / kStreamWaves : 0;
+    auto load_next = [&](int slot, uint32_t index) {
+        if (index < count) load(slot, wave + index * kStreamWaves);
+    };
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) load_next(d, d);
+    uint32_t x = 0;
+    for (; x + kAhead <= count; x += kAhead)
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) {
+            multiply(d);
+            load_next(d, x + d + kAhead);
+        }
+#pragma unroll
+    for (int d = 0; d < kAhead - 1; ++d)
+        if (x + d < count) multiply(d);
+    if (whole < groups && whole % kStreamWaves == wave) {
+        const int left = (int)(k - whole * kFp8Group) - (int)at;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            fb[0][j] = load_fragment(row_b[j] + whole * kFp8Group, left);
+            in_b[0][j] = scale_b[j][whole];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            fa[0][i] = load_fragment(row_a[i] + whole * kFp8Group, left);
+            in_a[0][i] = scale_a[i][whole];
+        }
+        multiply(0);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[wave][i * NT + j][lane] = sum[i][j];
     __syncthreads();
-    if (wave == 0) {
-        sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-        const uint32_t row = i0 + lane % 16, col = j0 + lane / 16 * 4;
-        if (row < m && col < n) store_four(c + row * ld_c + col, (int)(n - col), sum);
+    for (uint32_t f = wave; f < MT * NT; f += kStreamWaves) {
+        float4x total = part[0][f][lane];
+        for (int w = 1; w < kStreamWaves; ++w) total += part[w][f][lane];
+        const uint32_t row = i0 + f / NT * 16 + lane % 16, col = j0 + f % NT * 16 + lane / 16 * 4;
+        if (row < m && col < n) store_four(c + row * ld_c + col, (int)(n - col), total);
     }
 }
 
@@ -141,66 +220,98 @@ __device__ __forceinline__ void buffer_to_lds(__amdgpu_buffer_rsrc_t from, void*
 #endif
 }
 
-// A workgroup makes TM x TN outputs, WM x WN waves a part each.  While one
-// group's rows of A and B (128 bytes each) are multiplied, the next group's go
-// from memory to the other half of the LDS.
-template <typename T, int TM, int TN, int WM, int WN, bool kDirect>
-__global__ void __launch_bounds__(WM* WN * 64)
-    tile_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
-                const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
-                uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m, uint32_t tiles) {
-    constexpr int kThreads = WM * WN * 64;
+// What a launch of tiles has besides the operands.
+struct Tiles {
+    uint32_t rows, count;     // of tiles, down and in all
+    uint32_t splits, groups;  // the columns in `splits` parts of `groups` groups
+    float* sums;              // where there are several parts: [part][m][n]
+};
+
+// A workgroup makes TM x TN outputs over one of the splits' columns.  KS sets of
+// WM x WN waves each take a part of these columns, a wave a part of the tile.
+// While one group's rows of A and B (128 bytes each) are multiplied, the next
+// group's go from memory to the other half of the LDS: directly, or where rows are not
+// 16-byte aligned (kDirect = false) through registers.
+template <typename T, int TM, int TN, int WM, int WN, int KS, bool kDirect>
+__global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Tiles tiles) {
+    constexpr int kThreads = WM * WN * 64;  // of a set
     constexpr int MT = TM / WM / 16, NT = TN / WN / 16;
     constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte loads of a lane
     static_assert(TN / WN <= kFp8Group && kFp8Group % (TN / WN) == 0, "a wave's columns share a scale");
     constexpr int kScales = TM + 64;  // A's, then B's
     static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
-    static_assert(MT >= 3 && kLoadsA <= NT && kLoadsB <= (MT - 2) * NT, "a group's loads fit between its products");
-    __shared__ alignas(1024) uint8_t a0[TM * 128], b0[TN * 128], a1[TM * 128], b1[TN * 128];
-    __shared__ alignas(256) float4x scales[2][kScales];  // of four groups, and of the next four
+    static_assert(MT >= 4 && kLoadsA <= NT && kLoadsB <= NT, "a group's loads fit between its products");
+    constexpr int kA = TM * 128, kB = TN * 128;  // bytes of a group's rows
+    __shared__ alignas(1024) uint8_t a0[KS * kA], b0[KS * kB], a1[KS * kA], b1[KS * kB];
+    __shared__ alignas(256) float4x scales[2][KS * kScales];  // of four groups, and of the next four
 
     // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, in
     // panels of 8 tiles' rows, so that the 32 it has at a time are 8 x 4 and its L2
     // serves each row of A and B several times.
     const uint32_t per_xcd = gridDim.x / 8;
-    const uint32_t tile = blockIdx.x % 8 * per_xcd + blockIdx.x / 8;
-    if (tile >= tiles) return;
-    const uint32_t tiles_n = tiles / tiles_m;
-    const uint32_t panel = tile / (8 * tiles_n), in_panel = tile - panel * 8 * tiles_n;
-    const uint32_t panel_rows = min(8u, tiles_m - panel * 8);
+    const uint32_t index = blockIdx.x % 8 * per_xcd + blockIdx.x / 8;
+    if (index >= tiles.count * tiles.splits) return;
+    const uint32_t split = index / tiles.count, tile = index % tiles.count;
+    const uint32_t panel_tiles = 8 * (tiles.count / tiles.rows);
+    const uint32_t panel = tile / panel_tiles, in_panel = tile % panel_tiles;
+    const uint32_t panel_rows = min(8u, tiles.rows - panel * 8);
     const uint32_t i0 = (panel * 8 + in_panel % panel_rows) * TM, j0 = in_panel / panel_rows * TN;
 
+    const uint32_t m = (uint32_t)x.m, n = (uint32_t)x.n, k = (uint32_t)x.k;
     const uint32_t lane = threadIdx.x % 64;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t set = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % (WM * WN);
     const uint32_t wave_i = wave / WN * (TM / WM), wave_j = wave % WN * (TN / WN);
-    const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;
+    const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;  // of a row
+    // The split's groups are [begin, end).  Each set takes `whole` of them, from `base` on, and
+    // those that are left over, a last one that the columns do not fill among
+    // them, are taken one by each set at the end.
+    const uint32_t begin = split * tiles.groups, end = min(begin + tiles.groups, groups);
+    const uint32_t whole = (min(end, k / kFp8Group) - begin) / KS;
+    const uint32_t base = begin + set * whole, rest = begin + KS * whole + set;
 
     // The row of LDS that a lane of load instruction l fills is 8 * (l * waves + wave) + lane / 8; its
     // 16-byte places hold the row's chunks in the order place ^ (row % 8), so that
     // the lanes of a fragment read from different banks.
     const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
-    const uint8_t* const tile_a = a + i0 * ld_a;
-    const uint8_t* const tile_b = b + j0 * ld_b;
+    const uint8_t* const tile_a = x.a + i0 * x.ld_a;
+    const uint8_t* const tile_b = x.b + j0 * x.ld_b;
     uint32_t from_a[kLoadsA], from_b[kLoadsB];
 #pragma unroll
     for (int l = 0; l < kLoadsA; ++l)
-        from_a[l] = min(8 * (l * WM * WN + wave) + lane / 8, m - 1 - i0) * (uint32_t)ld_a + chunk;
+        from_a[l] = min(8 * (l * WM * WN + wave) + lane / 8, m - 1 - i0) * (uint32_t)x.ld_a + chunk;
 #pragma unroll
     for (int l = 0; l < kLoadsB; ++l)
-        from_b[l] = min(8 * (l * WM * WN + wave) + lane / 8, n - 1 - j0) * (uint32_t)ld_b + chunk;
+        from_b[l] = min(8 * (l * WM * WN + wave) + lane / 8, n - 1 - j0) * (uint32_t)x.ld_b + chunk;
     const uint32_t part_s = wave % (kScales / 64);  // waves beyond them load a part again
     const bool scales_of_a = part_s < TM / 64;
-    const float* const tile_s = scales_of_a ? sa + (uint64_t)i0 * groups : sb + (uint64_t)(j0 / kFp8Group) * groups;
+    const float* const tile_s = scales_of_a ? x.a_scales + (uint64_t)i0 * groups
+                                            : x.b_scales + (uint64_t)(j0 / kFp8Group) * groups;
     const uint32_t from_s = (scales_of_a ? min(part_s * 64 + lane, m - 1 - i0)
                                          : min(lane, (n - 1) / kFp8Group - j0 / kFp8Group)) * groups;
 
     // Buffer loads: a lane's offset stays, the group's is a scalar.
     const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b);
+    auto at_a = [&](int l) { return set * kA + 1024 * (l * WM * WN + wave); };
+    auto at_b = [&](int l) { return set * kB + 1024 * (l * WM * WN + wave); };
+    int4x held_a[kLoadsA], held_b[kLoadsB];  // on their way through registers
     auto load_a = [&](int l, uint32_t g, uint8_t* la) {
-        buffer_to_lds(all_a, la + 1024 * (l * WM * WN + wave), from_a[l], g * kFp8Group);
+        if constexpr (kDirect)
+            buffer_to_lds(all_a, la + at_a(l), from_a[l], g * kFp8Group);
+        else
+            __builtin_memcpy(&held_a[l], tile_a + g * kFp8Group + from_a[l], 16);
     };
     auto load_b = [&](int l, uint32_t g, uint8_t* lb) {
-        buffer_to_lds(all_b, lb + 1024 * (l * WM * WN + wave), from_b[l], g * kFp8Group);
+        if constexpr (kDirect)
+            buffer_to_lds(all_b, lb + at_b(l), from_b[l], g * kFp8Group);
+        else
+            __builtin_memcpy(&held_b[l], tile_b + g * kFp8Group + from_b[l], 16);
+    };
+    auto keep_a = [&](int l, uint8_t* la) {
+        if constexpr (!kDirect) *(int4x*)(la + at_a(l) + 16 * lane) = held_a[l];
+    };
+    auto keep_b = [&](int l, uint8_t* lb) {
+        if constexpr (!kDirect) *(int4x*)(lb + at_b(l) + 16 * lane) = held_b[l];
     };
     // Scales come four groups at a time (a load of one group's takes as many
     // requests as a load of a tile's 128-byte rows), the last four of a row where
@@ -208,21 +319,20 @@ __global__ void __launch_bounds__(WM* WN * 64)
     const uint32_t last_four = max(groups, 4u) - 4;
     float4x four;
     auto load_four = [&](uint32_t q) { __builtin_memcpy(&four, tile_s + from_s + min(4 * q, last_four), 16); };
-    auto keep_four = [&](uint32_t q) { scales[q % 2][64 * part_s + lane] = four; };
+    auto keep_four = [&](uint32_t q) { scales[q % 2][set * kScales + 64 * part_s + lane] = four; };
     // where group g's scales stand, from a row's first one on
     auto scales_at = [&](uint32_t g) {
-        return (const float*)scales + (g / 4 % 2 * kScales * 4 + g - min(g / 4 * 4, last_four));
+        return (const float*)scales + (g / 4 % 2 * KS * kScales * 4 + g - min(g / 4 * 4, last_four));
     };
-    // The columns beyond the last whole group, with zeros after them.
-    auto load_rest = [&](uint32_t g, uint8_t* la, uint8_t* lb) {
+    // One group, with zeros beyond the columns.
+    auto load_rest = [&](uint32_t g) {
         const uint32_t at = g * kFp8Group;
         const int left = (int)(k - at) - (int)chunk;
 #pragma unroll
-        for (int l = 0; l < kLoadsA; ++l)
-            *(int4x*)(la + 1024 * (l * WM * WN + wave) + 16 * lane) = load_16(tile_a + at + from_a[l], left);
+        for (int l = 0; l < kLoadsA; ++l) *(int4x*)(a0 + at_a(l) + 16 * lane) = load_16(tile_a + at + from_a[l], left);
 #pragma unroll
-        for (int l = 0; l < kLoadsB; ++l)
-            *(int4x*)(lb + 1024 * (l * WM * WN + wave) + 16 * lane) = load_16(tile_b + at + from_b[l], left);
+        for (int l = 0; l < kLoadsB; ++l) *(int4x*)(b0 + at_b(l) + 16 * lane) = load_16(tile_b + at + from_b[l], left);
+        scales[0][set * kScales + 64 * part_s + lane][0] = tile_s[from_s + g];
     };
 
     float4x sum[MT][NT];
@@ -235,9 +345,9 @@ __global__ void __launch_bounds__(WM* WN * 64)
     // row is an offset in its instruction and takes no register.
     const uint32_t row16 = lane % 16, quarter = lane / 16;
     const uint32_t place = row16 * 128 + (quarter ^ row16 % 8) * 16;
-    uint32_t a_lo = wave_i * 128 + place, a_hi = wave_i * 128 + (place ^ 64);
-    uint32_t b_lo = wave_j * 128 + place, b_hi = wave_j * 128 + (place ^ 64);
-    uint32_t a_scale = 4 * (wave_i + row16);
+    uint32_t a_lo = set * kA + wave_i * 128 + place, a_hi = set * kA + wave_i * 128 + (place ^ 64);
+    uint32_t b_lo = set * kB + wave_j * 128 + place, b_hi = set * kB + wave_j * 128 + (place ^ 64);
+    uint32_t a_scale = 4 * (set * kScales + wave_i + row16);
     asm("" : "+v"(a_lo), "+v"(a_hi), "+v"(b_lo), "+v"(b_hi), "+v"(a_scale));
     auto fragment = [&](const uint8_t* rows, uint32_t at_lo, uint32_t at_hi) {
         const int4x lo = *(const int4x*)(rows + at_lo), hi = *(const int4x*)(rows + at_hi);
@@ -254,7 +364,7 @@ __global__ void __launch_bounds__(WM* WN * 64)
         asm volatile("" ::: "memory");
     };
     constexpr std::integral_constant<int, 0> kNone;
-    constexpr std::integral_constant<int, kLoadsB> kOfB;
+    constexpr std::integral_constant<int, kDirect ? kLoadsB : 63> kLater;  // B's of the group after the next
 
     // One group.  The fragments of A's next 16 rows come from LDS while these are
     // multiplied, and the next group's first ones while this group's last are.  By
@@ -264,18 +374,11 @@ __global__ void __launch_bounds__(WM* WN * 64)
     // (Past the last group the last one is loaded again: nobody reads it.)  Loads are
     // issued one after each product, so that no wave stands in line for them.  A
     // product is added to its sum two instructions later, when the matrix unit has it.
-    const uint32_t whole = k / kFp8Group;
     int8x fb[NT], fa;
     float scale_a, scale_b;
-    const uint32_t b_scale = 4 * (TM + wave_j / kFp8Group);
-    auto first = [&](const uint8_t* la, const uint8_t* lb, uint32_t g) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j) fb[j] = fragment_b(lb, j);
-        fa = fragment_a(la, 0);
-        scale_a = scales_at(g)[a_scale];
-        scale_b = scales_at(g)[b_scale];
-    };
-    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, const uint8_t* next_a, const uint8_t* next_b) {
+    const uint32_t b_scale = 4 * (set * kScales + TM + wave_j / kFp8Group);
+    const uint32_t last_group = base + whole - 1;
+    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, uint8_t* next_a, const uint8_t* next_b) {
         const bool new_four = g % 4 == 1 && g / 4 * 4 + 4 < groups;
         const float* const now = scales_at(g);
         const float* const next = scales_at(g + 1);
@@ -294,7 +397,7 @@ __global__ void __launch_bounds__(WM* WN * 64)
             const bool last = i == MT - 1;
             if (i == 1) meet(std::integral_constant<int, 63>{});
             if (last) {
-                meet(kOfB);
+                meet(kLater);
                 if (new_four) keep_four(g / 4 + 1);
                 scale_b = next[b_scale];
             }
@@ -308,9 +411,12 @@ __global__ void __launch_bounds__(WM* WN * 64)
                 __builtin_amdgcn_sched_barrier(0);
                 if (last) {
                     fb[j] = fragment_b(next_b, j);
-                    if (j < kLoadsA) load_a(j, min(g + 2, whole - 1), la);
-                } else if (i >= 1 && t - NT < kLoadsB) {
-                    load_b(t - NT, min(g + 2, whole - 1), lb);
+                    if (j < kLoadsA) load_a(j, min(g + 2, last_group), la);
+                } else if (i == (kDirect ? 1 : 0) && j < kLoadsB) {
+                    load_b(j, min(g + 2, last_group), lb);
+                } else if (i == MT - 2) {
+                    if (j < kLoadsA) keep_a(j, next_a);
+                    if (j < kLoadsB) keep_b(j, lb);
                 }
                 if (t >= 2) add(t - 2);
                 __builtin_amdgcn_sched_barrier(0);
@@ -322,83 +428,179 @@ __global__ void __launch_bounds__(WM* WN * 64)
         add(MT * NT - 1);
     };
 
-    for (uint32_t e = 0; e < 4; ++e) four[e] = e < groups ? tile_s[from_s + e] : 0.0f;
-    keep_four(0);
     if (whole > 0) {
-        const uint32_t second = min(1u, whole - 1);
+        const uint32_t q = base / 4 * 4, start = min(q, last_four);
 #pragma unroll
-        for (int l = 0; l < kLoadsA; ++l) load_a(l, 0, a0);
+        for (uint32_t e = 0; e < 4; ++e) four[e] = tile_s[from_s + min(start + e, groups - 1)];
+        keep_four(base / 4);
+        if (base % 4 >= 2 && q + 4 < groups) {  // past where the loop asks for the next four
+            load_four(base / 4 + 1);
+            keep_four(base / 4 + 1);
+        }
+        const uint32_t second = min(base + 1, last_group);
 #pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) load_b(l, 0, b0);
+        for (int l = 0; l < kLoadsA; ++l) load_a(l, base, a0);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l) load_b(l, base, b0);
+#pragma unroll
+        for (int l = 0; l < kLoadsA; ++l) keep_a(l, a0);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l) keep_b(l, b0);
 #pragma unroll
         for (int l = 0; l < kLoadsB; ++l) load_b(l, second, b1);
-        meet(kOfB);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l) keep_b(l, b1);
+        meet(kLater);
 #pragma unroll
         for (int l = 0; l < kLoadsA; ++l) load_a(l, second, a1);
-        first(a0, b0, 0);
-        for (uint32_t g = 0; g + 1 < whole; g += 2) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
+        fa = fragment_a(a0, 0);
+        scale_a = scales_at(base)[a_scale];
+        scale_b = scales_at(base)[b_scale];
+        uint32_t g = base;
+        for (; g < last_group; g += 2) {
             multiply(g, a0, b0, a1, b1);
             multiply(g + 1, a1, b1, a0, b0);
         }
-        if (whole % 2 != 0) multiply(whole - 1, a0, b0, a1, b1);
+        if (g == last_group) multiply(g, a0, b0, a1, b1);
         meet(kNone);
     }
-    if (whole < groups) {
-        load_rest(whole, a0, b0);
+    if (begin + KS * whole < end) {
+        if (rest < end) load_rest(rest);
         __syncthreads();
-        first(a0, b0, whole);
+        if (rest < end) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int8x rest = fragment_a(a0, i);
-            const float s = scales_at(whole)[a_scale + 64 * i] * scale_b;
+            for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
+            const float in_b = ((const float*)scales)[b_scale];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const float4x p = group_product<T>(fb[j], rest);
+            for (int i = 0; i < MT; ++i) {
+                const int8x rows = fragment_a(a0, i);
+                const float s = ((const float*)scales)[a_scale + 64 * i] * in_b;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
+                for (int j = 0; j < NT; ++j) {
+                    const float4x p = group_product<T>(fb[j], rows);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
+                }
             }
         }
+        __syncthreads();
     }
+
+    // The sets join their sums in LDS, in their order.
+    static_assert(KS <= 2 && (KS - 1) * TM * TN * 4 <= 2 * KS * kA, "the second set's sums fit where A's rows were");
+    if (KS == 2) {
+        constexpr int kHalf = MT * NT / 2;
+        auto place_of = [&](int t) {
+            return (float4x*)(t < kHalf ? a0 : a1) + (wave * kHalf + t % kHalf) * 64 + lane;
+        };
+        if (set == 1)
+#pragma unroll
+            for (int t = 0; t < MT * NT; ++t) *place_of(t) = sum[t / NT][t % NT];
+        __syncthreads();
+        if (set == 1) return;
+#pragma unroll
+        for (int t = 0; t < MT * NT; ++t) sum[t / NT][t % NT] += *place_of(t);
+    }
+
     const bool inside = i0 + TM <= m && j0 + TN <= n;
-    T* const out = c + (uint64_t)(i0 + wave_i + row16) * ld_c + j0 + wave_j + quarter * 4;
-    const int rows_left = (int)(m - i0 - wave_i - row16), cols_left = (int)(n - j0 - wave_j - quarter * 4);
-    if (inside) {
+    const uint32_t row = i0 + wave_i + row16, col = j0 + wave_j + quarter * 4;
+    auto store = [&](auto* out, uint64_t ld) {
+        using O = std::remove_pointer_t<decltype(out)>;
+        if (inside) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) store_four(out + 16 * i * ld_c + 16 * j, 4, sum[i][j]);
-    } else {
+                for (int j = 0; j < NT; ++j) store_four(out + 16 * i * ld + 16 * j, 4, sum[i][j]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+                for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (16 * i < rows_left && 16 * j + e < cols_left)
-                        out[16 * i * ld_c + 16 * j + e] = (T)sum[i][j][e];
+                    for (int e = 0; e < 4; ++e)
+                        if (row + 16 * i < m && col + 16 * j + e < n) out[16 * i * ld + 16 * j + e] = (O)sum[i][j][e];
+        }
+    };
+    if (tiles.splits > 1)
+        store(tiles.sums + ((uint64_t)split * m + row) * n + col, (uint64_t)n);
+    else
+        store((T*)x.c + row * x.ld_c + col, x.ld_c);
+}
+
+// Adds the splits' sums, in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ sums, uint32_t splits, uint32_t m,
+                                                   uint32_t n, T* __restrict__ c, uint64_t ld_c) {
+    const uint32_t fours = (n + 3) / 4;
+    const uint64_t size = (uint64_t)m * n, count = (uint64_t)m * fours;
+    for (uint64_t f = (uint64_t)blockIdx.x * 256 + threadIdx.x; f < count; f += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = f / fours;
+        const uint32_t col = (uint32_t)(f % fours) * 4, valid = min(n - col, 4u);
+        const float* p = sums + row * n + col;
+        float4x total = {0, 0, 0, 0};
+        for (uint32_t s = 0; s < splits; ++s, p += size) {
+            float4x v = {0, 0, 0, 0};
+            if (valid == 4)
+                __builtin_memcpy(&v, p, 16);
+            else
+                for (uint32_t e = 0; e < valid; ++e) v[e] = p[e];
+            total += v;
+        }
+        store_four(c + row * ld_c + col, (int)valid, total);
     }
 }
 
 }  // namespace
 
-hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s) {
+namespace {
+
+template <typename T, int TM, int TN, int WM, int WN, int KS, bool kDirect>
+hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
+    const uint32_t groups = (uint32_t)((x.k + kFp8Group - 1) / kFp8Group);
+    Tiles tiles;
+    tiles.rows = (uint32_t)((x.m + TM - 1) / TM);
+    tiles.count = tiles.rows * (uint32_t)((x.n + TN - 1) / TN);
+    tiles.groups = (groups + splits - 1) / splits;
+    tiles.splits = (groups + tiles.groups - 1) / tiles.groups;
+    tiles.sums = (float*)x.workspace;
+    const uint32_t grid = (tiles.count * tiles.splits + 7) / 8 * 8;
+    tile_kernel<T, TM, TN, WM, WN, KS, kDirect><<<grid, WM * WN * KS * 64, 0, s>>>(x, tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || tiles.splits == 1) return e;
+    const uint64_t blocks = (x.m * ((x.n + 3) / 4) + 255) / 256;
+    join_kernel<T><<<(uint32_t)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(tiles.sums, tiles.splits, (uint32_t)x.m,
+                                                                            (uint32_t)x.n, (T*)x.c, x.ld_c);
+    return hipGetLastError();
+}
+
+template <typename T, int MT, int NT, int kAhead>
+hipError_t launch_stream(const MatmulArgs& x, hipStream_t s) {
+    const uint32_t tiles_m = (uint32_t)((x.m + 16 * MT - 1) / (16 * MT));
+    const uint64_t tiles = tiles_m * ((x.n + 16 * NT - 1) / (16 * NT));
+    stream_kernel<T, MT, NT, kAhead><<<(uint32_t)tiles, kStreamWaves * 64, 0, s>>>(
+        x.a, x.ld_a, x.a_scales, x.b, x.ld_b, x.b_scales, (uint32_t)x.m, (uint32_t)x.n, (uint32_t)x.k, (T*)x.c, x.ld_c,
+        tiles_m);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fp8_matmul(int type, const MatmulArgs& x, hipStream_t s) {
     auto run = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const bool direct = a.ld_a % 16 == 0 && a.ld_b % 16 == 0 && (uintptr_t)a.a % 16 == 0 && (uintptr_t)a.b % 16 == 0 &&
-                            a.ld_a <= kMaxTileLd && a.ld_b <= kMaxTileLd;
-        if (direct && a.m > 64 && a.k > 0) {
-            constexpr int TM = sizeof(T) == 4 ? 128 : 256, TN = TM;
-            const uint32_t tiles_m = (uint32_t)((a.m + TM - 1) / TM);
-            const uint32_t tiles = tiles_m * (uint32_t)((a.n + TN - 1) / TN);
-            tile_kernel<T, TM, TN, 2, TN / 64, true><<<(tiles + 7) / 8 * 8, TN / 64 * 128, 0, s>>>(
-                a.a, a.ld_a, a.a_scales, a.b, a.ld_b, a.b_scales, (uint32_t)a.m, (uint32_t)a.n, (uint32_t)a.k, (T*)a.c,
-                a.ld_c, tiles_m, tiles);
-            return hipGetLastError();
-        }
-        const dim3 grid((uint32_t)((a.n + 15) / 16), (uint32_t)((a.m + 15) / 16));
-        stream_kernel<T><<<grid, 256, 0, s>>>(a.a, a.ld_a, a.a_scales, a.b, a.ld_b, a.b_scales, (uint32_t)a.m,
-                                              (uint32_t)a.n, (uint32_t)a.k, (T*)a.c, a.ld_c);
-        return hipGetLastError();
+        const bool direct = x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 &&
+                            (uintptr_t)x.b % 16 == 0;
+        const bool tiled = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd && x.m > 64 && x.k > 0;
+#ifdef FORCE_M2
+        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 2, 2, true>(x, FORCE_M2, s);
+#endif
+        if constexpr (sizeof(T) == 2)
+            if (tiled && direct) return launch_tiles<T, 256, 256, 2, 4, 1, true>(x, 1, s);
+        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 2, 2, true>(x, 1, s);
+        if (tiled) return launch_tiles<T, 128, 128, 2, 2, 2, false>(x, 1, s);
+        return launch_stream<T, 1, 1, 2>(x, s);
     };
     switch (type) {
         case kTypeBf16: return run((__bf16*)nullptr);
