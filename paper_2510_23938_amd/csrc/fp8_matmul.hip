@@ -227,23 +227,42 @@ struct Tiles {
     float* sums;              // where there are several parts: [part][m][n]
 };
 
-// A workgroup makes TM x TN outputs over one of the splits' columns.  KS sets of
-// WM x WN waves each take a part of these columns, a wave a part of the tile.
-// While one group's rows of A and B (128 bytes each) are multiplied, the next
-// group's go from memory to the other half of the LDS: directly, or where rows are not
-// 16-byte aligned (kDirect = false) through registers.
-template <typename T, int TM, int TN, int WM, int WN, int KS, bool kDirect>
-__global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Tiles tiles) {
-    constexpr int kThreads = WM * WN * 64;  // of a set
+// Groups whose scales a lane loads at once, where the LDS holds `stages` groups.
+constexpr int scale_run(int stages) { return stages == 3 ? 3 : 4; }
+
+// A workgroup makes TM x TN outputs over one of the splits' columns, with WM x
+// WN waves.  While one group's rows of A and B (128 bytes each) are multiplied, the
+// next groups' go from memory to LDS, which holds S groups: directly, or where
+// rows are not 16-byte aligned (kDirect = false) through registers.
+//
+// LDS bounds how much can be on its way, and with it how soon a step may follow the
+// last: a step takes at least the time a load takes, divided by the steps it is
+// asked for ahead.
+template <typename T, int TM, int TN, int WM, int WN, int S, bool kDirect>
+__global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles tiles) {
+    constexpr int kThreads = WM * WN * 64;
     constexpr int MT = TM / WM / 16, NT = TN / WN / 16;
     constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte loads of a lane
+    constexpr int kLoads = kLoadsA + kLoadsB;
     static_assert(TN / WN <= kFp8Group && kFp8Group % (TN / WN) == 0, "a wave's columns share a scale");
     constexpr int kScales = TM + 64;  // A's, then B's
     static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
     static_assert(MT >= 4 && kLoadsA <= NT && kLoadsB <= NT, "a group's loads fit between its products");
-    constexpr int kA = TM * 128, kB = TN * 128;  // bytes of a group's rows
-    __shared__ alignas(1024) uint8_t a0[KS * kA], b0[KS * kB], a1[KS * kA], b1[KS * kB];
-    __shared__ alignas(256) float4x scales[2][KS * kScales];  // of four groups, and of the next four
+    constexpr int kRun = scale_run(S), kUnroll = S == 2 ? 4 : S;  // groups of a run; a multiple of S and of that
+    static_assert(S >= 2 && S <= 4 && (kDirect || S == 4), "the LDS arrays and the registers' ring");
+    // separate arrays: the compiler then sees that a fragment's read does not touch a stage that loads go to
+    __shared__ alignas(1024) uint8_t a0[TM * 128], b0[TN * 128], a1[TM * 128], b1[TN * 128];
+    __shared__ alignas(1024) uint8_t a2[S > 2 ? TM * 128 : 16], b2[S > 2 ? TN * 128 : 16];
+    __shared__ alignas(1024) uint8_t a3[S > 3 ? TM * 128 : 16], b3[S > 3 ? TN * 128 : 16];
+    __shared__ alignas(256) float4x scales[2][kScales];  // of kRun groups, and of the next ones
+    auto stage_a = [&](auto st) {
+        constexpr int i = decltype(st)::value % S;
+        return i == 0 ? a0 : i == 1 ? a1 : i == 2 ? a2 : a3;
+    };
+    auto stage_b = [&](auto st) {
+        constexpr int i = decltype(st)::value % S;
+        return i == 0 ? b0 : i == 1 ? b1 : i == 2 ? b2 : b3;
+    };
 
     // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, in
     // panels of 8 tiles' rows, so that the 32 it has at a time are 8 x 4 and its L2
@@ -259,16 +278,13 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
 
     const uint32_t m = (uint32_t)x.m, n = (uint32_t)x.n, k = (uint32_t)x.k;
     const uint32_t lane = threadIdx.x % 64;
-    const uint32_t set = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % (WM * WN);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wave_i = wave / WN * (TM / WM), wave_j = wave % WN * (TN / WN);
     const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;  // of a row
-    // The split's groups are [begin, end).  Each set takes `whole` of them, from `base` on, and
-    // those that are left over, a last one that the columns do not fill among
-    // them, are taken one by each set at the end.
-    const uint32_t begin = split * tiles.groups, end = min(begin + tiles.groups, groups);
-    const uint32_t whole = (min(end, k / kFp8Group) - begin) / KS;
-    const uint32_t base = begin + set * whole, rest = begin + KS * whole + set;
+    // The split's groups are [base, end), `whole` of them filled by the columns; base
+    // is a multiple of kRun.
+    const uint32_t base = split * tiles.groups, end = min(base + tiles.groups, groups);
+    const uint32_t whole = min(end, k / kFp8Group) - base, last_group = base + whole - 1;
 
     // The row of LDS that a lane of load instruction l fills is 8 * (l * waves + wave) + lane / 8; its
     // 16-byte places hold the row's chunks in the order place ^ (row % 8), so that
@@ -292,49 +308,38 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
 
     // Buffer loads: a lane's offset stays, the group's is a scalar.
     const auto all_a = rows_at(tile_a), all_b = rows_at(tile_b);
-    auto at_a = [&](int l) { return set * kA + 1024 * (l * WM * WN + wave); };
-    auto at_b = [&](int l) { return set * kB + 1024 * (l * WM * WN + wave); };
-    int4x held_a[kLoadsA], held_b[kLoadsB];  // on their way through registers
-    auto load_a = [&](int l, uint32_t g, uint8_t* la) {
-        if constexpr (kDirect)
-            buffer_to_lds(all_a, la + at_a(l), from_a[l], g * kFp8Group);
-        else
-            __builtin_memcpy(&held_a[l], tile_a + g * kFp8Group + from_a[l], 16);
+    auto at = [&](int l) { return 1024 * (l * WM * WN + wave); };
+    // the group's load l, of A's rows and then of B's
+    int4x held[kDirect ? 1 : S][kLoads];  // on their way through registers
+    auto load = [&](int l, uint32_t g, auto st) {
+        constexpr int i = decltype(st)::value % S;
+        if constexpr (kDirect) {
+            if (l < kLoadsA)
+                buffer_to_lds(all_a, stage_a(st) + at(l), from_a[l], g * kFp8Group);
+            else
+                buffer_to_lds(all_b, stage_b(st) + at(l - kLoadsA), from_b[l - kLoadsA], g * kFp8Group);
+        } else {
+            const uint8_t* const p = l < kLoadsA ? tile_a + from_a[l] : tile_b + from_b[l - kLoadsA];
+            __builtin_memcpy(&held[i][l], p + g * kFp8Group, 16);
+        }
     };
-    auto load_b = [&](int l, uint32_t g, uint8_t* lb) {
-        if constexpr (kDirect)
-            buffer_to_lds(all_b, lb + at_b(l), from_b[l], g * kFp8Group);
-        else
-            __builtin_memcpy(&held_b[l], tile_b + g * kFp8Group + from_b[l], 16);
+    auto keep = [&](int l, int4x v, auto st) {
+        *(int4x*)((l < kLoadsA ? stage_a(st) + at(l) : stage_b(st) + at(l - kLoadsA)) + 16 * lane) = v;
     };
-    auto keep_a = [&](int l, uint8_t* la) {
-        if constexpr (!kDirect) *(int4x*)(la + at_a(l) + 16 * lane) = held_a[l];
-    };
-    auto keep_b = [&](int l, uint8_t* lb) {
-        if constexpr (!kDirect) *(int4x*)(lb + at_b(l) + 16 * lane) = held_b[l];
-    };
-    // Scales come four groups at a time (a load of one group's takes as many
-    // requests as a load of a tile's 128-byte rows), the last four of a row where
-    // there are fewer left, and are kept in LDS as [row][4].
-    const uint32_t last_four = max(groups, 4u) - 4;
-    float4x four;
-    auto load_four = [&](uint32_t q) { __builtin_memcpy(&four, tile_s + from_s + min(4 * q, last_four), 16); };
-    auto keep_four = [&](uint32_t q) { scales[q % 2][set * kScales + 64 * part_s + lane] = four; };
+    // Scales come kRun groups at a time (a load of one group's takes as many
+    // requests as a load of a tile's 128-byte rows), a row's last kRun where there
+    // are fewer left, and are kept in LDS as [row][4].  A run is asked for kRun
+    // groups before it goes there, at steps that the unrolled loop fixes: where a branch
+    // decided, the compiler would wait there for all loads.
+    const uint32_t last_run = max(groups, (uint32_t)kRun) - kRun;
+    const bool runs = groups > kRun;
+    float4x held_scales;
+    auto load_run = [&](uint32_t r) { __builtin_memcpy(&held_scales, tile_s + from_s + min(kRun * r, last_run), 4 * kRun); };
+    auto keep_run = [&](uint32_t r) { scales[r % 2][64 * part_s + lane] = held_scales; };
     // where group g's scales stand, from a row's first one on
     auto scales_at = [&](uint32_t g) {
-        return (const float*)scales + (g / 4 % 2 * KS * kScales * 4 + g - min(g / 4 * 4, last_four));
+        return (const float*)scales + (g / kRun % 2 * kScales * 4 + g - min(g / kRun * kRun, last_run));
     };
-    // One group, with zeros beyond the columns.
-    auto load_rest = [&](uint32_t g) {
-        const uint32_t at = g * kFp8Group;
-        const int left = (int)(k - at) - (int)chunk;
-#pragma unroll
-        for (int l = 0; l < kLoadsA; ++l) *(int4x*)(a0 + at_a(l) + 16 * lane) = load_16(tile_a + at + from_a[l], left);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) *(int4x*)(b0 + at_b(l) + 16 * lane) = load_16(tile_b + at + from_b[l], left);
-        scales[0][set * kScales + 64 * part_s + lane][0] = tile_s[from_s + g];
-    };
-
     float4x sum[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -345,9 +350,9 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
     // row is an offset in its instruction and takes no register.
     const uint32_t row16 = lane % 16, quarter = lane / 16;
     const uint32_t place = row16 * 128 + (quarter ^ row16 % 8) * 16;
-    uint32_t a_lo = set * kA + wave_i * 128 + place, a_hi = set * kA + wave_i * 128 + (place ^ 64);
-    uint32_t b_lo = set * kB + wave_j * 128 + place, b_hi = set * kB + wave_j * 128 + (place ^ 64);
-    uint32_t a_scale = 4 * (set * kScales + wave_i + row16);
+    uint32_t a_lo = wave_i * 128 + place, a_hi = wave_i * 128 + (place ^ 64);
+    uint32_t b_lo = wave_j * 128 + place, b_hi = wave_j * 128 + (place ^ 64);
+    uint32_t a_scale = 4 * (wave_i + row16);
     asm("" : "+v"(a_lo), "+v"(a_hi), "+v"(b_lo), "+v"(b_hi), "+v"(a_scale));
     auto fragment = [&](const uint8_t* rows, uint32_t at_lo, uint32_t at_hi) {
         const int4x lo = *(const int4x*)(rows + at_lo), hi = *(const int4x*)(rows + at_hi);
@@ -363,26 +368,33 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    // loads issued after the next group's: with two stages, B's of the group after the next (see below)
+    constexpr int kAfter = !kDirect ? 63 : S == 2 ? kLoadsB : (S - 2) * kLoads;
+    constexpr std::integral_constant<int, kAfter> kLater;
+    constexpr std::integral_constant<int, kAfter> kLaterAndRun;
     constexpr std::integral_constant<int, 0> kNone;
-    constexpr std::integral_constant<int, kDirect ? kLoadsB : 63> kLater;  // B's of the group after the next
+    constexpr std::integral_constant<int, 63> kAll;
 
-    // One group.  The fragments of A's next 16 rows come from LDS while these are
-    // multiplied, and the next group's first ones while this group's last are.  By
-    // then every wave has read all it needs of this half's A, so the group after
-    // the next may be loaded there; of B every wave holds all it needs from the
-    // start, so the group after the next is loaded over it as soon as they have met.
-    // (Past the last group the last one is loaded again: nobody reads it.)  Loads are
-    // issued one after each product, so that no wave stands in line for them.  A
-    // product is added to its sum two instructions later, when the matrix unit has it.
+    // One group, in LDS stage st.  The fragments of A's next 16 rows come from LDS
+    // while these are multiplied, and the next group's first ones while this group's last
+    // are.  By then every wave has read all it needs of this stage, so the group S
+    // further on may be loaded there (past the last group the last one again: nobody
+    // reads it), a load after each product so that no wave stands in line for them.
+    // With two stages B's rows are asked for sooner: every wave holds all it needs
+    // of them from the start, and their place is free as soon as the waves have met.
+    // A product is added to its sum two instructions later, when the matrix unit has it.
     int8x fb[NT], fa;
     float scale_a, scale_b;
-    const uint32_t b_scale = 4 * (set * kScales + TM + wave_j / kFp8Group);
-    const uint32_t last_group = base + whole - 1;
-    auto multiply = [&](uint32_t g, uint8_t* la, uint8_t* lb, uint8_t* next_a, const uint8_t* next_b) {
-        const bool new_four = g % 4 == 1 && g / 4 * 4 + 4 < groups;
+    const uint32_t b_scale = 4 * (TM + wave_j / kFp8Group);
+    auto multiply = [&](uint32_t g, auto step) {
+        constexpr int U = decltype(step)::value, ST = U % S;  // g is U modulo kUnroll, from base on
+        constexpr std::integral_constant<int, ST> st;
+        constexpr std::integral_constant<int, ST + 1> kNext;
+        constexpr std::integral_constant<int, ST + S - 1> kLast;  // the stage before, which loads still go to
+        constexpr std::integral_constant<int, ST + 2> kKept;      // through registers: the group written to LDS
+        constexpr bool kAsk = U % kRun == kRun - 1, kKeep = U % kRun == kRun - 2;
         const float* const now = scales_at(g);
         const float* const next = scales_at(g + 1);
-        if (new_four) load_four(g / 4 + 1);
         const float in_b = scale_b;
         float4x p[3];
         float s[2];
@@ -395,13 +407,19 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const bool last = i == MT - 1;
-            if (i == 1) meet(std::integral_constant<int, 63>{});
+            if (kDirect && S == 2 && i == 1) meet(kAll);
             if (last) {
-                meet(kLater);
-                if (new_four) keep_four(g / 4 + 1);
+                if constexpr (kAsk) {
+                    if (runs) load_run(g / kRun + 2);
+                    meet(kLaterAndRun);
+                } else {
+                    meet(kLater);
+                }
+                if constexpr (kKeep)
+                    if (runs) keep_run(g / kRun + 1);
                 scale_b = next[b_scale];
             }
-            const int8x next_fa = last ? fragment_a(next_a, 0) : fragment_a(la, i + 1);
+            const int8x next_fa = last ? fragment_a(stage_a(kNext), 0) : fragment_a(stage_a(st), i + 1);
             const float next_scale = last ? next[a_scale] : now[a_scale + 64 * (i + 1)];
             s[i % 2] = scale_a * in_b;
 #pragma unroll
@@ -409,14 +427,22 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
                 const int t = i * NT + j;
                 p[t % 3] = group_product<T>(fb[j], fa);
                 __builtin_amdgcn_sched_barrier(0);
-                if (last) {
-                    fb[j] = fragment_b(next_b, j);
-                    if (j < kLoadsA) load_a(j, min(g + 2, last_group), la);
-                } else if (i == (kDirect ? 1 : 0) && j < kLoadsB) {
-                    load_b(j, min(g + 2, last_group), lb);
-                } else if (i == MT - 2) {
-                    if (j < kLoadsA) keep_a(j, next_a);
-                    if (j < kLoadsB) keep_b(j, lb);
+                if (last) fb[j] = fragment_b(stage_b(kNext), j);
+                if constexpr (!kDirect) {
+                    // four groups on their way; the one after the next goes to LDS, and its place in the ring to
+                    // the group four further on
+                    if (i == MT - 2)
+#pragma unroll
+                        for (int l = j; l < kLoads; l += NT) keep(l, held[kKept.value % S][l], kKept);
+                    if (last)
+#pragma unroll
+                        for (int l = j; l < kLoads; l += NT) load(l, min(g + 2 + S, last_group), kKept);
+                } else if constexpr (S == 2) {
+                    if (last && j < kLoadsA) load(j, min(g + 2, last_group), st);
+                    if (i == 1 && j < kLoadsB) load(kLoadsA + j, min(g + 2, last_group), st);
+                } else {
+                    if (last && j < kLoads) load(j, min(g + S, last_group), st);
+                    if (!last && t + NT < kLoads) load(t + NT, min(g + S - 1, last_group), kLast);
                 }
                 if (t >= 2) add(t - 2);
                 __builtin_amdgcn_sched_barrier(0);
@@ -427,81 +453,88 @@ __global__ void __launch_bounds__(WM* WN* KS * 64) tile_kernel(MatmulArgs x, Til
         add(MT * NT - 2);
         add(MT * NT - 1);
     };
+    constexpr std::integral_constant<int, 0> kStage0;
+    constexpr std::integral_constant<int, 1> kStage1;
+    constexpr std::integral_constant<int, 2> kStage2;
+    constexpr std::integral_constant<int, 3> kStage3;
 
     if (whole > 0) {
-        const uint32_t q = base / 4 * 4, start = min(q, last_four);
+        auto load_all = [&](uint32_t ahead, auto st, int first, int count) {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) four[e] = tile_s[from_s + min(start + e, groups - 1)];
-        keep_four(base / 4);
-        if (base % 4 >= 2 && q + 4 < groups) {  // past where the loop asks for the next four
-            load_four(base / 4 + 1);
-            keep_four(base / 4 + 1);
+            for (int l = first; l < count; ++l) load(l, min(base + ahead, last_group), st);
+        };
+        if constexpr (!kDirect) {
+            load_all(0, kStage0, 0, kLoads);
+            load_all(1, kStage1, 0, kLoads);
+            load_all(2, kStage2, 0, kLoads);
+            load_all(3, kStage3, 0, kLoads);
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                keep(l, held[0][l], kStage0);
+                keep(l, held[1][l], kStage1);
+            }
+            load_all(4, kStage0, 0, kLoads);
+            load_all(5, kStage1, 0, kLoads);
+        } else if constexpr (S == 2) {
+            load_all(0, kStage0, 0, kLoads);
+            load_all(1, kStage1, kLoadsA, kLoads);
+        } else {
+            load_all(0, kStage0, 0, kLoads);
+            load_all(1, kStage1, 0, kLoads);
+            if constexpr (S > 3) load_all(2, kStage2, 0, kLoads);
         }
-        const uint32_t second = min(base + 1, last_group);
+        const uint32_t run = base / kRun, start = min(run * kRun, last_run);
 #pragma unroll
-        for (int l = 0; l < kLoadsA; ++l) load_a(l, base, a0);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) load_b(l, base, b0);
-#pragma unroll
-        for (int l = 0; l < kLoadsA; ++l) keep_a(l, a0);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) keep_b(l, b0);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) load_b(l, second, b1);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l) keep_b(l, b1);
-        meet(kLater);
-#pragma unroll
-        for (int l = 0; l < kLoadsA; ++l) load_a(l, second, a1);
+        for (uint32_t e = 0; e < kRun; ++e) held_scales[e] = tile_s[from_s + min(start + e, groups - 1)];
+        keep_run(run);
+        if (runs) load_run(run + 1);
+        meet(kNone);
+        if constexpr (kDirect && S == 2) load_all(1, kStage1, 0, kLoadsA);
+        if constexpr (kDirect && S == 3) load_all(2, kStage2, 0, NT < kLoads ? NT : kLoads);
+        if constexpr (kDirect && S == 4) load_all(3, kStage3, 0, NT < kLoads ? NT : kLoads);
 #pragma unroll
         for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
         fa = fragment_a(a0, 0);
         scale_a = scales_at(base)[a_scale];
         scale_b = scales_at(base)[b_scale];
         uint32_t g = base;
-        for (; g < last_group; g += 2) {
-            multiply(g, a0, b0, a1, b1);
-            multiply(g + 1, a1, b1, a0, b0);
+        const uint32_t stop = base + whole;
+        for (; g + kUnroll <= stop; g += kUnroll) {
+            multiply(g, kStage0);
+            multiply(g + 1, kStage1);
+            multiply(g + 2, kStage2);
+            if constexpr (kUnroll > 3) multiply(g + 3, kStage3);
         }
-        if (g == last_group) multiply(g, a0, b0, a1, b1);
+        if (g < stop) multiply(g, kStage0);
+        if (g + 1 < stop) multiply(g + 1, kStage1);
+        if constexpr (kUnroll > 3)
+            if (g + 2 < stop) multiply(g + 2, kStage2);
         meet(kNone);
     }
-    if (begin + KS * whole < end) {
-        if (rest < end) load_rest(rest);
+    if (base + whole < end) {  // a last group, with zeros beyond the columns
+        const uint32_t begin = (base + whole) * kFp8Group;
+        const int left = (int)(k - begin) - (int)chunk;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint8_t* const p = l < kLoadsA ? tile_a + from_a[l] : tile_b + from_b[l - kLoadsA];
+            keep(l, load_16(p + begin, left), kStage0);
+        }
+        scales[0][64 * part_s + lane][0] = tile_s[from_s + groups - 1];
         __syncthreads();
-        if (rest < end) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
-            const float in_b = ((const float*)scales)[b_scale];
+        for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
+        const float in_b = ((const float*)scales)[b_scale];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int8x rows = fragment_a(a0, i);
-                const float s = ((const float*)scales)[a_scale + 64 * i] * in_b;
+        for (int i = 0; i < MT; ++i) {
+            const int8x rows = fragment_a(a0, i);
+            const float s = ((const float*)scales)[a_scale + 64 * i] * in_b;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const float4x p = group_product<T>(fb[j], rows);
+            for (int j = 0; j < NT; ++j) {
+                const float4x p = group_product<T>(fb[j], rows);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
-                }
+                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
             }
         }
-        __syncthreads();
-    }
-
-    // The sets join their sums in LDS, in their order.
-    static_assert(KS <= 2 && (KS - 1) * TM * TN * 4 <= 2 * KS * kA, "the second set's sums fit where A's rows were");
-    if (KS == 2) {
-        constexpr int kHalf = MT * NT / 2;
-        auto place_of = [&](int t) {
-            return (float4x*)(t < kHalf ? a0 : a1) + (wave * kHalf + t % kHalf) * 64 + lane;
-        };
-        if (set == 1)
-#pragma unroll
-            for (int t = 0; t < MT * NT; ++t) *place_of(t) = sum[t / NT][t % NT];
-        __syncthreads();
-        if (set == 1) return;
-#pragma unroll
-        for (int t = 0; t < MT * NT; ++t) sum[t / NT][t % NT] += *place_of(t);
     }
 
     const bool inside = i0 + TM <= m && j0 + TN <= n;
@@ -556,17 +589,17 @@ __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ sum
 
 namespace {
 
-template <typename T, int TM, int TN, int WM, int WN, int KS, bool kDirect>
+template <typename T, int TM, int TN, int WM, int WN, int S, bool kDirect>
 hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
     const uint32_t groups = (uint32_t)((x.k + kFp8Group - 1) / kFp8Group);
     Tiles tiles;
     tiles.rows = (uint32_t)((x.m + TM - 1) / TM);
     tiles.count = tiles.rows * (uint32_t)((x.n + TN - 1) / TN);
-    tiles.groups = (groups + splits - 1) / splits;
+    tiles.groups = ((groups + splits - 1) / splits + scale_run(S) - 1) / scale_run(S) * scale_run(S);
     tiles.splits = (groups + tiles.groups - 1) / tiles.groups;
     tiles.sums = (float*)x.workspace;
     const uint32_t grid = (tiles.count * tiles.splits + 7) / 8 * 8;
-    tile_kernel<T, TM, TN, WM, WN, KS, kDirect><<<grid, WM * WN * KS * 64, 0, s>>>(x, tiles);
+    tile_kernel<T, TM, TN, WM, WN, S, kDirect><<<grid, WM * WN * 64, 0, s>>>(x, tiles);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || tiles.splits == 1) return e;
     const uint64_t blocks = (x.m * ((x.n + 3) / 4) + 255) / 256;
@@ -593,13 +626,10 @@ hipError_t launch_fp8_matmul(int type, const MatmulArgs& x, hipStream_t s) {
         const bool direct = x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 &&
                             (uintptr_t)x.b % 16 == 0;
         const bool tiled = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd && x.m > 64 && x.k > 0;
-#ifdef FORCE_M2
-        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 2, 2, true>(x, FORCE_M2, s);
-#endif
         if constexpr (sizeof(T) == 2)
-            if (tiled && direct) return launch_tiles<T, 256, 256, 2, 4, 1, true>(x, 1, s);
-        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 2, 2, true>(x, 1, s);
-        if (tiled) return launch_tiles<T, 128, 128, 2, 2, 2, false>(x, 1, s);
+            if (tiled && direct) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, 1, s);
+        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, 1, s);
+        if (tiled) return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, 1, s);
         return launch_stream<T, 1, 1, 2>(x, s);
     };
     switch (type) {
