@@ -247,7 +247,8 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
     static_assert(TN / WN <= kFp8Group && kFp8Group % (TN / WN) == 0, "a wave's columns share a scale");
     constexpr int kScales = TM + 64;  // A's, then B's
     static_assert(kScales / 64 <= WM * WN, "a wave loads 64 scales");
-    static_assert(MT >= 4 && kLoadsA <= NT && kLoadsB <= NT, "a group's loads fit between its products");
+    static_assert(MT >= 4 && (S > 2 || (kLoadsA <= NT && kLoadsB <= NT)) && kLoads <= (MT - 1) * NT,
+                  "a group's loads fit between its products");
     constexpr int kRun = scale_run(S), kUnroll = S == 2 ? 4 : S;  // groups of a run; a multiple of S and of that
     static_assert(S >= 2 && S <= 4 && (kDirect || S == 4), "the LDS arrays and the registers' ring");
     // separate arrays: the compiler then sees that a fragment's read does not touch a stage that loads go to
@@ -509,9 +510,9 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
         if (g + 1 < stop) multiply(g + 1, kStage1);
         if constexpr (kUnroll > 3)
             if (g + 2 < stop) multiply(g + 2, kStage2);
-        meet(kNone);
     }
     if (base + whole < end) {  // a last group, with zeros beyond the columns
+        meet(kNone);
         const uint32_t begin = (base + whole) * kFp8Group;
         const int left = (int)(k - begin) - (int)chunk;
 #pragma unroll
@@ -537,29 +538,52 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
         }
     }
 
-    const bool inside = i0 + TM <= m && j0 + TN <= n;
-    const uint32_t row = i0 + wave_i + row16, col = j0 + wave_j + quarter * 4;
-    auto store = [&](auto* out, uint64_t ld) {
+    // A lane has four columns of a row; to store whole lines a wave turns 16 rows at a
+    // time in LDS, so that neighbouring lanes have 16 bytes each of one row (stores
+    // of the lanes' own columns, 32 bytes of a row, took 7 us of a 256 x 256
+    // tile's 50).
+    meet(kNone);  // nobody reads stages any more
+    auto store = [&](auto* out, uint64_t ld) {  // out: the matrix
         using O = std::remove_pointer_t<decltype(out)>;
-        if (inside) {
+        constexpr int kSize = sizeof(O), kRow = TN / WN * kSize, kPlaces = kRow / 16, kElements = 16 / kSize;
+        static_assert(WM * WN * 16 * kRow <= TM * 128, "the waves' 16 rows fit a stage");
+        uint8_t* const area = a0 + wave * 16 * kRow;
+        auto place = [&](uint32_t row, uint32_t chunk) { return area + row * kRow + (chunk ^ row % kPlaces) * 16; };
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) store_four(out + 16 * i * ld + 16 * j, 4, sum[i][j]);
-        } else {
+            for (int j = 0; j < NT; ++j) {
+                O four[4];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 4; ++e) four[e] = (O)sum[i][j][e];
+                const uint32_t byte = (16 * j + 4 * quarter) * kSize;
+                __builtin_memcpy(place(row16, byte / 16) + byte % 16, four, sizeof four);
+            }
+            asm volatile("" ::: "memory");  // a wave's LDS accesses stay in order
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+            for (int r = 0; r < 16; r += 64 / kPlaces) {
+                const uint32_t in_16 = r + lane / kPlaces, chunk_of = lane % kPlaces;
+                const int4x v = *(const int4x*)place(in_16, chunk_of);
+                const uint32_t row = i0 + wave_i + 16 * i + in_16, col = j0 + wave_j + chunk_of * kElements;
+                if (row >= m || col >= n) continue;
+                O* const to = out + row * ld + col;
+                if (col + kElements <= n) {
+                    __builtin_memcpy(to, &v, 16);
+                } else {
+                    O elements[kElements];
+                    __builtin_memcpy(elements, &v, 16);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (row + 16 * i < m && col + 16 * j + e < n) out[16 * i * ld + 16 * j + e] = (O)sum[i][j][e];
+                    for (int e = 0; e < kElements; ++e)
+                        if (col + e < n) to[e] = elements[e];
+                }
+            }
+            asm volatile("" ::: "memory");
         }
     };
     if (tiles.splits > 1)
-        store(tiles.sums + ((uint64_t)split * m + row) * n + col, (uint64_t)n);
+        store(tiles.sums + (uint64_t)split * m * n, (uint64_t)n);
     else
-        store((T*)x.c + row * x.ld_c + col, x.ld_c);
+        store((T*)x.c, x.ld_c);
 }
 
 // Adds the splits' sums, in their order.
