@@ -107,7 +107,8 @@ size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
  *   workspace: >= hv_fp8_matmul_workspace_bytes(m, n, k), 256-byte aligned; NULL
  *              where that is 0.  Scratch: calls that share one must share a
  *              stream.
- * Errors: HV_ERR_WORKSPACE for a missing, short or misaligned workspace. */
+ * Errors: HV_ERR_INVALID_ARG also for m or n above 2^27; HV_ERR_WORKSPACE for a
+ * missing, short or misaligned workspace. */
 hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const float* a_scales, const uint8_t* b,
                         uint64_t ld_b, const float* b_scales, uint64_t m, uint64_t n, uint64_t k, void* c,
                         uint64_t ld_c, void* workspace, size_t workspace_bytes, hipStream_t stream);

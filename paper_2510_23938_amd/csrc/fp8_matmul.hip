@@ -98,65 +98,55 @@ __device__ __forceinline__ void store_four(T* p, int valid, float4x v) {
 // ---------------------------------------------------------------------------
 // few rows: B straight from memory
 
-// A workgroup makes MT x NT fragments of 16 x 16 outputs; its waves take the
-// groups of columns in turn and join their sums through LDS.  Nothing is
-// shared between waves but A, which the caches hold, so B goes to registers with
-// kAhead groups on their way per wave.
+// A workgroup makes NT fragments of 16 x 16 outputs; its waves take the groups of
+// columns in turn and join their sums through LDS.  Nothing is shared between
+// waves but A, which the caches hold, so B goes to registers with kAhead groups on
+// their way per wave.
 constexpr int kStreamWaves = 8;
 
-template <typename T, int MT, int NT, int kAhead>
+template <typename T, int NT, int kAhead>
 __global__ void __launch_bounds__(kStreamWaves * 64)
     stream_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
                   const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
                   uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m) {
-    __shared__ float4x part[kStreamWaves][MT * NT][64];
+    __shared__ float4x part[kStreamWaves][NT][64];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t i0 = blockIdx.x % tiles_m * 16 * MT, j0 = blockIdx.x / tiles_m * 16 * NT;
+    const uint32_t i0 = blockIdx.x % tiles_m * 16, j0 = blockIdx.x / tiles_m * 16 * NT;
     const uint32_t groups = (k + kFp8Group - 1) / kFp8Group, whole = k / kFp8Group;
     const uint32_t at = lane / 16 * 16;
-    const uint8_t *row_a[MT], *row_b[NT];
-    const float* scale_a[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const uint32_t row = min(i0 + 16 * i + lane % 16, m - 1);
-        row_a[i] = a + row * ld_a + at;
-        scale_a[i] = sa + (uint64_t)row * groups;
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) row_b[j] = b + min(j0 + 16 * j + lane % 16, n - 1) * ld_b + at;
+    const uint32_t row_of_a = min(i0 + lane % 16, m - 1);
+    const uint8_t* const row_a = a + row_of_a * ld_a + at;
+    const float* const scale_a = sa + (uint64_t)row_of_a * groups;
+    const uint8_t* row_b[NT];
     const float* scale_b[NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) scale_b[j] = sb + (uint64_t)(min(j0 + 16 * j, n - 1) / kFp8Group) * groups;
+    for (int j = 0; j < NT; ++j) {
+        row_b[j] = b + min(j0 + 16 * j + lane % 16, n - 1) * ld_b + at;
+        scale_b[j] = sb + (uint64_t)(min(j0 + 16 * j, n - 1) / kFp8Group) * groups;
+    }
 
-    float4x sum[MT][NT];
+    float4x sum[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) sum[i][j] = float4x{0, 0, 0, 0};
-    int8x fa[kAhead][MT], fb[kAhead][NT];
-    float in_a[kAhead][MT], in_b[kAhead][NT];
+    for (int j = 0; j < NT; ++j) sum[j] = float4x{0, 0, 0, 0};
+    int8x fa[kAhead], fb[kAhead][NT];
+    float in_a[kAhead], in_b[kAhead][NT];
     auto load = [&](int slot, uint32_t g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             fb[slot][j] = load_whole(row_b[j] + g * kFp8Group);
             in_b[slot][j] = scale_b[j][g];
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            fa[slot][i] = load_whole(row_a[i] + g * kFp8Group);
-            in_a[slot][i] = scale_a[i][g];
-        }
+        fa[slot] = load_whole(row_a + g * kFp8Group);
+        in_a[slot] = scale_a[g];
     };
     auto multiply = [&](int slot) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int j = 0; j < NT; ++j) {
+            const float4x p = group_product<T>(fb[slot][j], fa[slot]);
+            const float s = in_a[slot] * in_b[slot][j];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const float4x p = group_product<T>(fb[slot][j], fa[slot][i]);
-                const float s = in_a[slot][i] * in_b[slot][j];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
-            }
+            for (int e = 0; e < 4; ++e) sum[j][e] = fmaf(p[e], s, sum[j][e]);
+        }
     };
     // The wave's groups are wave, wave + kStreamWaves, ...; count of the whole ones among them.
     const uint32_t count = whole > wave ? (whole - wave + kStreamWaves - 1) / kStreamWaves : 0;
@@ -175,29 +165,24 @@ __global__ void __launch_bounds__(kStreamWaves * 64)
 #pragma unroll
     for (int d = 0; d < kAhead - 1; ++d)
         if (x + d < count) multiply(d);
-    if (whole < groups && whole % kStreamWaves == wave) {
+    if (whole < groups && whole % kStreamWaves == wave) {  // a last group, with zeros beyond the columns
         const int left = (int)(k - whole * kFp8Group) - (int)at;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             fb[0][j] = load_fragment(row_b[j] + whole * kFp8Group, left);
             in_b[0][j] = scale_b[j][whole];
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            fa[0][i] = load_fragment(row_a[i] + whole * kFp8Group, left);
-            in_a[0][i] = scale_a[i][whole];
-        }
+        fa[0] = load_fragment(row_a + whole * kFp8Group, left);
+        in_a[0] = scale_a[whole];
         multiply(0);
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) part[wave][i * NT + j][lane] = sum[i][j];
+    for (int j = 0; j < NT; ++j) part[wave][j][lane] = sum[j];
     __syncthreads();
-    for (uint32_t f = wave; f < MT * NT; f += kStreamWaves) {
-        float4x total = part[0][f][lane];
-        for (int w = 1; w < kStreamWaves; ++w) total += part[w][f][lane];
-        const uint32_t row = i0 + f / NT * 16 + lane % 16, col = j0 + f % NT * 16 + lane / 16 * 4;
+    for (uint32_t j = wave; j < NT; j += kStreamWaves) {
+        float4x total = part[0][j][lane];
+        for (int w = 1; w < kStreamWaves; ++w) total += part[w][j][lane];
+        const uint32_t row = i0 + lane % 16, col = j0 + j * 16 + lane / 16 * 4;
         if (row < m && col < n) store_four(c + row * ld_c + col, (int)(n - col), total);
     }
 }
@@ -586,7 +571,7 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
         store((T*)x.c, x.ld_c);
 }
 
-// Adds the splits' sums, in their order.
+// Adds the splits' sums, in their order (no splits: zeros).
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ sums, uint32_t splits, uint32_t m,
                                                    uint32_t n, T* __restrict__ c, uint64_t ld_c) {
@@ -613,6 +598,14 @@ __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ sum
 
 namespace {
 
+template <typename T>
+hipError_t launch_join(const float* sums, uint32_t splits, const MatmulArgs& x, hipStream_t s) {
+    const uint64_t blocks = (x.m * ((x.n + 3) / 4) + 255) / 256;
+    join_kernel<T><<<(uint32_t)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(sums, splits, (uint32_t)x.m,
+                                                                            (uint32_t)x.n, (T*)x.c, x.ld_c);
+    return hipGetLastError();
+}
+
 template <typename T, int TM, int TN, int WM, int WN, int S, bool kDirect>
 hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
     const uint32_t groups = (uint32_t)((x.k + kFp8Group - 1) / kFp8Group);
@@ -625,41 +618,187 @@ hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
     const uint32_t grid = (tiles.count * tiles.splits + 7) / 8 * 8;
     tile_kernel<T, TM, TN, WM, WN, S, kDirect><<<grid, WM * WN * 64, 0, s>>>(x, tiles);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || tiles.splits == 1) return e;
-    const uint64_t blocks = (x.m * ((x.n + 3) / 4) + 255) / 256;
-    join_kernel<T><<<(uint32_t)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(tiles.sums, tiles.splits, (uint32_t)x.m,
-                                                                            (uint32_t)x.n, (T*)x.c, x.ld_c);
-    return hipGetLastError();
+    return e != hipSuccess || tiles.splits == 1 ? e : launch_join<T>(tiles.sums, tiles.splits, x, s);
 }
 
-template <typename T, int MT, int NT, int kAhead>
+template <typename T, int NT, int kAhead>
 hipError_t launch_stream(const MatmulArgs& x, hipStream_t s) {
-    const uint32_t tiles_m = (uint32_t)((x.m + 16 * MT - 1) / (16 * MT));
+    const uint32_t tiles_m = (uint32_t)((x.m + 15) / 16);
     const uint64_t tiles = tiles_m * ((x.n + 16 * NT - 1) / (16 * NT));
-    stream_kernel<T, MT, NT, kAhead><<<(uint32_t)tiles, kStreamWaves * 64, 0, s>>>(
+    stream_kernel<T, NT, kAhead><<<(uint32_t)tiles, kStreamWaves * 64, 0, s>>>(
         x.a, x.ld_a, x.a_scales, x.b, x.ld_b, x.b_scales, (uint32_t)x.m, (uint32_t)x.n, (uint32_t)x.k, (T*)x.c, x.ld_c,
         tiles_m);
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// which kernels a product takes
+
+enum Shape { k256x256, k256x128, k192x128, k128x128, kUnaligned, kShapes };
+
+// What a tile takes, in us: `fixed`, and a group's `full` where every compute unit
+// has a tile and `lone` where few have.  Measured at 8 and 64 groups with 256 tiles, half of that and one; one
+// tile of 256 x 256 over 64 groups takes 128 us on a full chip, two of 256 x 128 take 140,
+// four of 128 x 128 164.
+struct Cost {
+    uint32_t rows, cols;
+    float fixed, full, lone;
+};
+constexpr Cost kCost[2][kShapes] = {
+    {{256, 256, 8.8f, 1.86f, 1.17f},
+     {256, 128, 7.2f, 0.98f, 0.63f},
+     {192, 128, 6.3f, 0.77f, 0.53f},
+     {128, 128, 5.4f, 0.56f, 0.38f},
+     {128, 128, 6.4f, 0.72f, 0.56f}},
+    {{256, 256, 0, 0, 0},  // 32-bit results: the widened codes leave no registers for it
+     {256, 128, 8.5f, 2.03f, 1.35f},
+     {192, 128, 7.8f, 1.60f, 1.13f},
+     {128, 128, 8.0f, 1.10f, 0.88f},
+     {128, 128, 8.6f, 1.27f, 0.95f}}};
+constexpr uint64_t kUnits = 256;  // compute units: one tile each at a time
+constexpr uint32_t kMaxSplits = 16;
+// Adding up the splits' sums: a launch and 4 bytes of each sum there and back (three
+// splits of 128 x 8192 8 us, of 32 x 1024 3 us).
+float join_cost(uint64_t m, uint64_t n, uint32_t splits) {
+    return splits == 1 ? 0.0f : 3.0f + (float)m * (float)n * 4.0f * (float)splits / 3.1e6f;
+}
+
+uint64_t tiles_of(const Cost& c, uint64_t m, uint64_t n) {
+    return (m + c.rows - 1) / c.rows * ((n + c.cols - 1) / c.cols);
+}
+
+// Whole rounds of a tile on every unit, and a last one that fewer units share.
+float rounds_cost(const Cost& c, uint64_t tiles, uint64_t groups) {
+    const float full = c.fixed + c.full * (float)groups, rest = (float)(tiles % kUnits) / (float)kUnits;
+    return (float)(tiles / kUnits) * full +
+           (rest > 0 ? c.fixed + (c.lone + (c.full - c.lone) * rest) * (float)groups : 0.0f);
+}
+
+// The cheapest single shape, with the columns of A and B in parts where that
+// pays: few tiles, many groups.
+struct Choice {
+    Shape shape;
+    uint32_t splits;
+    float cost;
+};
+Choice choose(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
+    Choice best = {kShapes, 1, 0};
+    for (int s = aligned ? (wide ? k256x128 : k256x256) : kUnaligned; s < (aligned ? kUnaligned : kShapes); ++s) {
+        const Cost& c = kCost[wide][s];
+        const uint64_t tiles = tiles_of(c, m, n);
+        const uint32_t most = c.rows != 128 || tiles >= kUnits ? 1 : kMaxSplits;
+        for (uint32_t p = 1; p <= most && (p == 1 || groups / p >= 4); ++p) {
+            const float cost = rounds_cost(c, tiles * p, (groups + p - 1) / p) + join_cost(m, n, p);
+            if (best.shape == kShapes || cost < best.cost) best = {(Shape)s, p, cost};
+        }
+    }
+    return best;
+}
+
+// A product by tiles: `main` over its first rows and columns, and where the largest tiles
+// would leave a last round mostly empty, the rest by smaller ones (2048 x 28672
+// over 64 groups: 768 of 896 tiles of 256 x 256, then 256 of 256 x 128).
+struct Plan {
+    Choice main, rest;
+    uint64_t rows, cols;  // main's
+};
+Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
+    Plan plan = {choose(wide, aligned, m, n, groups), {}, m, n};
+    if (wide || !aligned) return plan;
+    const Cost& c = kCost[0][k256x256];
+    const uint64_t down = (m + 255) / 256, across = (n + 255) / 256, rounds = down * across / kUnits;
+    if (rounds == 0 || down * across % kUnits == 0) return plan;
+    const uint64_t less = across >= down ? rounds * kUnits / down : rounds * kUnits / across;
+    if (less == 0) return plan;
+    const uint64_t rows = across >= down ? m : less * 256, cols = across >= down ? less * 256 : n;
+    const Choice rest = choose(false, true, across >= down ? m : m - rows, across >= down ? n - cols : n, groups);
+    const float main_cost = rounds_cost(c, tiles_of(c, rows, cols), groups);
+    if (main_cost + rest.cost + 2.0f < plan.main.cost) plan = {{k256x256, 1, main_cost}, rest, rows, cols};
+    return plan;
+}
+
+// Tiles serve more than 16 rows: a workgroup then reads B's rows for 128 of A's at
+// once (32 x 8192 x 8192 17 us, 28 by fragments of 16 rows).
+bool by_tiles(const MatmulArgs& x) {
+    return x.m > 16 && x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd;
+}
+
+bool aligned_rows(const MatmulArgs& x) {
+    return x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
+}
+
+template <typename T>
+hipError_t launch_choice(const Choice& c, const MatmulArgs& x, hipStream_t s) {
+    switch (c.shape) {
+        case k256x256:
+            if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, c.splits, s);
+            return hipErrorInvalidValue;
+        case k256x128: return launch_tiles<T, 256, 128, 4, 2, 3, true>(x, c.splits, s);
+        case k192x128: return launch_tiles<T, 192, 128, 2, 4, 3, true>(x, c.splits, s);
+        case k128x128: return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, c.splits, s);
+        default: return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, c.splits, s);
+    }
+}
+
+template <typename T>
+hipError_t launch(const MatmulArgs& x, hipStream_t s) {
+    const uint64_t groups = (x.k + kFp8Group - 1) / kFp8Group;
+    if (groups == 0) return launch_join<T>(nullptr, 0, x, s);  // zeros
+    if (!by_tiles(x)) {
+        // A workgroup's fragments of B share one of A, whose 16 rows take as many
+        // loads as theirs: several pay where there are several rows of A and enough
+        // columns for every unit (8 x 28672 x 8192: 57 us by single fragments, 47 by 7; 1
+        // x 28672 x 8192: 42 and 48).
+        const uint64_t fragments = (x.n + 15) / 16;
+        if (x.m > 4 && fragments > 6 * kUnits) return launch_stream<T, 7, 1>(x, s);
+        if (x.m > 4 && fragments > 3 * kUnits) return launch_stream<T, 4, 1>(x, s);
+        if (x.m > 4 && fragments > kUnits && groups > 64) return launch_stream<T, 2, 2>(x, s);
+        return launch_stream<T, 1, 2>(x, s);
+    }
+    const Plan plan = plan_of(sizeof(T) == 4, aligned_rows(x), x.m, x.n, groups);
+    MatmulArgs part = x;
+    part.m = plan.rows;
+    part.n = plan.cols;
+    const hipError_t e = launch_choice<T>(plan.main, part, s);
+    if (e != hipSuccess || (plan.rows == x.m && plan.cols == x.n)) return e;
+    part = x;
+    if (plan.rows < x.m) {
+        part.a += plan.rows * x.ld_a;
+        part.a_scales += plan.rows * groups;
+        part.c = (T*)x.c + plan.rows * x.ld_c;
+        part.m -= plan.rows;
+    } else {
+        part.b += plan.cols * x.ld_b;
+        part.b_scales += plan.cols / kFp8Group * groups;
+        part.c = (T*)x.c + plan.cols;
+        part.n -= plan.cols;
+    }
+    return launch_choice<T>(plan.rest, part, s);
+}
+
 }  // namespace
 
+uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k) {
+    if (m <= 16 || n == 0 || k == 0) return 0;
+    const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
+    uint64_t most = 0;
+    for (int v = 0; v < 4; ++v) {  // any type, any alignment
+        const Plan p = plan_of(v % 2 != 0, v / 2 != 0, m, n, groups);
+        const uint64_t rest_rows = p.rows < m ? m - p.rows : m, rest_cols = p.cols < n ? n - p.cols : n;
+        const uint64_t main = p.main.splits > 1 ? p.main.splits * p.rows * p.cols * 4 : 0;
+        const bool two = p.rows < m || p.cols < n;
+        const uint64_t rest = two && p.rest.splits > 1 ? p.rest.splits * rest_rows * rest_cols * 4 : 0;
+        const uint64_t need = main > rest ? main : rest;
+        if (need > most) most = need;
+    }
+    return most;
+}
+
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& x, hipStream_t s) {
-    auto run = [&](auto* t) {
-        using T = std::remove_pointer_t<decltype(t)>;
-        const bool direct = x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 &&
-                            (uintptr_t)x.b % 16 == 0;
-        const bool tiled = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd && x.m > 64 && x.k > 0;
-        if constexpr (sizeof(T) == 2)
-            if (tiled && direct) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, 1, s);
-        if (tiled && direct) return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, 1, s);
-        if (tiled) return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, 1, s);
-        return launch_stream<T, 1, 1, 2>(x, s);
-    };
     switch (type) {
-        case kTypeBf16: return run((__bf16*)nullptr);
-        case kTypeF16: return run((_Float16*)nullptr);
-        default: return run((float*)nullptr);
+        case kTypeBf16: return launch<__bf16>(x, s);
+        case kTypeF16: return launch<_Float16>(x, s);
+        default: return launch<float>(x, s);
     }
 }
 

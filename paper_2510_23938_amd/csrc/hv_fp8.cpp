@@ -8,6 +8,7 @@ namespace {
 
 constexpr uint64_t kMaxRows = ((uint64_t)1 << 31) - 1;
 constexpr uint64_t kMaxCols = (uint64_t)1 << 24;
+constexpr uint64_t kMaxSide = (uint64_t)1 << 27;  // of a product: a workgroup of 512 per 16 columns stays below 2^32
 constexpr uint64_t kMaxLd = (uint64_t)1 << 31;
 
 static_assert(HV_BF16 == hv::kTypeBf16 && HV_F16 == hv::kTypeF16 && HV_F32 == hv::kTypeF32, "element types");
@@ -106,16 +107,17 @@ hv_status hv_fp8_gated(hv_type type, const void* gate, uint64_t ld_gate, const v
 }
 
 size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k) {
-    if (m > kMaxRows || n > kMaxRows || k > kMaxCols) return 0;
-    return 0;
+    if (m > kMaxSide || n > kMaxSide || k > kMaxCols) return 0;
+    return round_up(hv::fp8_matmul_workspace(m, n, k));
 }
 
 hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const float* a_scales, const uint8_t* b,
                         uint64_t ld_b, const float* b_scales, uint64_t m, uint64_t n, uint64_t k, void* c,
                         uint64_t ld_c, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     HV_TRY(check_type(type));
-    HV_TRY(check_size(m, k));
-    HV_TRY(check_size(n, k));
+    if (m > kMaxSide || n > kMaxSide || k > kMaxCols)
+        return fail(HV_ERR_INVALID_ARG, "m = %llu, n = %llu, k = %llu exceed the limits of 2^27, 2^27 and 2^24",
+                    (unsigned long long)m, (unsigned long long)n, (unsigned long long)k);
     if (m == 0 || n == 0) return HV_OK;
     if (k > 0) {
         HV_TRY(check_matrix("a", a, 1, ld_a, k));

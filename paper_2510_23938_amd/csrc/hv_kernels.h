@@ -252,6 +252,8 @@ hipError_t launch_fp8_rms_norm(int type, const NormArgs& a, hipStream_t s);
 hipError_t launch_fp8_gated(int type, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
                             uint64_t rows, uint64_t cols, uint8_t* codes, uint64_t ld_codes, float* scales,
                             hipStream_t s);
+// Scratch bytes for any type and alignment.
+uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 
 }  // namespace hv

@@ -289,6 +289,20 @@ def test_matmul_strides_and_offsets(m, n, k):
         product(m, n, k, "bf16", pad, offset, out_pad)
 
 
+@pytest.mark.parametrize("m,n,k", [(2048, 8448, 256), (8448, 2048, 384), (2300, 8200, 130)])
+def test_matmul_larger_than_the_chip(m, n, k):
+    """A round of the largest tiles, then the rest by smaller ones: the last columns, the last rows, odd edges."""
+    product(m, n, k, "bf16", pad=-k % 16)
+
+
+@pytest.mark.parametrize("m,n,k", [(40, 300, 9000), (100, 130, 20000), (17, 2000, 4100)])
+@pytest.mark.parametrize("pad", [0, 16, 5])
+def test_matmul_columns_in_parts(m, n, k, pad):
+    """Few tiles and many groups: the columns are split and the parts' sums added."""
+    for dtype in TYPES:
+        product(m, n, k, dtype, pad)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("m,n,k", [(1, 500, 1024), (40, 300, 500), (150, 256, 2048), (512, 512, 768)])
 def test_matmul_codes_of_all_magnitudes(m, n, k, dtype):
