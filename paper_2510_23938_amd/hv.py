@@ -1122,26 +1122,26 @@ def _matrix(t, dtypes, what: str, device, shape=None) -> tuple:
     """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
     lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
     what it is given, so anything it would overrun or misread is refused here."""
-    if _device_of(t, what) != device:
-        raise ValueError(f"{what} is on {t.device}, but the call runs on {device}")
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on {device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
-    if shape is not None and t.shape != torch.Size(shape):
-        raise ValueError(f"{what} has shape {tuple(t.shape)}; the call needs {tuple(shape)}")
-    if t.dim() == 0:
+    s = t.shape
+    if shape is not None and s != shape:
+        raise ValueError(f"{what} has shape {tuple(s)}; the call needs {tuple(shape)}")
+    if len(s) == 0:
         raise ValueError(f"{what} has no dimensions")
-    cols = t.shape[-1]
-    rows = t.numel() // cols if cols else 0
-    ld = cols
-    if t.dim() == 2:
-        if cols > 1 and t.stride(1) != 1:
-            raise ValueError(f"{what}: the elements of a row must be adjacent")
-        if rows > 1:
-            ld = t.stride(0)
-        if ld < cols:
-            raise ValueError(f"{what}: rows overlap (stride {ld}, {cols} columns)")
-    elif not t.is_contiguous():
+    cols = s[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), cols, t.numel() // cols if cols else 0, cols
+    if len(s) != 2:
         raise ValueError(f"{what} must be two-dimensional or contiguous")
+    rows = s[0]
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be adjacent")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap (stride {ld}, {cols} columns)")
     return t.data_ptr(), ld, rows, cols
 
 
@@ -1151,6 +1151,7 @@ def _groups(n: int) -> int:
 
 _CODES = (torch.float8_e4m3fn,)
 _SCALES = (torch.float32,)
+_current_stream = torch._C._cuda_getCurrentRawStream  # of a device index; 0.1 us, a Stream object takes 2
 
 
 def _scales(t, what: str, device, shape) -> int:
@@ -1164,7 +1165,7 @@ def _coded(shape, scales_shape, device, out, scales) -> tuple:
     """(codes, scales, codes pointer, codes' leading dimension, scales pointer), allocated where not given."""
     if out is None:
         out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
-        ptr, ld = out.data_ptr(), max(shape[-1], 1)
+        ptr, ld = out.data_ptr(), shape[-1]
     else:
         ptr, ld, _, _ = _matrix(out, _CODES, "out", device, shape)
     if scales is None:
@@ -1191,7 +1192,7 @@ def hv_fp8_quantize(x: torch.Tensor, tile: str = "rows", out=None, scales=None):
         scales_shape = (*x.shape[:-1], _groups(cols))
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x.shape, scales_shape, dev, out, scales)
     _check(lib.hv_fp8_quantize(TYPES[x.dtype], ptr, ld, rows, cols, 1 if tile == "rows" else HV_FP8_GROUP, codes_ptr,
-                               ld_codes, scales_ptr, _stream(dev)))
+                               ld_codes, scales_ptr, _current_stream(dev.index)))
     return out, scales
 
 
@@ -1209,12 +1210,14 @@ def hv_fp8_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual=
         res_ptr, ld_res, _, _ = _matrix(residual, same, "residual", dev, x.shape)
         if residual_out is None:
             residual_out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        h_ptr, ld_h, _, _ = _matrix(residual_out, same, "residual_out", dev, x.shape)
+            h_ptr, ld_h = residual_out.data_ptr(), cols
+        else:
+            h_ptr, ld_h, _, _ = _matrix(residual_out, same, "residual_out", dev, x.shape)
     elif residual_out is not None:
         raise ValueError("residual_out without a residual")
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x.shape, (*x.shape[:-1], _groups(cols)), dev, out, scales)
     _check(lib.hv_fp8_rms_norm(TYPES[x.dtype], ptr, ld, res_ptr, ld_res, weight_ptr, eps, rows, cols, h_ptr, ld_h,
-                               codes_ptr, ld_codes, scales_ptr, _stream(dev)))
+                               codes_ptr, ld_codes, scales_ptr, _current_stream(dev.index)))
     return out, scales, residual_out
 
 
@@ -1227,7 +1230,7 @@ def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(gate.shape, (*gate.shape[:-1], _groups(cols)), dev, out,
                                                           scales)
     _check(lib.hv_fp8_gated(TYPES[gate.dtype], ptr, ld, up_ptr, ld_up, rows, cols, codes_ptr, ld_codes, scales_ptr,
-                            _stream(dev)))
+                            _current_stream(dev.index)))
     return out, scales
 
 
@@ -1255,5 +1258,5 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
     need = lib.hv_fp8_matmul_workspace_bytes(m, n, k)
     ws = (workspace or Workspace(dev)).get(need) if need else None
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
-                             ws.data_ptr() if need else None, ws.numel() if need else 0, _stream(dev)))
+                             ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(dev.index)))
     return out
