@@ -21,11 +21,9 @@
  * the code's number times its group's scale.
  *
  * Quantisation.  A group's scale is max|y| / 448 over its finite values, at
- * least 2^-126, and 1 where that maximum is 0.  A value's code is y / scale
- * rounded to the nearest E4M3 number, ties to even; the quotient is formed with
- * the scale's rounded reciprocal, within 2 units in the last place of its 32
- * bits.  A NaN or an infinity becomes a NaN code and leaves the rest of its
- * group alone.
+ * least 2^-126, and 1 where that maximum is 0.  A value's code is y / scale in 32
+ * bits, rounded to the nearest E4M3 number, ties to even.  A NaN or an infinity
+ * becomes a NaN code and leaves the rest of its group alone.
  *
  * Every call is asynchronous on `stream`: it queues kernels only (no upload, no
  * host wait, no allocation, no memset), so it may be captured in a HIP graph.

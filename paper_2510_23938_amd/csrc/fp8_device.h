@@ -70,18 +70,19 @@ __device__ __forceinline__ float fp8_scale(float largest) {
     return largest > 0.0f ? fmaxf(largest / kFp8Largest, kFp8SmallestScale) : 1.0f;
 }
 
-// Codes of eight values under a scale.  The quotient is y times the scale's
-// rounded reciprocal: a division per value would cost the kernels that write codes
-// more arithmetic than their bytes take time, and moves a code only where the
-// quotient is within 2 units in the last place of 32 bits of a tie.  Quotients of finite
-// values are at most 448 (1 + 2^-22), which rounds to 448, so nothing is clamped;
-// an infinity, or the infinity that a NaN's neighbour cannot make, converts to NaN.
+// Codes of eight values under a scale.  The quotient y / scale is the correctly
+// rounded one: y times the scale's reciprocal, and one correction by the exact
+// remainder, two instructions where a division takes ten.  (Without it ties, which are
+// frequent among 16-bit values, went either way: 0.25% of a weight matrix's codes.)
+// Quotients of finite values are at most 448 (1 + 2^-23), which rounds to 448, so
+// nothing is clamped; a NaN and an infinity become NaN.
 __device__ __forceinline__ uint2 fp8_codes(const float (&y)[8], float scale) {
     const float inv = 1.0f / scale;
     float q[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        q[i] = y[i] * inv;
+        const float near = y[i] * inv;
+        q[i] = fmaf(-fmaf(near, scale, -y[i]), inv, near);  // with these signs a zero keeps its own
         q[i] = __builtin_fabsf(y[i]) < __builtin_inff() ? q[i] : __builtin_nanf("");
     }
     uint2 w;

@@ -123,6 +123,17 @@ def test_quantize_special_values(tile, dtype):
     check_codes(bytes_of(codes), y, scales.cpu().numpy(), t, Q_ERROR)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantize_divides(dtype):
+    """The codes of the rounded quotient, ties among them (frequent for 16-bit values), for scales of many binades."""
+    rng = np.random.default_rng(15)
+    x = on_gpu(values(rng, (512, 1024)) * np.exp(rng.uniform(-60, 60, (512, 1)) if dtype != "f16" else 0), TYPES[dtype])
+    codes, scales = hv.hv_fp8_quantize(x)
+    quotient = x.float().cpu().numpy() / np.repeat(scales.cpu().numpy(), 128, 1)
+    assert quotient.dtype == np.float32
+    assert np.array_equal(bytes_of(codes), fp8.round_to_code(quotient))
+
+
 def test_quantize_keeps_ties_to_even():
     # every midpoint of neighbouring codes under a scale of one: exact quotients
     v = fp8.VALUES[:127]
