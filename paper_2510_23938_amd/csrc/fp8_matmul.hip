@@ -49,28 +49,31 @@ __device__ __forceinline__ float4x group_product<float>(int8x rows, int8x cols) 
     return sum;
 }
 
-// 16 bytes of a row that has `left` bytes from p on; zeros beyond them.
-__device__ __forceinline__ int4x load_16(const uint8_t* p, int left) {
-    int4x f = {0, 0, 0, 0};
+// 16 bytes of a row that has `left` bytes from p on, and k in all; zeros beyond them.
+__device__ __forceinline__ int4x load_16(const uint8_t* p, int left, uint32_t k) {
+    uint64_t v[2] = {0, 0};
     if (left >= 16) {
-        __builtin_memcpy(&f, p, 16);
+        __builtin_memcpy(v, p, 16);
+    } else if (left > 0 && k >= 16) {  // the row's last 16 bytes, and down by what is before p
+        __builtin_memcpy(v, p + left - 16, 16);
+        const int down = 8 * (16 - left);
+        v[0] = down < 64 ? v[0] >> down | v[1] << (64 - down) : v[1] >> (down - 64);
+        v[1] = down < 64 ? v[1] >> down : 0;
     } else {
-        uint64_t lo = 0, hi = 0;
 #pragma unroll 1
         for (int b = left - 1; b >= 0; --b) {
-            hi = hi << 8 | lo >> 56;
-            lo = lo << 8 | p[b];
+            v[1] = v[1] << 8 | v[0] >> 56;
+            v[0] = v[0] << 8 | p[b];
         }
-        f = int4x{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
     }
-    return f;
+    return int4x{(int)v[0], (int)(v[0] >> 32), (int)v[1], (int)(v[1] >> 32)};
 }
 
 // A lane's part of a 16-row fragment over a group: 16 bytes from p and 16 from
 // p + 64 (which columns a lane holds does not matter, as long as both
 // operands go by the same rule).
-__device__ __forceinline__ int8x load_fragment(const uint8_t* p, int left) {
-    const int4x lo = load_16(p, left), hi = load_16(p + 64, left - 64);
+__device__ __forceinline__ int8x load_fragment(const uint8_t* p, int left, uint32_t k) {
+    const int4x lo = load_16(p, left, k), hi = load_16(p + 64, left - 64, k);
     return int8x{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 
@@ -169,10 +172,10 @@ __global__ void __launch_bounds__(kStreamWaves * 64)
         const int left = (int)(k - whole * kFp8Group) - (int)at;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            fb[0][j] = load_fragment(row_b[j] + whole * kFp8Group, left);
+            fb[0][j] = load_fragment(row_b[j] + whole * kFp8Group, left, k);
             in_b[0][j] = scale_b[j][whole];
         }
-        fa[0] = load_fragment(row_a + whole * kFp8Group, left);
+        fa[0] = load_fragment(row_a + whole * kFp8Group, left, k);
         in_a[0] = scale_a[whole];
         multiply(0);
     }
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
             const uint8_t* const p = l < kLoadsA ? tile_a + from_a[l] : tile_b + from_b[l - kLoadsA];
-            keep(l, load_16(p + begin, left), kStage0);
+            keep(l, load_16(p + begin, left, k), kStage0);
         }
         scales[0][64 * part_s + lane][0] = tile_s[from_s + groups - 1];
         __syncthreads();
