@@ -638,6 +638,7 @@ hipError_t launch_stream(const MatmulArgs& x, hipStream_t s) {
 // which kernels a product takes
 
 enum Shape { k256x256, k256x128, k192x128, k128x128, kUnaligned, kShapes };
+static_assert(kMatmul256x256 - k256x256 == kMatmulUnaligned - kUnaligned, "tile kinds in the shapes' order");
 
 // What a tile takes, in us: `fixed`, and a group's `full` where every compute unit
 // has a tile and `lone` where few have.  Measured at 8 and 64 groups with 256 tiles, half of that and one; one
@@ -720,79 +721,89 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
     return plan;
 }
 
+// A workgroup's fragments of B share one of A, whose 16 rows take as many loads as
+// theirs: several pay where there are several rows of A and enough columns for
+// every unit (8 x 28672 x 8192: 57 us by single fragments, 47 by 7; 1 x 28672 x
+// 8192: 42 and 48; 16 x 8192 x 28672: 71 by single ones, 56 by 2).
+int stream_kind(uint64_t m, uint64_t n, uint64_t groups) {
+    const uint64_t fragments = (n + 15) / 16;
+    if (m <= 4) return kMatmulStream1;
+    if (fragments > 6 * kUnits) return kMatmulStream7;
+    if (fragments > 3 * kUnits) return kMatmulStream4;
+    return fragments > kUnits && groups > 64 ? kMatmulStream2 : kMatmulStream1;
+}
+
+}  // namespace
+
 // Tiles serve more than 16 rows: a workgroup then reads B's rows for 128 of A's at
 // once (32 x 8192 x 8192 17 us, 28 by fragments of 16 rows).
-bool by_tiles(const MatmulArgs& x) {
-    return x.m > 16 && x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd;
+int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k, MatmulPart parts[2]) {
+    const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
+    if (groups == 0 || m <= 16 || !tiles) {
+        parts[0] = {groups == 0 ? kMatmulZeros : stream_kind(m, n, groups), 1, m, n};
+        return 1;
+    }
+    const Plan plan = plan_of(wide, aligned, m, n, groups);
+    parts[0] = {kMatmul256x256 + plan.main.shape, plan.main.splits, plan.rows, plan.cols};
+    if (plan.rows == m && plan.cols == n) return 1;
+    parts[1] = {kMatmul256x256 + plan.rest.shape, plan.rest.splits, plan.rows < m ? m - plan.rows : m,
+                plan.cols < n ? n - plan.cols : n};
+    return 2;
 }
 
-bool aligned_rows(const MatmulArgs& x) {
-    return x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
-}
+namespace {
 
 template <typename T>
-hipError_t launch_choice(const Choice& c, const MatmulArgs& x, hipStream_t s) {
-    switch (c.shape) {
-        case k256x256:
-            if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, c.splits, s);
-            return hipErrorInvalidValue;
-        case k256x128: return launch_tiles<T, 256, 128, 4, 2, 3, true>(x, c.splits, s);
-        case k192x128: return launch_tiles<T, 192, 128, 2, 4, 3, true>(x, c.splits, s);
-        case k128x128: return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, c.splits, s);
-        default: return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, c.splits, s);
+hipError_t launch_part(const MatmulPart& p, const MatmulArgs& x, hipStream_t s) {
+    switch (p.kind) {
+        case kMatmulZeros: return launch_join<T>(nullptr, 0, x, s);
+        case kMatmulStream1: return launch_stream<T, 1, 2>(x, s);
+        case kMatmulStream2: return launch_stream<T, 2, 2>(x, s);
+        case kMatmulStream4: return launch_stream<T, 4, 1>(x, s);
+        case kMatmulStream7: return launch_stream<T, 7, 1>(x, s);
+        case kMatmul256x256:
+            if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, p.splits, s);
+            return hipErrorInvalidValue;  // not among a 32-bit result's shapes
+        case kMatmul256x128: return launch_tiles<T, 256, 128, 4, 2, 3, true>(x, p.splits, s);
+        case kMatmul192x128: return launch_tiles<T, 192, 128, 2, 4, 3, true>(x, p.splits, s);
+        case kMatmul128x128: return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, p.splits, s);
+        default: return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, p.splits, s);
     }
 }
 
 template <typename T>
 hipError_t launch(const MatmulArgs& x, hipStream_t s) {
-    const uint64_t groups = (x.k + kFp8Group - 1) / kFp8Group;
-    if (groups == 0) return launch_join<T>(nullptr, 0, x, s);  // zeros
-    if (!by_tiles(x)) {
-        // A workgroup's fragments of B share one of A, whose 16 rows take as many
-        // loads as theirs: several pay where there are several rows of A and enough
-        // columns for every unit (8 x 28672 x 8192: 57 us by single fragments, 47 by 7; 1
-        // x 28672 x 8192: 42 and 48).
-        const uint64_t fragments = (x.n + 15) / 16;
-        if (x.m > 4 && fragments > 6 * kUnits) return launch_stream<T, 7, 1>(x, s);
-        if (x.m > 4 && fragments > 3 * kUnits) return launch_stream<T, 4, 1>(x, s);
-        if (x.m > 4 && fragments > kUnits && groups > 64) return launch_stream<T, 2, 2>(x, s);
-        return launch_stream<T, 1, 2>(x, s);
-    }
-    const Plan plan = plan_of(sizeof(T) == 4, aligned_rows(x), x.m, x.n, groups);
+    const bool aligned = x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
+    const bool tiles = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd;
+    MatmulPart parts[2];
+    const int count = fp8_matmul_parts(sizeof(T) == 4, aligned, tiles, x.m, x.n, x.k, parts);
     MatmulArgs part = x;
-    part.m = plan.rows;
-    part.n = plan.cols;
-    const hipError_t e = launch_choice<T>(plan.main, part, s);
-    if (e != hipSuccess || (plan.rows == x.m && plan.cols == x.n)) return e;
-    part = x;
-    if (plan.rows < x.m) {
-        part.a += plan.rows * x.ld_a;
-        part.a_scales += plan.rows * groups;
-        part.c = (T*)x.c + plan.rows * x.ld_c;
-        part.m -= plan.rows;
-    } else {
-        part.b += plan.cols * x.ld_b;
-        part.b_scales += plan.cols / kFp8Group * groups;
-        part.c = (T*)x.c + plan.cols;
-        part.n -= plan.cols;
-    }
-    return launch_choice<T>(plan.rest, part, s);
+    part.m = parts[0].rows;
+    part.n = parts[0].cols;
+    const hipError_t e = launch_part<T>(parts[0], part, s);
+    if (e != hipSuccess || count == 1) return e;
+    const uint64_t groups = (x.k + kFp8Group - 1) / kFp8Group, row = x.m - parts[1].rows, col = x.n - parts[1].cols;
+    part.m = parts[1].rows;
+    part.n = parts[1].cols;
+    part.a += row * x.ld_a;
+    part.a_scales += row * groups;
+    part.b += col * x.ld_b;
+    part.b_scales += col / kFp8Group * groups;
+    part.c = (T*)x.c + row * x.ld_c + col;
+    return launch_part<T>(parts[1], part, s);
 }
 
 }  // namespace
 
 uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k) {
-    if (m <= 16 || n == 0 || k == 0) return 0;
-    const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
     uint64_t most = 0;
     for (int v = 0; v < 4; ++v) {  // any type, any alignment
-        const Plan p = plan_of(v % 2 != 0, v / 2 != 0, m, n, groups);
-        const uint64_t rest_rows = p.rows < m ? m - p.rows : m, rest_cols = p.cols < n ? n - p.cols : n;
-        const uint64_t main = p.main.splits > 1 ? p.main.splits * p.rows * p.cols * 4 : 0;
-        const bool two = p.rows < m || p.cols < n;
-        const uint64_t rest = two && p.rest.splits > 1 ? p.rest.splits * rest_rows * rest_cols * 4 : 0;
-        const uint64_t need = main > rest ? main : rest;
-        if (need > most) most = need;
+        MatmulPart parts[2];
+        const int count = fp8_matmul_parts(v % 2 != 0, v / 2 != 0, true, m, n, k, parts);
+        for (int i = 0; i < count; ++i) {
+            const uint64_t need = parts[i].splits > 1 ? parts[i].splits * parts[i].rows * parts[i].cols * 4 : 0;
+            if (need > most) most = need;
+        }
     }
     return most;
 }

@@ -1,6 +1,7 @@
 // hv_fp8.cpp -- C ABI of the 8-bit operators: argument checks and launches.
 #include "hv_fp8.h"
 #include "hv_host.h"
+#include "hv_inspect.h"
 
 using namespace hvh;
 
@@ -25,6 +26,13 @@ hv_status check_size(uint64_t rows, uint64_t cols) {
         return fail(HV_ERR_INVALID_ARG, "%llu x %llu exceeds the limit of %llu rows and %llu columns",
                     (unsigned long long)rows, (unsigned long long)cols, (unsigned long long)kMaxRows,
                     (unsigned long long)kMaxCols);
+    return HV_OK;
+}
+
+hv_status check_product(uint64_t m, uint64_t n, uint64_t k) {
+    if (m > kMaxSide || n > kMaxSide || k > kMaxCols)
+        return fail(HV_ERR_INVALID_ARG, "m = %llu, n = %llu, k = %llu exceed the limits of 2^27, 2^27 and 2^24",
+                    (unsigned long long)m, (unsigned long long)n, (unsigned long long)k);
     return HV_OK;
 }
 
@@ -107,7 +115,7 @@ hv_status hv_fp8_gated(hv_type type, const void* gate, uint64_t ld_gate, const v
 }
 
 size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k) {
-    if (m > kMaxSide || n > kMaxSide || k > kMaxCols) return 0;
+    if (m == 0 || n == 0 || m > kMaxSide || n > kMaxSide || k > kMaxCols) return 0;
     return round_up(hv::fp8_matmul_workspace(m, n, k));
 }
 
@@ -115,9 +123,7 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
                         uint64_t ld_b, const float* b_scales, uint64_t m, uint64_t n, uint64_t k, void* c,
                         uint64_t ld_c, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     HV_TRY(check_type(type));
-    if (m > kMaxSide || n > kMaxSide || k > kMaxCols)
-        return fail(HV_ERR_INVALID_ARG, "m = %llu, n = %llu, k = %llu exceed the limits of 2^27, 2^27 and 2^24",
-                    (unsigned long long)m, (unsigned long long)n, (unsigned long long)k);
+    HV_TRY(check_product(m, n, k));
     if (m == 0 || n == 0) return HV_OK;
     if (k > 0) {
         HV_TRY(check_matrix("a", a, 1, ld_a, k));
@@ -135,6 +141,23 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
     }
     const hv::MatmulArgs args = {a, ld_a, a_scales, b, ld_b, b_scales, m, n, k, c, ld_c, workspace};
     return done(hv::launch_fp8_matmul(type, args, stream), "product kernel");
+}
+
+hv_status hv_fp8_matmul_launches(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k, int* launches, int* kind,
+                                 uint64_t* rows, uint64_t* cols, uint32_t* splits) {
+    HV_TRY(check_type(type));
+    HV_TRY(check_product(m, n, k));
+    if (launches == nullptr || kind == nullptr || rows == nullptr || cols == nullptr || splits == nullptr)
+        return fail(HV_ERR_INVALID_ARG, "launches, kind, rows, cols and splits must be non-NULL");
+    hv::MatmulPart parts[2];
+    *launches = m == 0 || n == 0 ? 0 : hv::fp8_matmul_parts(type == HV_F32, aligned != 0, true, m, n, k, parts);
+    for (int i = 0; i < *launches; ++i) {
+        kind[i] = parts[i].kind;
+        rows[i] = parts[i].rows;
+        cols[i] = parts[i].cols;
+        splits[i] = parts[i].splits;
+    }
+    return HV_OK;
 }
 
 }  // extern "C"

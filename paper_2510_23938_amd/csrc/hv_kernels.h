@@ -252,6 +252,28 @@ hipError_t launch_fp8_rms_norm(int type, const NormArgs& a, hipStream_t s);
 hipError_t launch_fp8_gated(int type, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
                             uint64_t rows, uint64_t cols, uint8_t* codes, uint64_t ld_codes, float* scales,
                             hipStream_t s);
+// What a product is made by: its kernels (hv_fp8_matmul_launches has the same
+// numbers), the parts of A's columns each takes, and the outputs it makes; the second
+// part has the last rows or the last columns.
+enum : int {
+    kMatmulZeros = 0,    // no columns
+    kMatmulStream1 = 1,  // 16 rows, B straight from memory; 1, 2, 4 or 7 fragments a workgroup
+    kMatmulStream2 = 2,
+    kMatmulStream4 = 3,
+    kMatmulStream7 = 4,
+    kMatmul256x256 = 5,  // tiles in LDS
+    kMatmul256x128 = 6,
+    kMatmul192x128 = 7,
+    kMatmul128x128 = 8,
+    kMatmulUnaligned = 9,  // 128 x 128, rows at any address
+};
+struct MatmulPart {
+    int kind;
+    uint32_t splits;
+    uint64_t rows, cols;
+};
+// wide: a 32-bit result; aligned: 16-byte aligned rows; tiles: leading dimensions below 2^23.
+int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k, MatmulPart parts[2]);
 // Scratch bytes for any type and alignment.
 uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);

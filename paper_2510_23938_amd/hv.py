@@ -54,7 +54,7 @@ EXPORTS = (
     "hv_hash_chunks_alg", "hv_merkle_workspace_bytes_alg", "hv_merkle_reduce_alg", "hv_verify_root_alg",
     "hv_compare_roots_alg", "hv_hash_chunks_noalloc", "hv_last_error", "hv_set_kernel_timing", "hv_leaf_kernel_ms",
     "hv_leaf_schedule", "hv_set_leaf_kernel", "hv_leaf_kernel_for", "hv_leaf_launch_for", "hv_set_handover_polls",
-    "hv_merkle_launches",  # include/hv_inspect.h
+    "hv_merkle_launches", "hv_fp8_matmul_launches",  # include/hv_inspect.h
     "hv_mb_valu", "hv_mb_sha256", "hv_mb_valu64", "hv_mb_sha384", "hv_mb_op_rate",
     "hv_mb_hbm_read",  # include/hv_microbench.h
     "hv_stream_workspace_bytes", "hv_hash_host_chunks", "hv_hash_host_chunks_alg",  # include/hv_stream.h
@@ -138,6 +138,7 @@ def _load():
         "hv_set_handover_polls": ([u32], ctypes.c_int),
         "hv_merkle_launches": ([ctypes.c_int32, ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_void_p,
                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+        "hv_fp8_matmul_launches": ([ctypes.c_int32, ctypes.c_int, u64, u64, u64, vp, vp, vp, vp, vp], ctypes.c_int),
         "hv_mb_valu": ([vp, u32, u32, vp, vp], ctypes.c_int),
         "hv_mb_hbm_read": ([vp, u64, vp, u32, vp], ctypes.c_int),
         "hv_mb_sha256": ([vp, u32, u32, vp, vp], ctypes.c_int),
@@ -653,6 +654,20 @@ def merkle_launches(seg_offsets, alg: str = "sha256", cus: int = 0) -> list:
     units, one = (ctypes.c_uint64 * 8)(), (ctypes.c_uint64 * 8)()
     _check(lib.hv_merkle_launches(code, seg.ctypes.data, len(seg) - 1, int(cus), ctypes.byref(n), kind, units, one))
     return [({1: "group", 2: "tile"}[kind[k]], int(units[k]), int(one[k])) for k in range(n.value)]
+
+
+_MATMUL_KINDS = ("zeros", "stream16", "stream32", "stream64", "stream112", "256x256", "256x128", "192x128", "128x128",
+                 "128x128 unaligned")
+
+
+def matmul_launches(m: int, n: int, k: int, dtype=torch.bfloat16, aligned: bool = True) -> list:
+    """The launches hv_fp8_matmul makes for these sizes (rows 16-byte aligned or not): (kernel, rows, cols,
+    parts of the columns whose sums one more launch adds) each."""
+    count = ctypes.c_int(0)
+    kind, rows, cols, splits = (ctypes.c_int * 2)(), (ctypes.c_uint64 * 2)(), (ctypes.c_uint64 * 2)(), (ctypes.c_uint32 * 2)()
+    _check(lib.hv_fp8_matmul_launches(TYPES[dtype], 1 if aligned else 0, m, n, k, ctypes.byref(count), kind, rows, cols,
+                                      splits))
+    return [(_MATMUL_KINDS[kind[i]], int(rows[i]), int(cols[i]), int(splits[i])) for i in range(count.value)]
 
 
 def set_kernel_timing(enable: bool):

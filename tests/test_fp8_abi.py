@@ -64,3 +64,29 @@ def test_workspace_sizes():
                 args = {**MATMUL, "m": m, "n": n, "k": k, "ld_a": k, "ld_b": k, "ld_c": n}
                 for change in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 8)):
                     assert hv.lib.hv_fp8_matmul(*{**args, **change}.values(), None) == hv.HV_ERR_WORKSPACE
+
+
+def test_which_kernels_a_product_takes():
+    """The rule's cases: each kernel is taken for some size, and each part covers its rows and columns."""
+    bf16, f32 = hv.torch.bfloat16, hv.torch.float32
+    taken = {}
+    for dtype in (bf16, f32):
+        for aligned in (True, False):
+            for m in (1, 4, 8, 16, 17, 64, 150, 256, 333, 1000, 2048, 4096):
+                for n in (64, 1024, 4096, 5001, 11008, 16384, 28672):
+                    for k in (0, 100, 1024, 4093, 28672):
+                        parts = hv.matmul_launches(m, n, k, dtype, aligned)
+                        assert sum(r * c for _, r, c, _ in parts) == m * n
+                        if len(parts) == 2:
+                            (_, r0, c0, _), (_, r1, c1, _) = parts
+                            assert (r0 == r1 == m and c0 + c1 == n and c0 % 256 == 0) or \
+                                (c0 == c1 == n and r0 + r1 == m and r0 % 256 == 0)
+                        for kind, _, _, splits in parts:
+                            taken.setdefault(kind, set()).add(splits > 1)
+                            assert splits == 1 or kind.startswith("128x128")
+                            assert (kind == "128x128 unaligned") == (not aligned and m > 16 and k > 0)
+    assert set(taken) == set(hv._MATMUL_KINDS)
+    assert taken["128x128"] == taken["128x128 unaligned"] == {True, False}
+    assert [p[0] for p in hv.matmul_launches(2048, 28672, 8192)] == ["256x256", "256x128"]
+    assert hv.matmul_launches(0, 5, 5) == []
+    assert hv.lib.hv_fp8_matmul_launches(0, 1, 1, 1, 1, None, None, None, None, None) == hv.HV_ERR_INVALID_ARG

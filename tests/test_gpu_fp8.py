@@ -314,6 +314,36 @@ def test_matmul_columns_in_parts(m, n, k, pad):
         product(m, n, k, dtype, pad)
 
 
+def test_matmul_offsets_past_32_bits():
+    """Rows that start beyond 4 GiB, of every operand and of the result."""
+    rng = np.random.default_rng(16)
+    rows, ld, k = 70000, 65536, 200
+    host, (a, sa, b, sb) = operands(rng, rows, 130, k)
+    wide = torch.empty(rows, ld, dtype=torch.uint8, device=DEV)
+    at = slice(rows - 40, rows)  # the oracle looks at the last rows
+    for kind in ("a", "b"):
+        big = wide[:, 16:16 + k].view(torch.float8_e4m3fn)
+        big.view(torch.uint8).copy_(a.view(torch.uint8))
+        if kind == "a":  # many rows of A: tiles; and C's rows as far apart
+            out = torch.empty(rows, 40000, dtype=torch.bfloat16, device=DEV)[:, :130]
+            got = hv.hv_fp8_matmul(big, sa, b, sb, out=out)[at].double().cpu().numpy()
+            check_product(got, (host[0][at], host[1][at], host[2], host[3]), "bf16", near=False)
+        else:  # many rows of B: few rows of A straight from memory, then tiles
+            scales = torch.ones(-(-rows // 128), 2, device=DEV)
+            for m in (3, 130):
+                got = hv.hv_fp8_matmul(b[:m], sb[0].expand(m, 2).contiguous(), big, scales, torch.float32)
+                want = (host[2][:m], np.repeat(host[3][:1], m, 0), host[0][rows - 96:], np.ones((1, 2)))
+                check_product(got[:, rows - 96:].double().cpu().numpy(), want, "f32")
+    x = torch.empty(rows, ld, dtype=torch.float16, device=DEV)[:, :k]
+    x.copy_(torch.randn(rows, k, device=DEV))
+    for tile, t in (("rows", 1), ("blocks", 128)):
+        codes, scales = hv.hv_fp8_quantize(x, tile, out=big)
+        y = x[rows - 112:].double().cpu().numpy()
+        want = fp8.group_scales(y, t)
+        assert np.array_equal(scales.cpu().numpy()[-len(want):], want)
+        check_codes(bytes_of(codes[rows - 112:]), y, want, t, Q_ERROR)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("m,n,k", [(1, 500, 1024), (40, 300, 500), (150, 256, 2048), (512, 512, 768)])
 def test_matmul_codes_of_all_magnitudes(m, n, k, dtype):
