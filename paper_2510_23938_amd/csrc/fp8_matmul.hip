@@ -660,7 +660,7 @@ constexpr Cost kCost[2][kShapes] = {
      {128, 128, 8.0f, 1.10f, 0.88f},
      {128, 128, 8.6f, 1.27f, 0.95f}}};
 constexpr uint64_t kUnits = 256;  // compute units: one tile each at a time
-constexpr uint32_t kMaxSplits = 16;
+constexpr uint32_t kMaxSplits = 64;
 // Adding up the splits' sums: a launch and 4 bytes of each sum there and back (three
 // splits of 128 x 8192 8 us, of 32 x 1024 3 us).
 float join_cost(uint64_t m, uint64_t n, uint32_t splits) {
@@ -679,7 +679,7 @@ float rounds_cost(const Cost& c, uint64_t tiles, uint64_t groups) {
 }
 
 // The cheapest single shape, with the columns of A and B in parts where that
-// pays: few tiles, many groups.
+// pays: few tiles or a last round of few, many groups.
 struct Choice {
     Shape shape;
     uint32_t splits;
@@ -690,7 +690,7 @@ Choice choose(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) 
     for (int s = aligned ? (wide ? k256x128 : k256x256) : kUnaligned; s < (aligned ? kUnaligned : kShapes); ++s) {
         const Cost& c = kCost[wide][s];
         const uint64_t tiles = tiles_of(c, m, n);
-        const uint32_t most = c.rows != 128 || tiles >= kUnits ? 1 : kMaxSplits;
+        const uint32_t most = c.rows != 128 || tiles >= 4 * kUnits ? 1 : kMaxSplits;
         for (uint32_t p = 1; p <= most && (p == 1 || groups / p >= 4); ++p) {
             const float cost = rounds_cost(c, tiles * p, (groups + p - 1) / p) + join_cost(m, n, p);
             if (best.shape == kShapes || cost < best.cost) best = {(Shape)s, p, cost};
@@ -721,16 +721,22 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
     return plan;
 }
 
-// A workgroup's fragments of B share one of A, whose 16 rows take as many loads as
-// theirs: several pay where there are several rows of A and enough columns for
-// every unit (8 x 28672 x 8192: 57 us by single fragments, 47 by 7; 1 x 28672 x
-// 8192: 42 and 48; 16 x 8192 x 28672: 71 by single ones, 56 by 2).
-int stream_kind(uint64_t m, uint64_t n, uint64_t groups) {
+// A workgroup's fragments of B share one of A, whose rows take as many loads as
+// theirs, and a unit with one workgroup more than others is the last to end: the
+// fewest loads of a unit that has the most (8 x 28672 x 8192: 57 us by single
+// fragments, 56 by 2, 50 by 4, 47 by 7; 16 x 8192 x 28672 71, 56, 78 and 112).  Up to four
+// rows of A take next to nothing (1 x 28672 x 8192: 42, 56, 48, 48).
+int stream_kind(uint64_t m, uint64_t n) {
+    constexpr int kFragments[] = {1, 2, 4, 7};
     const uint64_t fragments = (n + 15) / 16;
-    if (m <= 4) return kMatmulStream1;
-    if (fragments > 6 * kUnits) return kMatmulStream7;
-    if (fragments > 3 * kUnits) return kMatmulStream4;
-    return fragments > kUnits && groups > 64 ? kMatmulStream2 : kMatmulStream1;
+    int best = 0;
+    uint64_t least = 0;
+    for (int i = 0; i < (m <= 4 ? 1 : 4); ++i) {
+        const uint64_t each = kFragments[i], workgroups = (fragments + each - 1) / each;
+        const uint64_t loads = (workgroups + kUnits - 1) / kUnits * (16 * each + m);
+        if (i == 0 || loads < least) best = i, least = loads;
+    }
+    return kMatmulStream1 + best;
 }
 
 }  // namespace
@@ -740,7 +746,7 @@ int stream_kind(uint64_t m, uint64_t n, uint64_t groups) {
 int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k, MatmulPart parts[2]) {
     const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
     if (groups == 0 || m <= 16 || !tiles) {
-        parts[0] = {groups == 0 ? kMatmulZeros : stream_kind(m, n, groups), 1, m, n};
+        parts[0] = {groups == 0 ? kMatmulZeros : stream_kind(m, n), 1, m, n};
         return 1;
     }
     const Plan plan = plan_of(wide, aligned, m, n, groups);

@@ -205,6 +205,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
     };
     if (lanes <= tx) return run(norm_kernel<T, 1, kResidual>);
     if (lanes <= 2 * tx) return run(norm_kernel<T, 2, kResidual>);
+    if (lanes <= 3 * tx) return run(norm_kernel<T, 3, kResidual>);
     if (lanes <= 4 * tx) return run(norm_kernel<T, 4, kResidual>);
     return run(norm_kernel<T, 0, kResidual>);
 }
