@@ -87,9 +87,11 @@ hv_status hv_fp8_gated(hv_type type, const void* gate, uint64_t ld_gate, const v
                        uint64_t rows, uint64_t cols, uint8_t* codes, uint64_t ld_codes, float* scales,
                        hipStream_t stream);
 
-/* Scratch bytes hv_fp8_matmul needs for these sizes; 0 where it needs none, and
- * for sizes that the call refuses. */
-size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
+/* Scratch bytes hv_fp8_matmul needs for a result of the type and these sizes; 0
+ * where it needs none, and for a type or sizes that the call refuses.
+ *   aligned: nonzero where a and b are 16-byte aligned and ld_a and ld_b multiples
+ *            of 16 (other rows may be copied to aligned ones first). */
+size_t hv_fp8_matmul_workspace_bytes(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k);
 
 /* c [m][n] = A times the transpose of B, for A [m][k] with scales by rows and B
  * [n][k] with scales by blocks:
@@ -102,8 +104,8 @@ size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
  * k = 0 gives zeros.  The product of any two scales that meet has to be finite in
  * 32 bits.
  *   c: [m][n] of the type, with leading dimension ld_c.
- *   workspace: >= hv_fp8_matmul_workspace_bytes(m, n, k), 256-byte aligned; NULL
- *              where that is 0.  Scratch: calls that share one must share a
+ *   workspace: >= hv_fp8_matmul_workspace_bytes(...), 256-byte aligned; NULL where
+ *              that is 0.  Scratch: calls that share one must share a
  *              stream.
  * Errors: HV_ERR_INVALID_ARG also for m or n above 2^27; HV_ERR_WORKSPACE for a
  * missing, short or misaligned workspace. */

@@ -574,6 +574,19 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
         store((T*)x.c, x.ld_c);
 }
 
+// A's or B's rows, 16 bytes a lane, to aligned ones of ld_to >= k bytes (a multiple of
+// 16; zeros beyond the columns).
+__global__ void __launch_bounds__(256) pack_kernel(const uint8_t* __restrict__ from, uint64_t ld, uint32_t rows,
+                                                   uint32_t k, uint8_t* __restrict__ to, uint64_t ld_to) {
+    const uint32_t chunks = (uint32_t)(ld_to / 16);
+    const uint64_t count = (uint64_t)rows * chunks;
+    for (uint64_t c = (uint64_t)blockIdx.x * 256 + threadIdx.x; c < count; c += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = c / chunks;
+        const uint32_t at = (uint32_t)(c % chunks) * 16;
+        *(int4x*)(to + row * ld_to + at) = load_16(from + row * ld + at, (int)(k - at), k);
+    }
+}
+
 // Adds the splits' sums, in their order (no splits: zeros).
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ sums, uint32_t splits, uint32_t m,
@@ -653,12 +666,12 @@ constexpr Cost kCost[2][kShapes] = {
      {256, 128, 7.2f, 0.98f, 0.63f},
      {192, 128, 6.3f, 0.77f, 0.53f},
      {128, 128, 5.4f, 0.56f, 0.38f},
-     {128, 128, 6.4f, 0.72f, 0.56f}},
+     {128, 128, 10.0f, 0.95f, 0.78f}},
     {{256, 256, 0, 0, 0},  // 32-bit results: the widened codes leave no registers for it
      {256, 128, 8.5f, 2.03f, 1.35f},
      {192, 128, 7.8f, 1.60f, 1.13f},
      {128, 128, 8.0f, 1.10f, 0.88f},
-     {128, 128, 8.6f, 1.27f, 0.95f}}};
+     {128, 128, 12.7f, 1.35f, 1.10f}}};
 constexpr uint64_t kUnits = 256;  // compute units: one tile each at a time
 constexpr uint32_t kMaxSplits = 64;
 // Adding up the splits' sums: a launch and 4 bytes of each sum there and back (three
@@ -739,22 +752,39 @@ int stream_kind(uint64_t m, uint64_t n) {
     return kMatmulStream1 + best;
 }
 
+// Copying rows to aligned ones, in us: two launches (a small product waits for the
+// host to make them), and each byte there and back.
+float pack_cost(uint64_t m, uint64_t n, uint64_t k) { return 12.0f + (float)(m + n) * (float)k * 2.0f / 4.5e6f; }
+
 }  // namespace
 
 // Tiles serve more than 16 rows: a workgroup then reads B's rows for 128 of A's at
 // once (32 x 8192 x 8192 17 us, 28 by fragments of 16 rows).
-int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k, MatmulPart parts[2]) {
+int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k,
+                     MatmulPart parts[kMatmulMostParts]) {
     const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
     if (groups == 0 || m <= 16 || !tiles) {
         parts[0] = {groups == 0 ? kMatmulZeros : stream_kind(m, n), 1, m, n};
         return 1;
     }
-    const Plan plan = plan_of(wide, aligned, m, n, groups);
-    parts[0] = {kMatmul256x256 + plan.main.shape, plan.main.splits, plan.rows, plan.cols};
-    if (plan.rows == m && plan.cols == n) return 1;
-    parts[1] = {kMatmul256x256 + plan.rest.shape, plan.rest.splits, plan.rows < m ? m - plan.rows : m,
-                plan.cols < n ? n - plan.cols : n};
-    return 2;
+    int count = 0;
+    Plan plan = plan_of(wide, true, m, n, groups);
+    if (!aligned) {
+        // Rows at any address go through registers to LDS in tiles of 128 x 128 alone;
+        // where there is much to multiply a copy of them is paid for by the larger tiles
+        // (866 x 16640 x 9809: 384 us, 250 with the copy).
+        const float cost = plan.main.cost + (plan.rows < m || plan.cols < n ? plan.rest.cost : 0.0f);
+        const Plan direct = plan_of(wide, false, m, n, groups);
+        if (cost + pack_cost(m, n, k) < direct.main.cost)
+            parts[count++] = {kMatmulPack, 1, m, n};
+        else
+            plan = direct;
+    }
+    parts[count++] = {kMatmul256x256 + plan.main.shape, plan.main.splits, plan.rows, plan.cols};
+    if (plan.rows < m || plan.cols < n)
+        parts[count++] = {kMatmul256x256 + plan.rest.shape, plan.rest.splits, plan.rows < m ? m - plan.rows : m,
+                          plan.cols < n ? n - plan.cols : n};
+    return count;
 }
 
 namespace {
@@ -773,45 +803,84 @@ hipError_t launch_part(const MatmulPart& p, const MatmulArgs& x, hipStream_t s) 
         case kMatmul256x128: return launch_tiles<T, 256, 128, 4, 2, 3, true>(x, p.splits, s);
         case kMatmul192x128: return launch_tiles<T, 192, 128, 2, 4, 3, true>(x, p.splits, s);
         case kMatmul128x128: return launch_tiles<T, 128, 128, 2, 4, 4, true>(x, p.splits, s);
-        default: return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, p.splits, s);
+        case kMatmulUnaligned: return launch_tiles<T, 128, 128, 2, 4, 4, false>(x, p.splits, s);
+        default: return hipErrorInvalidValue;
     }
 }
 
+// Where the copies of A and B and the splits' sums stand in the workspace.
+struct Scratch {
+    uint64_t ld, a, b, sums, bytes;
+};
+Scratch scratch_of(const MatmulPart* parts, int count, uint64_t m, uint64_t n, uint64_t k) {
+    auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
+    Scratch s = {(k + 15) / 16 * 16, 0, 0, 0, 0};
+    for (int i = 0; i < count; ++i) {
+        if (parts[i].kind == kMatmulPack) {
+            s.b = up(m * s.ld);
+            s.sums = s.b + up(n * s.ld);
+            s.bytes = s.sums;
+        }
+        const uint64_t sums = parts[i].splits > 1 ? parts[i].splits * parts[i].rows * parts[i].cols * 4 : 0;
+        if (s.sums + sums > s.bytes) s.bytes = s.sums + sums;
+    }
+    return s;
+}
+
+hipError_t launch_pack(const uint8_t* from, uint64_t ld, uint64_t rows, uint64_t k, uint8_t* to, uint64_t ld_to,
+                       hipStream_t s) {
+    const uint64_t blocks = (rows * (ld_to / 16) + 255) / 256;
+    pack_kernel<<<(uint32_t)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(from, ld, (uint32_t)rows, (uint32_t)k, to,
+                                                                        ld_to);
+    return hipGetLastError();
+}
+
+bool rows_aligned(const MatmulArgs& x) {
+    return x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
+}
+
 template <typename T>
-hipError_t launch(const MatmulArgs& x, hipStream_t s) {
-    const bool aligned = x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
+hipError_t launch(MatmulArgs x, hipStream_t s) {
     const bool tiles = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd;
-    MatmulPart parts[2];
-    const int count = fp8_matmul_parts(sizeof(T) == 4, aligned, tiles, x.m, x.n, x.k, parts);
-    MatmulArgs part = x;
-    part.m = parts[0].rows;
-    part.n = parts[0].cols;
-    const hipError_t e = launch_part<T>(parts[0], part, s);
-    if (e != hipSuccess || count == 1) return e;
-    const uint64_t groups = (x.k + kFp8Group - 1) / kFp8Group, row = x.m - parts[1].rows, col = x.n - parts[1].cols;
-    part.m = parts[1].rows;
-    part.n = parts[1].cols;
-    part.a += row * x.ld_a;
-    part.a_scales += row * groups;
-    part.b += col * x.ld_b;
-    part.b_scales += col / kFp8Group * groups;
-    part.c = (T*)x.c + row * x.ld_c + col;
-    return launch_part<T>(parts[1], part, s);
+    MatmulPart parts[kMatmulMostParts];
+    const int count = fp8_matmul_parts(sizeof(T) == 4, rows_aligned(x), tiles, x.m, x.n, x.k, parts);
+    const Scratch scratch = scratch_of(parts, count, x.m, x.n, x.k);
+    uint8_t* const workspace = (uint8_t*)x.workspace;
+    x.workspace = workspace + scratch.sums;
+    const uint64_t groups = (x.k + kFp8Group - 1) / kFp8Group;
+    const MatmulPart whole = {0, 1, x.m, x.n};
+    for (int i = 0; i < count; ++i) {
+        hipError_t e;
+        if (parts[i].kind == kMatmulPack) {
+            e = launch_pack(x.a, x.ld_a, x.m, x.k, workspace + scratch.a, scratch.ld, s);
+            if (e == hipSuccess) e = launch_pack(x.b, x.ld_b, x.n, x.k, workspace + scratch.b, scratch.ld, s);
+            x.a = workspace + scratch.a;
+            x.b = workspace + scratch.b;
+            x.ld_a = x.ld_b = scratch.ld;
+        } else {  // its first rows and columns, or (a second one) the last
+            const bool last = i > 0 && parts[i - 1].kind != kMatmulPack;
+            const uint64_t row = last ? whole.rows - parts[i].rows : 0, col = last ? whole.cols - parts[i].cols : 0;
+            MatmulArgs part = x;
+            part.m = parts[i].rows;
+            part.n = parts[i].cols;
+            part.a += row * x.ld_a;
+            part.a_scales += row * groups;
+            part.b += col * x.ld_b;
+            part.b_scales += col / kFp8Group * groups;
+            part.c = (T*)x.c + row * x.ld_c + col;
+            e = launch_part<T>(parts[i], part, s);
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
-uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k) {
-    uint64_t most = 0;
-    for (int v = 0; v < 4; ++v) {  // any type, any alignment
-        MatmulPart parts[2];
-        const int count = fp8_matmul_parts(v % 2 != 0, v / 2 != 0, true, m, n, k, parts);
-        for (int i = 0; i < count; ++i) {
-            const uint64_t need = parts[i].splits > 1 ? parts[i].splits * parts[i].rows * parts[i].cols * 4 : 0;
-            if (need > most) most = need;
-        }
-    }
-    return most;
+uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k) {
+    MatmulPart parts[kMatmulMostParts];
+    const int count = fp8_matmul_parts(wide, aligned, true, m, n, k, parts);
+    return scratch_of(parts, count, m, n, k).bytes;
 }
 
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& x, hipStream_t s) {

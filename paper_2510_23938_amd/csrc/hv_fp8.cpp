@@ -114,9 +114,9 @@ hv_status hv_fp8_gated(hv_type type, const void* gate, uint64_t ld_gate, const v
                 "gated kernel");
 }
 
-size_t hv_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k) {
-    if (m == 0 || n == 0 || m > kMaxSide || n > kMaxSide || k > kMaxCols) return 0;
-    return round_up(hv::fp8_matmul_workspace(m, n, k));
+size_t hv_fp8_matmul_workspace_bytes(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k) {
+    if (check_type(type) != HV_OK || check_product(m, n, k) != HV_OK || m == 0 || n == 0) return 0;
+    return round_up(hv::fp8_matmul_workspace(type == HV_F32, aligned != 0, m, n, k));
 }
 
 hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const float* a_scales, const uint8_t* b,
@@ -132,7 +132,8 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
         HV_TRY(check_matrix("b_scales", b_scales, sizeof(float), k, k));
     }
     HV_TRY(check_matrix("c", c, size_of(type), ld_c, n));
-    const size_t need = hv_fp8_matmul_workspace_bytes(m, n, k);
+    const bool aligned = ld_a % 16 == 0 && ld_b % 16 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0;
+    const size_t need = hv_fp8_matmul_workspace_bytes(type, aligned, m, n, k);
     if (need > 0) {
         if (workspace == nullptr || workspace_bytes < need)
             return fail(HV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu%s", need, workspace_bytes,
@@ -149,7 +150,7 @@ hv_status hv_fp8_matmul_launches(hv_type type, int aligned, uint64_t m, uint64_t
     HV_TRY(check_product(m, n, k));
     if (launches == nullptr || kind == nullptr || rows == nullptr || cols == nullptr || splits == nullptr)
         return fail(HV_ERR_INVALID_ARG, "launches, kind, rows, cols and splits must be non-NULL");
-    hv::MatmulPart parts[2];
+    hv::MatmulPart parts[hv::kMatmulMostParts];
     *launches = m == 0 || n == 0 ? 0 : hv::fp8_matmul_parts(type == HV_F32, aligned != 0, true, m, n, k, parts);
     for (int i = 0; i < *launches; ++i) {
         kind[i] = parts[i].kind;

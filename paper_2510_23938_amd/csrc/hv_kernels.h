@@ -266,16 +266,19 @@ enum : int {
     kMatmul192x128 = 7,
     kMatmul128x128 = 8,
     kMatmulUnaligned = 9,  // 128 x 128, rows at any address
+    kMatmulPack = 10,      // before the others: rows copied to aligned ones
 };
+constexpr int kMatmulMostParts = 3;
 struct MatmulPart {
     int kind;
     uint32_t splits;
     uint64_t rows, cols;
 };
 // wide: a 32-bit result; aligned: 16-byte aligned rows; tiles: leading dimensions below 2^23.
-int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k, MatmulPart parts[2]);
-// Scratch bytes for any type and alignment.
-uint64_t fp8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);
+int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k,
+                     MatmulPart parts[kMatmulMostParts]);
+// Scratch bytes (0 where leading dimensions are not below 2^23).
+uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 
 }  // namespace hv

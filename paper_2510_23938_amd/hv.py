@@ -174,7 +174,7 @@ def _load():
         "hv_fp8_rms_norm": ([ctypes.c_int32, vp, u64, vp, u64, vp, ctypes.c_float, u64, u64, vp, u64, vp, u64, vp,
                              vp], ctypes.c_int),
         "hv_fp8_gated": ([ctypes.c_int32, vp, u64, vp, u64, u64, u64, vp, u64, vp, vp], ctypes.c_int),
-        "hv_fp8_matmul_workspace_bytes": ([u64, u64, u64], sz),
+        "hv_fp8_matmul_workspace_bytes": ([ctypes.c_int32, ctypes.c_int, u64, u64, u64], sz),
         "hv_fp8_matmul": ([ctypes.c_int32, vp, u64, vp, vp, u64, vp, u64, u64, u64, vp, u64, vp, sz, vp],
                           ctypes.c_int),
     }
@@ -657,14 +657,15 @@ def merkle_launches(seg_offsets, alg: str = "sha256", cus: int = 0) -> list:
 
 
 _MATMUL_KINDS = ("zeros", "stream16", "stream32", "stream64", "stream112", "256x256", "256x128", "192x128", "128x128",
-                 "128x128 unaligned")
+                 "128x128 unaligned", "pack")
 
 
 def matmul_launches(m: int, n: int, k: int, dtype=torch.bfloat16, aligned: bool = True) -> list:
     """The launches hv_fp8_matmul makes for these sizes (rows 16-byte aligned or not): (kernel, rows, cols,
     parts of the columns whose sums one more launch adds) each."""
     count = ctypes.c_int(0)
-    kind, rows, cols, splits = (ctypes.c_int * 2)(), (ctypes.c_uint64 * 2)(), (ctypes.c_uint64 * 2)(), (ctypes.c_uint32 * 2)()
+    kind, splits = (ctypes.c_int * 3)(), (ctypes.c_uint32 * 3)()
+    rows, cols = (ctypes.c_uint64 * 3)(), (ctypes.c_uint64 * 3)()
     _check(lib.hv_fp8_matmul_launches(TYPES[dtype], 1 if aligned else 0, m, n, k, ctypes.byref(count), kind, rows, cols,
                                       splits))
     return [(_MATMUL_KINDS[kind[i]], int(rows[i]), int(cols[i]), int(splits[i])) for i in range(count.value)]
@@ -1270,7 +1271,8 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
         out_ptr, ld_out = out.data_ptr(), n
     else:
         out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", dev, (*lead, n))
-    need = lib.hv_fp8_matmul_workspace_bytes(m, n, k)
+    aligned = not (ld_a % 16 or ld_b % 16 or a_ptr % 16 or b_ptr % 16)
+    need = lib.hv_fp8_matmul_workspace_bytes(TYPES[dtype], aligned, m, n, k)
     ws = (workspace or Workspace(dev)).get(need) if need else None
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
                              ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(dev.index)))

@@ -54,16 +54,21 @@ def test_empty_calls_need_no_pointers():
 
 
 def test_workspace_sizes():
+    size = hv.lib.hv_fp8_matmul_workspace_bytes
     for m, n, k in ((0, 100, 100), (100, 0, 100), (1 << 31, 8, 8), (8, 8, (1 << 24) + 1)):
-        assert hv.lib.hv_fp8_matmul_workspace_bytes(m, n, k) == 0
-    for m in (1, 2, 16, 17, 64, 65, 128, 300, 2048, 100000):
-        for n, k in ((1, 1), (128, 28672), (1000, 1000), (8192, 8192), (57344, 128)):
-            need = hv.lib.hv_fp8_matmul_workspace_bytes(m, n, k)
-            assert need % 256 == 0
-            if need:
-                args = {**MATMUL, "m": m, "n": n, "k": k, "ld_a": k, "ld_b": k, "ld_c": n}
-                for change in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 8)):
-                    assert hv.lib.hv_fp8_matmul(*{**args, **change}.values(), None) == hv.HV_ERR_WORKSPACE
+        assert size(hv.HV_BF16, 1, m, n, k) == 0
+    assert size(7, 1, 100, 100, 1 << 20) == 0 and size(hv.HV_BF16, 1, 100, 100, 1 << 20) > 0
+    for t in (hv.HV_BF16, hv.HV_F32):
+        for m in (1, 2, 16, 17, 64, 65, 128, 300, 2048, 100000):
+            for n, k in ((1, 1), (128, 28672), (1000, 1000), (8192, 8192), (57344, 128), (500, 8191)):
+                for aligned in (0, 1):
+                    need = size(t, aligned, m, n, k)
+                    assert need % 256 == 0
+                    if need:
+                        ld = k + -k % 16 + (0 if aligned else 1)
+                        args = {**MATMUL, "type": t, "m": m, "n": n, "k": k, "ld_a": ld, "ld_b": ld, "ld_c": n}
+                        for change in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 8)):
+                            assert hv.lib.hv_fp8_matmul(*{**args, **change}.values(), None) == hv.HV_ERR_WORKSPACE
 
 
 def test_which_kernels_a_product_takes():
@@ -76,6 +81,11 @@ def test_which_kernels_a_product_takes():
                 for n in (64, 1024, 4096, 5001, 11008, 16384, 28672):
                     for k in (0, 100, 1024, 4093, 28672):
                         parts = hv.matmul_launches(m, n, k, dtype, aligned)
+                        packed = parts[0][0] == "pack"
+                        if packed:
+                            assert not aligned and m > 16 and parts[0][1:] == (m, n, 1)
+                            taken["pack"] = {False}
+                            parts = parts[1:]
                         assert sum(r * c for _, r, c, _ in parts) == m * n
                         if len(parts) == 2:
                             (_, r0, c0, _), (_, r1, c1, _) = parts
@@ -84,7 +94,7 @@ def test_which_kernels_a_product_takes():
                         for kind, _, _, splits in parts:
                             taken.setdefault(kind, set()).add(splits > 1)
                             assert splits == 1 or kind.startswith("128x128")
-                            assert (kind == "128x128 unaligned") == (not aligned and m > 16 and k > 0)
+                            assert (kind == "128x128 unaligned") == (not aligned and not packed and m > 16 and k > 0)
     assert set(taken) == set(hv._MATMUL_KINDS)
     assert taken["128x128"] == taken["128x128 unaligned"] == {True, False}
     assert [p[0] for p in hv.matmul_launches(2048, 28672, 8192)] == ["256x256", "256x128"]
