@@ -452,6 +452,11 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
 #pragma unroll
             for (int l = first; l < count; ++l) load(l, min(base + ahead, last_group), st);
         };
+        // the first scales before all else: LDS waits for them, and loads end in their order
+        const uint32_t run = base / kRun, start = min(run * kRun, last_run);
+#pragma unroll
+        for (uint32_t e = 0; e < kRun; ++e) held_scales[e] = tile_s[from_s + min(start + e, groups - 1)];
+        asm volatile("" ::: "memory");
         if constexpr (!kDirect) {
             load_all(0, kStage0, 0, kLoads);
             load_all(1, kStage1, 0, kLoads);
@@ -472,12 +477,9 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
             load_all(1, kStage1, 0, kLoads);
             if constexpr (S > 3) load_all(2, kStage2, 0, kLoads);
         }
-        const uint32_t run = base / kRun, start = min(run * kRun, last_run);
-#pragma unroll
-        for (uint32_t e = 0; e < kRun; ++e) held_scales[e] = tile_s[from_s + min(start + e, groups - 1)];
         keep_run(run);
         if (runs) load_run(run + 1);
-        meet(kNone);
+        meet(kLater);
         if constexpr (kDirect && S == 2) load_all(1, kStage1, 0, kLoadsA);
         if constexpr (kDirect && S == 3) load_all(2, kStage2, 0, NT < kLoads ? NT : kLoads);
         if constexpr (kDirect && S == 4) load_all(3, kStage3, 0, NT < kLoads ? NT : kLoads);
