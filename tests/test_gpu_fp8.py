@@ -365,17 +365,32 @@ def test_matmul_drawn_sizes():
         product(m, n, k, dtype, pad, offset, int(rng.integers(0, 6)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,n,k", [(5, 40, 300), (100, 200, 300), (300, 300, 512), (520, 520, 1024)])
-def test_matmul_nan_stays_in_its_row_and_column(m, n, k):
+def test_matmul_nan_stays_in_its_row_and_column(m, n, k, dtype):
     (a, sa, b, sb), _ = operands(np.random.default_rng(12), m, n, k)
+    sa *= np.float32(2.0 ** -10)  # within half precision
     a[m // 2, k - 1] = 0x7f
     b[n // 3, 0] = 0xff
     got = hv.hv_fp8_matmul(codes_on_gpu(a, 16), torch.from_numpy(sa).to(DEV), codes_on_gpu(b, 16),
-                           torch.from_numpy(sb).to(DEV), torch.float32).cpu().numpy()
+                           torch.from_numpy(sb).to(DEV), TYPES[dtype]).float().cpu().numpy()
+    assert not np.isinf(got).any()
     want = np.zeros((m, n), dtype=bool)
     want[m // 2] = True
     want[:, n // 3] = True
     assert np.array_equal(np.isnan(got), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 40, 700), (100, 200, 1100), (520, 520, 1024)])
+def test_matmul_scales_of_zero_and_nan(m, n, k):
+    (a, sa, b, sb), (ga, gsa, gb, gsb) = operands(np.random.default_rng(17), m, n, k)
+    gsa[1] = 0
+    gsa[m - 1, -1] = float("nan")
+    got = hv.hv_fp8_matmul(ga, gsa, gb, gsb).float().cpu().numpy()
+    assert (got[1] == 0).all() and np.isnan(got[m - 1]).all() and np.isfinite(got[:m - 1]).all()
+    gsb[0, 2] = float("nan")  # the first 128 columns
+    got = hv.hv_fp8_matmul(ga, gsa, gb, gsb).float().cpu().numpy()
+    assert np.isnan(got[:, :128]).all() and np.isfinite(got[:m - 1, 128:]).all()
 
 
 @pytest.mark.parametrize("m,n", [(3, 50), (200, 300)])
