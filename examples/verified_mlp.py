@@ -88,13 +88,14 @@ def main(argv=None):
     def inputs(tokens):
         return (torch.randn(tokens, args.d, device=dev, dtype=torch.bfloat16) for _ in range(2))
 
-    def timed(x, r):
+    def timed(x, r, first=lambda: None):
         mlp(x, r)
         torch.cuda.synchronize(dev)
+        first()
         t = time.perf_counter()
         for _ in range(args.steps):
             y, _ = mlp(x, r)
-        torch.cuda.synchronize(dev)
+        torch.cuda.current_stream(dev).synchronize()  # this stream's work only
         t = time.perf_counter() - t
         assert bool(torch.isfinite(y).all())
         return t / args.steps
@@ -106,10 +107,10 @@ def main(argv=None):
     print(f"decode of {args.decode} sequences: {s * 1e6:.0f} us, {nbytes / s / 1e9:.0f} GB/s of weights")
 
     mon = mlp.monitor()
-    mon.sweep()  # its scans are in flight beside the decode steps
-    s = timed(*inputs(args.decode))
+    s = timed(*inputs(args.decode), mon.sweep)  # its scans are in flight beside the decode steps
+    still = "still" if not mon.stream.query() else "no longer"
     mon.poll(wait=True)
-    print(f"decode beside the monitor: {s * 1e6:.0f} us; changed chunks: {mon.mismatches}")
+    print(f"decode beside the monitor ({still} at work at the end): {s * 1e6:.0f} us; changed chunks: {mon.mismatches}")
     layer[1][0].view(torch.uint8)[0, 0] ^= 1  # one bit of one code
     torch.cuda.synchronize(dev)
     mon.sweep()
