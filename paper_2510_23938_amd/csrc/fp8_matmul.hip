@@ -122,10 +122,11 @@ template <typename T, int NT, int kAhead>
 __global__ void __launch_bounds__(kStreamWaves * 64)
     stream_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
                   const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
-                  uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m) {
+                  uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m, uint64_t first) {
     __shared__ float4x part[kStreamWaves][NT][64];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t i0 = blockIdx.x % tiles_m * 16, j0 = blockIdx.x / tiles_m * 16 * NT;
+    const uint64_t tile = first + blockIdx.x;
+    const uint32_t i0 = (uint32_t)(tile % tiles_m) * 16, j0 = (uint32_t)(tile / tiles_m) * 16 * NT;
     const uint32_t groups = (k + kFp8Group - 1) / kFp8Group, whole = k / kFp8Group;
     const uint32_t at = lane / 16 * 16;
     const uint32_t row_of_a = min(i0 + lane % 16, m - 1);
@@ -655,10 +656,16 @@ template <typename T, int NT, int kAhead>
 hipError_t launch_stream(const MatmulArgs& x, hipStream_t s) {
     const uint32_t tiles_m = (uint32_t)((x.m + 15) / 16);
     const uint64_t tiles = tiles_m * ((x.n + 16 * NT - 1) / (16 * NT));
-    stream_kernel<T, NT, kAhead><<<(uint32_t)tiles, kStreamWaves * 64, 0, s>>>(
-        x.a, x.ld_a, x.a_scales, x.b, x.ld_b, x.b_scales, (uint32_t)x.m, (uint32_t)x.n, (uint32_t)x.k, (T*)x.c, x.ld_c,
-        tiles_m);
-    return hipGetLastError();
+    constexpr uint64_t kMost = 1u << 22;  // workgroups of a launch: 2^31 lanes
+    for (uint64_t first = 0; first < tiles; first += kMost) {
+        const uint64_t count = tiles - first < kMost ? tiles - first : kMost;
+        stream_kernel<T, NT, kAhead><<<(uint32_t)count, kStreamWaves * 64, 0, s>>>(
+            x.a, x.ld_a, x.a_scales, x.b, x.ld_b, x.b_scales, (uint32_t)x.m, (uint32_t)x.n, (uint32_t)x.k, (T*)x.c,
+            x.ld_c, tiles_m, first);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ---------------------------------------------------------------------------

@@ -9,7 +9,7 @@ namespace {
 
 constexpr uint64_t kMaxRows = ((uint64_t)1 << 31) - 1;
 constexpr uint64_t kMaxCols = (uint64_t)1 << 24;
-constexpr uint64_t kMaxSide = (uint64_t)1 << 27;  // of a product: a workgroup of 512 per 16 columns stays below 2^32
+constexpr uint64_t kMaxSide = (uint64_t)1 << 27;  // of a product: rows and columns, rounded up to tiles, count in 32 bits
 constexpr uint64_t kMaxLd = (uint64_t)1 << 31;
 
 static_assert(HV_BF16 == hv::kTypeBf16 && HV_F16 == hv::kTypeF16 && HV_F32 == hv::kTypeF32, "element types");

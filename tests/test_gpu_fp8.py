@@ -314,6 +314,23 @@ def test_matmul_columns_in_parts(m, n, k, pad):
         product(m, n, k, dtype, pad)
 
 
+@pytest.mark.parametrize("call,rows,cols", [("rows", 1_100_000, 24), ("gated", 1_100_000, 24), ("blocks", (1 << 27) + 300, 1),
+                                            ("norm", (1 << 24) + 3000, 8), ("norm", (1 << 20) + 5, 1100)])
+def test_more_rows_than_a_launch_has_workgroups(call, rows, cols):
+    """The last rows, which a workgroup makes after its first ones, as a call of their own makes them."""
+    x = torch.randn(rows, cols, dtype=torch.bfloat16, device=DEV)
+
+    def run(x):
+        if call == "norm":
+            return hv.hv_fp8_rms_norm(x, torch.ones(cols, dtype=x.dtype, device=DEV), 1e-5, residual=x)
+        return hv.hv_fp8_gated(x, x) if call == "gated" else hv.hv_fp8_quantize(x, call)
+
+    last = (rows - 1000) // 128 * 128  # a block's first row
+    whole, first, tail = run(x), run(x[:1024]), run(x[last:])
+    for w, f, t in zip(whole, first, tail):
+        assert np.array_equal(bytes_of(w[:len(f)]), bytes_of(f)) and np.array_equal(bytes_of(w[-len(t):]), bytes_of(t))
+
+
 def test_matmul_offsets_past_32_bits():
     """Rows that start beyond 4 GiB, of every operand and of the result."""
     rng = np.random.default_rng(16)
@@ -342,6 +359,18 @@ def test_matmul_offsets_past_32_bits():
         want = fp8.group_scales(y, t)
         assert np.array_equal(scales.cpu().numpy()[-len(want):], want)
         check_codes(bytes_of(codes[rows - 112:]), y, want, t, Q_ERROR)
+
+
+def test_matmul_of_the_most_columns():
+    """2^27 columns by single fragments are more workgroups than a launch may have."""
+    n, k = 1 << 27, 16
+    b = torch.randint(0, 0x7f, (n, k), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    sb = torch.rand(n // 128, 1, device=DEV)
+    a, sa = hv.hv_fp8_quantize(torch.randn(1, k, device=DEV))
+    got = hv.hv_fp8_matmul(a, sa, b, sb)
+    for first in (0, (1 << 26) - 512, n - 1024):
+        part = hv.hv_fp8_matmul(a, sa, b[first:first + 1024], sb[first // 128:first // 128 + 8])
+        assert np.array_equal(bytes_of(got[:, first:first + 1024]), bytes_of(part))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
