@@ -21,7 +21,9 @@ Each of the four takes ``alg="sha256"`` (default; 32-byte digests) or
 plus compositions used by callers: ``manifest_root`` (per-tensor roots, then
 one root over them in the given order -- the paper's hierarchical roots) and
 ``verify`` (raises ``VerificationError`` on a mismatch, as the paper's
-loader does when a model fails its check).
+loader does when a model fails its check), and the operators on matrices held
+in 8 bits (``include/hv_fp8.h``): ``hv_fp8_quantize``, ``hv_fp8_rms_norm``,
+``hv_fp8_gated`` and ``hv_fp8_matmul``.
 """
 from __future__ import annotations
 
