@@ -283,17 +283,16 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wave_i = wave / WN * (TM / WM), wave_j = wave % WN * (TN / WN);
     const uint32_t groups = (k + kFp8Group - 1) / kFp8Group;  // of a row
-    // The split's groups are [base, end), `whole` of them filled by the columns; base
-    // is a multiple of kRun.
-    const uint32_t base = split * tiles.groups, end = min(base + tiles.groups, groups);
-    const uint32_t whole = min(end, k / kFp8Group) - base, last_group = base + whole - 1;
+    // The split's groups are counted from `base`: `count` of them, `whole` of them filled by the columns.
+    const uint32_t base = split * tiles.groups, count = min(tiles.groups, groups - base);
+    const uint32_t whole = min(base + count, k / kFp8Group) - base, last_group = whole - 1;
 
     // The row of LDS that a lane of load instruction l fills is 8 * (l * waves + wave) + lane / 8; its
     // 16-byte places hold the row's chunks in the order place ^ (row % 8), so that
     // the lanes of a fragment read from different banks.
     const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
-    const uint8_t* const tile_a = x.a + i0 * x.ld_a;
-    const uint8_t* const tile_b = x.b + j0 * x.ld_b;
+    const uint8_t* const tile_a = x.a + i0 * x.ld_a + base * kFp8Group;
+    const uint8_t* const tile_b = x.b + j0 * x.ld_b + base * kFp8Group;
     uint32_t from_a[kLoadsA], from_b[kLoadsB];
 #pragma unroll
     for (int l = 0; l < kLoadsA; ++l)
@@ -303,8 +302,8 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
         from_b[l] = min(8 * (l * WM * WN + wave) + lane / 8, n - 1 - j0) * (uint32_t)x.ld_b + chunk;
     const uint32_t part_s = wave % (kScales / 64);  // waves beyond them load a part again
     const bool scales_of_a = part_s < TM / 64;
-    const float* const tile_s = scales_of_a ? x.a_scales + (uint64_t)i0 * groups
-                                            : x.b_scales + (uint64_t)(j0 / kFp8Group) * groups;
+    const float* const tile_s =
+        base + (scales_of_a ? x.a_scales + (uint64_t)i0 * groups : x.b_scales + (uint64_t)(j0 / kFp8Group) * groups);
     const uint32_t from_s = (scales_of_a ? min(part_s * 64 + lane, m - 1 - i0)
                                          : min(lane, (n - 1) / kFp8Group - j0 / kFp8Group)) * groups;
 
@@ -333,8 +332,8 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
     // are fewer left, and are kept in LDS as [row][4].  A run is asked for kRun
     // groups before it goes there, at steps that the unrolled loop fixes: where a branch
     // decided, the compiler would wait there for all loads.
-    const uint32_t last_run = max(groups, (uint32_t)kRun) - kRun;
-    const bool runs = groups > kRun;
+    const uint32_t last_run = max(count, (uint32_t)kRun) - kRun;
+    const bool runs = count > kRun;
     float4x held_scales;
     auto load_run = [&](uint32_t r) { __builtin_memcpy(&held_scales, tile_s + from_s + min(kRun * r, last_run), 4 * kRun); };
     auto keep_run = [&](uint32_t r) { scales[r % 2][64 * part_s + lane] = held_scales; };
@@ -389,7 +388,7 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
     float scale_a, scale_b;
     const uint32_t b_scale = 4 * (TM + wave_j / kFp8Group);
     auto multiply = [&](uint32_t g, auto step) {
-        constexpr int U = decltype(step)::value, ST = U % S;  // g is U modulo kUnroll, from base on
+        constexpr int U = decltype(step)::value, ST = U % S;  // g is U modulo kUnroll
         constexpr std::integral_constant<int, ST> st;
         constexpr std::integral_constant<int, ST + 1> kNext;
         constexpr std::integral_constant<int, ST + S - 1> kLast;  // the stage before, which loads still go to
@@ -461,14 +460,13 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
     constexpr std::integral_constant<int, 3> kStage3;
 
     if (whole > 0) {
-        auto load_all = [&](uint32_t ahead, auto st, int first, int count) {
+        auto load_all = [&](uint32_t ahead, auto st, int first, int end) {
 #pragma unroll
-            for (int l = first; l < count; ++l) load(l, min(base + ahead, last_group), st);
+            for (int l = first; l < end; ++l) load(l, min(ahead, last_group), st);
         };
         // the first scales before all else: LDS waits for them, and loads end in their order
-        const uint32_t run = base / kRun, start = min(run * kRun, last_run);
 #pragma unroll
-        for (uint32_t e = 0; e < kRun; ++e) held_scales[e] = tile_s[from_s + min(start + e, groups - 1)];
+        for (uint32_t e = 0; e < kRun; ++e) held_scales[e] = tile_s[from_s + min(e, count - 1)];
         asm volatile("" ::: "memory");
         if constexpr (!kDirect) {
             load_all(0, kStage0, 0, kLoads);
@@ -490,8 +488,8 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
             load_all(1, kStage1, 0, kLoads);
             if constexpr (S > 3) load_all(2, kStage2, 0, kLoads);
         }
-        keep_run(run);
-        if (runs) load_run(run + 1);
+        keep_run(0);
+        if (runs) load_run(1);
         meet(kLater);
         if constexpr (kDirect && S == 2) load_all(1, kStage1, 0, kLoadsA);
         if constexpr (kDirect && S == 3) load_all(2, kStage2, 0, NT < kLoads ? NT : kLoads);
@@ -499,31 +497,29 @@ __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles t
 #pragma unroll
         for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
         fa = fragment_a(a0, 0);
-        scale_a = scales_at(base)[a_scale];
-        scale_b = scales_at(base)[b_scale];
-        uint32_t g = base;
-        const uint32_t stop = base + whole;
-        for (; g + kUnroll <= stop; g += kUnroll) {
+        scale_a = scales_at(0)[a_scale];
+        scale_b = scales_at(0)[b_scale];
+        uint32_t g = 0;
+        for (; g + kUnroll <= whole; g += kUnroll) {
             multiply(g, kStage0);
             multiply(g + 1, kStage1);
             multiply(g + 2, kStage2);
             if constexpr (kUnroll > 3) multiply(g + 3, kStage3);
         }
-        if (g < stop) multiply(g, kStage0);
-        if (g + 1 < stop) multiply(g + 1, kStage1);
+        if (g < whole) multiply(g, kStage0);
+        if (g + 1 < whole) multiply(g + 1, kStage1);
         if constexpr (kUnroll > 3)
-            if (g + 2 < stop) multiply(g + 2, kStage2);
+            if (g + 2 < whole) multiply(g + 2, kStage2);
     }
-    if (base + whole < end) {  // a last group, with zeros beyond the columns
+    if (whole < count) {  // a last group, with zeros beyond the columns
         meet(kNone);
-        const uint32_t begin = (base + whole) * kFp8Group;
-        const int left = (int)(k - begin) - (int)chunk;
+        const int left = (int)(k - (base + whole) * kFp8Group) - (int)chunk;
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
             const uint8_t* const p = l < kLoadsA ? tile_a + from_a[l] : tile_b + from_b[l - kLoadsA];
-            keep(l, load_16(p + begin, left, k), kStage0);
+            keep(l, load_16(p + whole * kFp8Group, left, k), kStage0);
         }
-        scales[0][64 * part_s + lane][0] = tile_s[from_s + groups - 1];
+        scales[0][64 * part_s + lane][0] = tile_s[from_s + whole];
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NT; ++j) fb[j] = fragment_b(b0, j);
@@ -643,7 +639,7 @@ hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
     Tiles tiles;
     tiles.rows = (uint32_t)((x.m + TM - 1) / TM);
     tiles.count = tiles.rows * (uint32_t)((x.n + TN - 1) / TN);
-    tiles.groups = ((groups + splits - 1) / splits + scale_run(S) - 1) / scale_run(S) * scale_run(S);
+    tiles.groups = (groups + splits - 1) / splits;
     tiles.splits = (groups + tiles.groups - 1) / tiles.groups;
     tiles.sums = (float*)x.workspace;
     const uint32_t grid = (tiles.count * tiles.splits + 7) / 8 * 8;
@@ -726,8 +722,10 @@ Choice choose(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) 
         const uint64_t tiles = tiles_of(c, m, n);
         const uint32_t most = c.rows != 128 || tiles >= 4 * kUnits ? 1 : kMaxSplits;
         for (uint32_t p = 1; p <= most && (p == 1 || groups / p >= 4); ++p) {
-            const float cost = rounds_cost(c, tiles * p, (groups + p - 1) / p) + join_cost(m, n, p);
-            if (best.shape == kShapes || cost < best.cost) best = {(Shape)s, p, cost};
+            const uint64_t each = (groups + p - 1) / p;
+            const uint32_t parts = (uint32_t)((groups + each - 1) / each);
+            const float cost = rounds_cost(c, tiles * parts, each) + join_cost(m, n, parts);
+            if (best.shape == kShapes || cost < best.cost) best = {(Shape)s, parts, cost};
         }
     }
     return best;
