@@ -10,13 +10,14 @@
 // columns of one row of C, and all of them take the same a_scale.
 //
 // Two kinds of kernels share the work, by the rows of A:
-//   up to 16   bound by reading B: stream_kernel.  1 x 8192 x 8192 13.7 us (4.9
+//   up to 16   (small products: 32) bound by reading B: stream_kernel.  1 x 8192 x 8192 13.7 us (4.9
 //              TB/s), 8 x 28672 x 8192 47 us (5.0 TB/s, where a copy reaches 5.1).
 //   more       bound by the matrix unit and its power: tile_kernel.  2048 x 28672 x
 //              8192 415 us (2.3 PFLOP/s; a library's product of the same codes
 //              without group scales 392).  A loop of this mix alone, products and four
 //              additions each from registers, reaches 3.1 PFLOP/s on ordinary codes and
 //              4.1 on equal ones: the chip lowers its clock to 1.7 GHz under it.
+#include <cmath>
 #include <type_traits>
 
 #include "fp8_device.h"
@@ -112,56 +113,66 @@ __device__ __forceinline__ void store_four(T* p, int valid, float4x v) {
 // ---------------------------------------------------------------------------
 // few rows: B straight from memory
 
-// A workgroup makes NT fragments of 16 x 16 outputs; its waves take the groups of
+// A workgroup makes MT x NT fragments of 16 x 16 outputs; its waves take the groups of
 // columns in turn and join their sums through LDS.  Nothing is shared between
 // waves but A, which the caches hold, so B goes to registers with kAhead groups on
 // their way per wave.
 constexpr int kStreamWaves = 8;
 
-template <typename T, int NT, int kAhead>
+template <typename T, int MT, int NT, int kAhead>
 __global__ void __launch_bounds__(kStreamWaves * 64)
     stream_kernel(const uint8_t* __restrict__ a, uint64_t ld_a, const float* __restrict__ sa,
                   const uint8_t* __restrict__ b, uint64_t ld_b, const float* __restrict__ sb, uint32_t m, uint32_t n,
                   uint32_t k, T* __restrict__ c, uint64_t ld_c, uint32_t tiles_m, uint64_t first) {
-    __shared__ float4x part[kStreamWaves][NT][64];
+    __shared__ float4x part[kStreamWaves][MT * NT][64];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint64_t tile = first + blockIdx.x;
-    const uint32_t i0 = (uint32_t)(tile % tiles_m) * 16, j0 = (uint32_t)(tile / tiles_m) * 16 * NT;
+    const uint32_t i0 = (uint32_t)(tile % tiles_m) * 16 * MT, j0 = (uint32_t)(tile / tiles_m) * 16 * NT;
     const uint32_t groups = (k + kFp8Group - 1) / kFp8Group, whole = k / kFp8Group;
     const uint32_t at = lane / 16 * 16;
-    const uint32_t row_of_a = min(i0 + lane % 16, m - 1);
-    const uint8_t* const row_a = a + row_of_a * ld_a + at;
-    const float* const scale_a = sa + (uint64_t)row_of_a * groups;
-    const uint8_t* row_b[NT];
-    const float* scale_b[NT];
+    const uint8_t *row_a[MT], *row_b[NT];
+    const float *scale_a[MT], *scale_b[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const uint32_t row = min(i0 + 16 * i + lane % 16, m - 1);
+        row_a[i] = a + row * ld_a + at;
+        scale_a[i] = sa + (uint64_t)row * groups;
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         row_b[j] = b + min(j0 + 16 * j + lane % 16, n - 1) * ld_b + at;
         scale_b[j] = sb + (uint64_t)(min(j0 + 16 * j, n - 1) / kFp8Group) * groups;
     }
 
-    float4x sum[NT];
+    float4x sum[MT][NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) sum[j] = float4x{0, 0, 0, 0};
-    int8x fa[kAhead], fb[kAhead][NT];
-    float in_a[kAhead], in_b[kAhead][NT];
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sum[i][j] = float4x{0, 0, 0, 0};
+    int8x fa[kAhead][MT], fb[kAhead][NT];
+    float in_a[kAhead][MT], in_b[kAhead][NT];
     auto load = [&](int slot, uint32_t g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             fb[slot][j] = load_whole(row_b[j] + g * kFp8Group);
             in_b[slot][j] = scale_b[j][g];
         }
-        fa[slot] = load_whole(row_a + g * kFp8Group);
-        in_a[slot] = scale_a[g];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            fa[slot][i] = load_whole(row_a[i] + g * kFp8Group);
+            in_a[slot][i] = scale_a[i][g];
+        }
     };
     auto multiply = [&](int slot) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const float4x p = group_product<T>(fb[slot][j], fa[slot]);
-            const float s = in_a[slot] * in_b[slot][j];
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[j][e] = fmaf(p[e], s, sum[j][e]);
-        }
+            for (int j = 0; j < NT; ++j) {
+                const float4x p = group_product<T>(fb[slot][j], fa[slot][i]);
+                const float s = in_a[slot][i] * in_b[slot][j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[e], s, sum[i][j][e]);
+            }
     };
     // The wave's groups are wave, wave + kStreamWaves, ...; count of the whole ones among them.
     const uint32_t count = whole > wave ? (whole - wave + kStreamWaves - 1) / kStreamWaves : 0;
@@ -187,17 +198,22 @@ __global__ void __launch_bounds__(kStreamWaves * 64)
             fb[0][j] = load_fragment(row_b[j] + whole * kFp8Group, left, k);
             in_b[0][j] = scale_b[j][whole];
         }
-        fa[0] = load_fragment(row_a + whole * kFp8Group, left, k);
-        in_a[0] = scale_a[whole];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            fa[0][i] = load_fragment(row_a[i] + whole * kFp8Group, left, k);
+            in_a[0][i] = scale_a[i][whole];
+        }
         multiply(0);
     }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) part[wave][j][lane] = sum[j];
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[wave][i * NT + j][lane] = sum[i][j];
     __syncthreads();
-    for (uint32_t j = wave; j < NT; j += kStreamWaves) {
-        float4x total = part[0][j][lane];
-        for (int w = 1; w < kStreamWaves; ++w) total += part[w][j][lane];
-        const uint32_t row = i0 + lane % 16, col = j0 + j * 16 + lane / 16 * 4;
+    for (uint32_t f = wave; f < MT * NT; f += kStreamWaves) {
+        float4x total = part[0][f][lane];
+        for (int w = 1; w < kStreamWaves; ++w) total += part[w][f][lane];
+        const uint32_t row = i0 + f / NT * 16 + lane % 16, col = j0 + f % NT * 16 + lane / 16 * 4;
         if (row < m && col < n) store_four(c + row * ld_c + col, (int)(n - col), total);
     }
 }
@@ -648,14 +664,14 @@ hipError_t launch_tiles(const MatmulArgs& x, uint32_t splits, hipStream_t s) {
     return e != hipSuccess || tiles.splits == 1 ? e : launch_join<T>(tiles.sums, tiles.splits, x, s);
 }
 
-template <typename T, int NT, int kAhead>
+template <typename T, int MT, int NT, int kAhead>
 hipError_t launch_stream(const MatmulArgs& x, hipStream_t s) {
-    const uint32_t tiles_m = (uint32_t)((x.m + 15) / 16);
+    const uint32_t tiles_m = (uint32_t)((x.m + 16 * MT - 1) / (16 * MT));
     const uint64_t tiles = tiles_m * ((x.n + 16 * NT - 1) / (16 * NT));
     constexpr uint64_t kMost = 1u << 22;  // workgroups of a launch: 2^31 lanes
     for (uint64_t first = 0; first < tiles; first += kMost) {
         const uint64_t count = tiles - first < kMost ? tiles - first : kMost;
-        stream_kernel<T, NT, kAhead><<<(uint32_t)count, kStreamWaves * 64, 0, s>>>(
+        stream_kernel<T, MT, NT, kAhead><<<(uint32_t)count, kStreamWaves * 64, 0, s>>>(
             x.a, x.ld_a, x.a_scales, x.b, x.ld_b, x.b_scales, (uint32_t)x.m, (uint32_t)x.n, (uint32_t)x.k, (T*)x.c,
             x.ld_c, tiles_m, first);
         const hipError_t e = hipGetLastError();
@@ -753,22 +769,36 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
     return plan;
 }
 
-// A workgroup's fragments of B share one of A, whose rows take as many loads as
-// theirs, and a unit with one workgroup more than others is the last to end: the
-// fewest loads of a unit that has the most (8 x 28672 x 8192: 57 us by single
-// fragments, 56 by 2, 50 by 4, 47 by 7; 16 x 8192 x 28672 71, 56, 78 and 112).  Up to four
-// rows of A take next to nothing (1 x 28672 x 8192: 42, 56, 48, 48).
-int stream_kind(uint64_t m, uint64_t n) {
+// Up to 16 rows of A (or 32, as two fragments) straight from memory.  A workgroup's
+// fragments of B share those of A, whose rows take as many loads as theirs, and a unit
+// with one workgroup more than others is the last to end: the fewest loads of a unit
+// that has the most (8 x 28672 x 8192: 57 us by single fragments, 56 by 2, 50 by 4, 47 by
+// 7; 16 x 8192 x 28672 71, 56, 78 and 112).  Up to four rows of A take next to nothing (1 x
+// 28672 x 8192: 42, 56, 48, 48).  Two fragments of A only where one workgroup on each unit is
+// enough (17 x 28672 x 8192 58 us, 49 by tiles).
+//
+// The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory. Rows
+// that are not 16-byte aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x
+// 1025 x 1023 5.9 and 14.1; aligned 17 x 4096 x 4096 7.4 and 11.1, 32 x 8192 x 8192 21.3 and 16.9).
+struct Stream {
+    int kind;
+    float cost;
+};
+Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t groups) {
     constexpr int kFragments[] = {1, 2, 4, 7};
+    const bool two = m > 16 && m <= 32;
     const uint64_t fragments = (n + 15) / 16;
-    int best = 0;
+    Stream best = {kMatmulStream1, INFINITY};
     uint64_t least = 0;
-    for (int i = 0; i < (m <= 4 ? 1 : 4); ++i) {
+    for (int i = 0; i < (m <= 4 ? 1 : two ? 3 : 4); ++i) {
         const uint64_t each = kFragments[i], workgroups = (fragments + each - 1) / each;
-        const uint64_t loads = (workgroups + kUnits - 1) / kUnits * (16 * each + m);
-        if (i == 0 || loads < least) best = i, least = loads;
+        const uint64_t rounds = (workgroups + kUnits - 1) / kUnits, loads = rounds * (16 * each + m);
+        if ((two && rounds > 1) || (least > 0 && loads >= least)) continue;
+        least = loads;
+        best = {(two ? kMatmulStreamTwo1 : kMatmulStream1) + i,
+                3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f), (float)n * (float)k / 3.9e6f)};
     }
-    return kMatmulStream1 + best;
+    return best;
 }
 
 // Copying rows to aligned ones, in us: two launches (a small product waits for the
@@ -777,27 +807,39 @@ float pack_cost(uint64_t m, uint64_t n, uint64_t k) { return 12.0f + (float)(m +
 
 }  // namespace
 
-// Tiles serve more than 16 rows: a workgroup then reads B's rows for 128 of A's at
-// once (32 x 8192 x 8192 17 us, 28 by fragments of 16 rows).
+// Tiles serve more rows: a workgroup then reads B's rows for 128 of A's at once (64 x
+// 4096 x 4096 14.6 us, 15.2 by four fragments of 16 rows; 64 x 8192 x 8192 18.5 and 31).
 int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k,
                      MatmulPart parts[kMatmulMostParts]) {
     const uint64_t groups = (k + kFp8Group - 1) / kFp8Group;
-    if (groups == 0 || m <= 16 || !tiles) {
-        parts[0] = {groups == 0 ? kMatmulZeros : stream_kind(m, n), 1, m, n};
+    if (groups == 0) {
+        parts[0] = {kMatmulZeros, 1, m, n};
+        return 1;
+    }
+    const Stream stream = stream_of(aligned, m, n, k, groups);
+    if (!tiles || (aligned && m <= 16)) {
+        parts[0] = {stream.kind, 1, m, n};
         return 1;
     }
     int count = 0;
     Plan plan = plan_of(wide, true, m, n, groups);
+    float cost = plan.main.cost + (plan.rows < m || plan.cols < n ? plan.rest.cost : 0.0f);
     if (!aligned) {
         // Rows at any address go through registers to LDS in tiles of 128 x 128 alone;
         // where there is much to multiply a copy of them is paid for by the larger tiles
         // (866 x 16640 x 9809: 384 us, 250 with the copy).
-        const float cost = plan.main.cost + (plan.rows < m || plan.cols < n ? plan.rest.cost : 0.0f);
         const Plan direct = plan_of(wide, false, m, n, groups);
-        if (cost + pack_cost(m, n, k) < direct.main.cost)
+        if (cost + pack_cost(m, n, k) < direct.main.cost) {
+            cost += pack_cost(m, n, k);
             parts[count++] = {kMatmulPack, 1, m, n};
-        else
+        } else {
+            cost = direct.main.cost;
             plan = direct;
+        }
+    }
+    if (m <= 32 && stream.cost < cost) {
+        parts[0] = {stream.kind, 1, m, n};
+        return 1;
     }
     parts[count++] = {kMatmul256x256 + plan.main.shape, plan.main.splits, plan.rows, plan.cols};
     if (plan.rows < m || plan.cols < n)
@@ -812,10 +854,13 @@ template <typename T>
 hipError_t launch_part(const MatmulPart& p, const MatmulArgs& x, hipStream_t s) {
     switch (p.kind) {
         case kMatmulZeros: return launch_join<T>(nullptr, 0, x, s);
-        case kMatmulStream1: return launch_stream<T, 1, 2>(x, s);
-        case kMatmulStream2: return launch_stream<T, 2, 2>(x, s);
-        case kMatmulStream4: return launch_stream<T, 4, 1>(x, s);
-        case kMatmulStream7: return launch_stream<T, 7, 1>(x, s);
+        case kMatmulStream1: return launch_stream<T, 1, 1, 2>(x, s);
+        case kMatmulStream2: return launch_stream<T, 1, 2, 2>(x, s);
+        case kMatmulStream4: return launch_stream<T, 1, 4, 1>(x, s);
+        case kMatmulStream7: return launch_stream<T, 1, 7, 1>(x, s);
+        case kMatmulStreamTwo1: return launch_stream<T, 2, 1, 1>(x, s);
+        case kMatmulStreamTwo2: return launch_stream<T, 2, 2, 1>(x, s);
+        case kMatmulStreamTwo4: return launch_stream<T, 2, 4, 1>(x, s);
         case kMatmul256x256:
             if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 2, true>(x, p.splits, s);
             return hipErrorInvalidValue;  // not among a 32-bit result's shapes

@@ -267,6 +267,9 @@ enum : int {
     kMatmul128x128 = 8,
     kMatmulUnaligned = 9,  // 128 x 128, rows at any address
     kMatmulPack = 10,      // before the others: rows copied to aligned ones
+    kMatmulStreamTwo1 = 11,  // 32 rows, B straight from memory; 1, 2 or 4 fragments a workgroup
+    kMatmulStreamTwo2 = 12,
+    kMatmulStreamTwo4 = 13,
 };
 constexpr int kMatmulMostParts = 3;
 struct MatmulPart {

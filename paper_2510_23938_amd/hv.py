@@ -659,7 +659,7 @@ def merkle_launches(seg_offsets, alg: str = "sha256", cus: int = 0) -> list:
 
 
 _MATMUL_KINDS = ("zeros", "stream16", "stream32", "stream64", "stream112", "256x256", "256x128", "192x128", "128x128",
-                 "128x128 unaligned", "pack")
+                 "128x128 unaligned", "pack", "stream 2x16", "stream 2x32", "stream 2x64")
 
 
 def matmul_launches(m: int, n: int, k: int, dtype=torch.bfloat16, aligned: bool = True) -> list:

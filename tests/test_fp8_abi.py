@@ -77,13 +77,13 @@ def test_which_kernels_a_product_takes():
     taken = {}
     for dtype in (bf16, f32):
         for aligned in (True, False):
-            for m in (1, 4, 8, 16, 17, 64, 150, 256, 333, 1000, 2048, 4096):
+            for m in (1, 4, 8, 16, 17, 32, 33, 64, 150, 256, 333, 1000, 2048, 4096):
                 for n in (64, 1024, 4096, 5001, 11008, 16384, 28672):
                     for k in (0, 100, 1024, 4093, 28672):
                         parts = hv.matmul_launches(m, n, k, dtype, aligned)
                         packed = parts[0][0] == "pack"
                         if packed:
-                            assert not aligned and m > 16 and parts[0][1:] == (m, n, 1)
+                            assert not aligned and parts[0][1:] == (m, n, 1)
                             taken["pack"] = {False}
                             parts = parts[1:]
                         assert sum(r * c for _, r, c, _ in parts) == m * n
@@ -94,7 +94,10 @@ def test_which_kernels_a_product_takes():
                         for kind, _, _, splits in parts:
                             taken.setdefault(kind, set()).add(splits > 1)
                             assert splits == 1 or kind.startswith("128x128")
-                            assert (kind == "128x128 unaligned") == (not aligned and not packed and m > 16 and k > 0)
+                            stream = kind.startswith("stream")
+                            assert stream if m <= 16 and k > 0 and aligned else not stream or m <= 32
+                            assert kind.startswith("stream 2") == (stream and m > 16)
+                            assert (kind == "128x128 unaligned") == (not aligned and not packed and not stream and k > 0)
     assert set(taken) == set(hv._MATMUL_KINDS)
     assert taken["128x128"] == taken["128x128 unaligned"] == {True, False}
     assert [p[0] for p in hv.matmul_launches(2048, 28672, 8192)] == ["256x256", "256x128"]

@@ -300,6 +300,15 @@ def test_matmul_strides_and_offsets(m, n, k):
         product(m, n, k, "bf16", pad, offset, out_pad)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad", [0, 16, 5])
+@pytest.mark.parametrize("m,n,k", [(17, 4096, 1100), (32, 40, 128), (25, 5001, 777), (32, 8192, 400), (19, 9000, 300),
+                                   (31, 16384, 129)])
+def test_matmul_two_fragments_of_rows(m, n, k, pad, dtype):
+    assert hv.matmul_launches(m, n, k, TYPES[dtype], (k + pad) % 16 == 0)[0][0].startswith("stream 2")
+    product(m, n, k, dtype, pad)
+
+
 @pytest.mark.parametrize("m,n,k", [(2048, 8448, 256), (8448, 2048, 384), (2300, 8200, 130)])
 def test_matmul_larger_than_the_chip(m, n, k):
     """A round of the largest tiles, then the rest by smaller ones: the last columns, the last rows, odd edges."""
