@@ -309,6 +309,15 @@ def test_matmul_two_fragments_of_rows(m, n, k, pad, dtype):
     product(m, n, k, dtype, pad)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 1000, 20479), (4, 515, 9001), (16, 130, 20003)])
+def test_matmul_few_rows_at_odd_addresses(m, n, k, dtype):
+    """Long rows that are not aligned go through tiles, a single one too."""
+    assert hv.matmul_launches(m, n, k, TYPES[dtype], False)[0][0] == "128x128 unaligned"
+    product(m, n, k, dtype)
+    product(m, n, k, dtype, pad=2, offset=3, out_pad=1)
+
+
 @pytest.mark.parametrize("m,n,k", [(2048, 8448, 256), (8448, 2048, 384), (2300, 8200, 130)])
 def test_matmul_larger_than_the_chip(m, n, k):
     """A round of the largest tiles, then the rest by smaller ones: the last columns, the last rows, odd edges."""
