@@ -79,7 +79,8 @@ hv_status hv_fp8_rms_norm(hv_type type, const void* x, uint64_t ld_x, const void
                           uint64_t ld_residual_out, uint8_t* codes, uint64_t ld_codes, float* scales,
                           hipStream_t stream);
 
-/* silu(gate) * up, quantised by rows: y = gate / (1 + exp(-gate)) * up in 32 bits.
+/* silu(gate) * up, quantised by rows: y = gate / (1 + exp(-gate)) * up in 32 bits,
+ * and gate * exp(gate) * up for gates below -87, where exp(-gate) leaves them.
  *   gate, up: [rows][cols] of the type; they may be the two halves of one
  *             matrix's rows.
  *   codes: [rows][cols]; scales: [rows][ceil(cols / 128)]. */

@@ -40,12 +40,36 @@ struct GatedOf {  // gate / (1 + exp(-gate)) * up
     uint64_t ld_gate, ld_up;
     __device__ __forceinline__ void get(uint64_t row, uint32_t col, uint32_t valid, float (&y)[8]) const {
         float u[8];
-        load_eight(gate + row * ld_gate + col, valid, y);
-        load_eight(up + row * ld_up + col, valid, u);
-        // the reciprocal instruction is within one unit in the last place; a division takes ten
-        // instructions more (2048 x 28672: 67 us instead of 54)
+        const T *const g = gate + row * ld_gate + col, *const f = up + row * ld_up + col;
+        if (valid >= 8) {  // one branch: both are asked for before either is waited for
+            load_eight(g, 8, y);
+            load_eight(f, 8, u);
+        } else {
+            load_eight(g, valid, y);
+            load_eight(f, valid, u);
+        }
+        // Where exp(-gate) comes near 2^128 its reciprocal is subnormal, which the reciprocal
+        // instruction does not give, and from there on 1 + exp(-gate) is exp(-gate) in 32 bits: y is then
+        // gate * up * exp(gate), by halves of the exponent, so that large factors up keep it in range.  A
+        // branch that few vectors take: one comparison of eight gates' least.
+        float low = y[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = y[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-y[i])) * u[i];
+        for (int i = 1; i < 8; ++i) low = fminf(low, y[i]);
+        if (low < -87.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float half = expf(0.5f * y[i]);
+                y[i] = y[i] < -87.0f ? (y[i] * half) * (u[i] * half) : ordinary(y[i], u[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = ordinary(y[i], u[i]);
+        }
+    }
+    // For gates from -87 on: the reciprocal instruction is within one unit in the last place of a normal
+    // result; a division takes ten instructions more (2048 x 28672: 67 us instead of 54).
+    static __device__ __forceinline__ float ordinary(float gate, float up) {
+        return gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up;
     }
 };
 
