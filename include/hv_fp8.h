@@ -27,11 +27,12 @@
  *
  * Every call is asynchronous on `stream`: it queues kernels only (no upload, no
  * host wait, no allocation, no memset), so it may be captured in a HIP graph.
- * All pointers are device pointers.  Leading dimensions (ld_*) count elements
- * between the starts of consecutive rows and are at least the columns of a row.
- * Rows need no alignment beyond that of their element type; 16-byte aligned
- * ones are read faster.  Inputs and outputs must not overlap, but for the case
- * that hv_fp8_rms_norm names.  A call with no elements to write does nothing.
+ * All pointers are device pointers of the device that is current.  Leading
+ * dimensions (ld_*) count elements between the starts of consecutive rows and are
+ * at least the columns of a row.  Rows need no alignment beyond that of their
+ * element type; 16-byte aligned ones are read faster.  Inputs and outputs must not
+ * overlap, but for the case that hv_fp8_rms_norm names.  A call with no elements to
+ * write does nothing.
  * Results do not depend on the stream or on what runs beside, and are equal bit
  * for bit from call to call.
  *

@@ -1170,6 +1170,7 @@ def _groups(n: int) -> int:
 _CODES = (torch.float8_e4m3fn,)
 _SCALES = (torch.float32,)
 _current_stream = torch._C._cuda_getCurrentRawStream  # of a device index; 0.1 us, a Stream object takes 2
+_current_device = torch._C._cuda_getDevice
 
 
 def _scales(t, what: str, device, shape) -> int:
@@ -1206,6 +1207,9 @@ def hv_fp8_quantize(x: torch.Tensor, tile: str = "rows", out=None, scales=None):
     if tile not in ("rows", "blocks"):
         raise ValueError(f"unknown tile {tile!r}; expected 'rows' or 'blocks'")
     dev = _device_of(x, "x")
+    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_quantize(x, tile, out, scales)
     ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
     if tile == "blocks":
         if x.dim() != 2:
@@ -1225,6 +1229,9 @@ def hv_fp8_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual=
     ``weight``, quantised by rows.  h comes back in x's type, for the next layer (``residual_out``
     may be ``x`` or ``residual``, for the addition in place); without a residual it is None."""
     dev = _device_of(x, "x")
+    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_rms_norm(x, weight, eps, residual, out, scales, residual_out)
     ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
     same = (x.dtype,)
     weight_ptr = _matrix(weight, same, "weight", dev, (cols,))[0]
@@ -1248,6 +1255,9 @@ def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
     """(codes, scales) of silu(gate) * up, quantised by rows.  ``gate`` and ``up`` may be the halves
     of one product's columns."""
     dev = _device_of(gate, "gate")
+    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_gated(gate, up, out, scales)
     ptr, ld, rows, cols = _matrix(gate, TYPES, "gate", dev)
     up_ptr, ld_up, _, _ = _matrix(up, (gate.dtype,), "up", dev, gate.shape)
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(gate, (*gate.shape[:-1], _groups(cols)), dev, out, scales)
@@ -1263,6 +1273,9 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
     if dtype not in TYPES:
         raise ValueError(f"dtype is {dtype}; expected one of {[str(d) for d in TYPES]}")
     dev = _device_of(a, "a")
+    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_matmul(a, a_scales, b, b_scales, dtype, out, workspace)
     a_ptr, ld_a, _, k = _matrix(a, _CODES, "a", dev)
     b_ptr, ld_b, _, _ = _matrix(b, _CODES, "b", dev)
     if b.dim() != 2 or b.shape[1] != k:

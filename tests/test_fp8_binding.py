@@ -1,0 +1,70 @@
+"""What the binding of the 8-bit operators does around the library's calls.  None of it needs a GPU: tensors in host
+memory say that they are on one, and a recorder stands in for the library."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
+
+OPERATORS = ("quantize", "rms_norm", "gated", "matmul")
+
+
+class OnGpu1(torch.Tensor):
+    """A tensor in host memory that says it is on the second GPU."""
+    device = property(lambda self: torch.device("cuda", 1))
+    is_cuda = True
+
+
+def tensor(*shape, dtype=torch.bfloat16, fill=1.0):
+    return torch.full(shape, fill, dtype=torch.float32).to(dtype).as_subclass(OnGpu1)
+
+
+def arguments():
+    """{operator: (function, arguments)}: small calls with every output given."""
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    x, w, s = tensor(4, 256), tensor(256), tensor(4, 2, dtype=f32)
+    q, b, sb = tensor(4, 256, dtype=e4m3), tensor(128, 256, dtype=e4m3), tensor(1, 2, dtype=f32)
+    return {"quantize": (hv.hv_fp8_quantize, dict(x=x, out=q, scales=s)),
+            "rms_norm": (hv.hv_fp8_rms_norm, dict(x=x, weight=w, eps=1e-6, residual=tensor(4, 256), out=q, scales=s,
+                                                  residual_out=tensor(4, 256))),
+            "gated": (hv.hv_fp8_gated, dict(gate=x, up=tensor(4, 256), out=q, scales=s)),
+            "matmul": (hv.hv_fp8_matmul, dict(a=q, a_scales=s, b=b, b_scales=sb, out=tensor(4, 128)))}
+
+
+class Library:
+    """Stands in for libhv.so: notes each operator's call, the device that is current then and its stream."""
+
+    def __init__(self, monkeypatch, current=0):
+        self.calls, self.current = [], current
+        monkeypatch.setattr(hv, "lib", self)
+        monkeypatch.setattr(hv, "_current_device", lambda: self.current, raising=False)
+        monkeypatch.setattr(hv, "_current_stream", lambda index: 1000 + index)
+        monkeypatch.setattr(torch.cuda, "device", self._device)
+
+    @contextlib.contextmanager
+    def _device(self, device):
+        before, self.current = self.current, torch.device(device).index
+        yield
+        self.current = before
+
+    def hv_fp8_matmul_workspace_bytes(self, *args):
+        return 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, self.current, args[-1]))
+            return hv.HV_OK
+        return call
+
+
+@pytest.mark.parametrize("operator", OPERATORS)
+@pytest.mark.parametrize("current", [0, 1])
+def test_the_tensors_gpu_is_current_for_the_call(monkeypatch, operator, current):
+    """A stream's handle of zero means the current device's default stream, so a call on another device's tensors
+    would run there, out of order with their own stream."""
+    library = Library(monkeypatch, current)
+    call, args = arguments()[operator]
+    call(**args)
+    assert library.calls == [("hv_fp8_" + operator, 1, 1001)]
+    assert library.current == current
