@@ -202,6 +202,11 @@ def _alg(alg: str) -> tuple:
         raise ValueError(f"unknown hash {alg!r}; expected one of {sorted(ALGS)}") from None
 
 
+_current_stream = torch._C._cuda_getCurrentRawStream  # of a device index; 0.1 us, a Stream object takes 2
+_current_device = torch._C._cuda_getDevice
+_capturing = torch._C._cuda_isCurrentStreamCapturing
+
+
 def _stream(device=None) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
@@ -230,17 +235,30 @@ def _buffer(t, nbytes: int, what: str, device) -> int:
 
 
 class Workspace:
-    """A growable device byte buffer handed to the library as scratch."""
+    """Growable device buffers handed to the library as scratch, one for each stream that calls run on.
+
+    Calls on different streams may run at once, and a HIP graph's replays write to the scratch that its
+    capture was given: captures have buffers apart from those of eager calls, and one that a larger request
+    outgrows stays allocated as long as this object.  Graphs captured on one stream with one Workspace
+    share scratch, so their replays must not overlap."""
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)
-        self.buf = None
+        self.bufs = {}      # (device, stream, whether it is being captured) -> buffer
+        self.captured = []  # every buffer that a capture was given
 
     def get(self, nbytes: int) -> torch.Tensor:
         nbytes = max(int(nbytes), 256)
-        if self.buf is None or self.buf.numel() < nbytes:
-            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        return self.buf
+        if not self.bufs and self.device.type == "cuda":
+            torch.cuda.init()
+        index = self.device.index if self.device.index is not None else _current_device()
+        key = (index, _current_stream(index), _capturing())
+        buf = self.bufs.get(key)
+        if buf is None or buf.numel() < nbytes:
+            buf = self.bufs[key] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            if key[2]:
+                self.captured.append(buf)
+        return buf
 
 
 class HostBuffer:
@@ -1169,8 +1187,6 @@ def _groups(n: int) -> int:
 
 _CODES = (torch.float8_e4m3fn,)
 _SCALES = (torch.float32,)
-_current_stream = torch._C._cuda_getCurrentRawStream  # of a device index; 0.1 us, a Stream object takes 2
-_current_device = torch._C._cuda_getDevice
 
 
 def _scales(t, what: str, device, shape) -> int:
@@ -1269,7 +1285,8 @@ def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
 def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
                   dtype=torch.bfloat16, out=None, workspace: Workspace | None = None):
     """a [..., k] times the transpose of b [n, k], both in codes, in ``dtype``: ``a_scales`` by rows
-    ([..., ceil(k / 128)]), ``b_scales`` by blocks ([ceil(n / 128), ceil(k / 128)])."""
+    ([..., ceil(k / 128)]), ``b_scales`` by blocks ([ceil(n / 128), ceil(k / 128)]).  A ``workspace`` given
+    has to outlive the HIP graphs that are captured with it."""
     if dtype not in TYPES:
         raise ValueError(f"dtype is {dtype}; expected one of {[str(d) for d in TYPES]}")
     dev = _device_of(a, "a")
@@ -1292,6 +1309,8 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
         out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", dev, (*lead, n))
     aligned = not (ld_a % 16 or ld_b % 16 or a_ptr % 16 or b_ptr % 16)
     need = lib.hv_fp8_matmul_workspace_bytes(TYPES[dtype], aligned, m, n, k)
+    if workspace is not None and (workspace.device.type != "cuda" or workspace.device.index not in (None, dev.index)):
+        raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {dev}")
     ws = (workspace or Workspace(dev)).get(need) if need else None
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
                              ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(dev.index)))

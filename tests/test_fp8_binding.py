@@ -1,6 +1,8 @@
 """What the binding of the 8-bit operators does around the library's calls.  None of it needs a GPU: tensors in host
 memory say that they are on one, and a recorder stands in for the library."""
 import contextlib
+import gc
+import weakref
 
 import pytest
 import torch
@@ -68,3 +70,57 @@ def test_the_tensors_gpu_is_current_for_the_call(monkeypatch, operator, current)
     call(**args)
     assert library.calls == [("hv_fp8_" + operator, 1, 1001)]
     assert library.current == current
+
+
+# --------------------------------------------------------------------------
+# scratch
+
+@pytest.fixture
+def streams(monkeypatch):
+    """The current stream's handle and whether it is being captured, to be set by the test."""
+    now = {"stream": 7, "capturing": False}
+    monkeypatch.setattr(hv, "_current_device", lambda: 0)
+    monkeypatch.setattr(hv, "_current_stream", lambda index: now["stream"])
+    monkeypatch.setattr(hv, "_capturing", lambda: now["capturing"], raising=False)
+    return now
+
+
+def test_each_stream_has_scratch_of_its_own(streams):
+    ws = hv.Workspace("cpu")
+    first = ws.get(1000)
+    assert first.numel() >= 1000 and ws.get(500) is first
+    streams["stream"] = 8  # its calls may run beside those of the first
+    second = ws.get(1000)
+    assert second.data_ptr() != first.data_ptr()
+    streams["stream"] = 7
+    assert ws.get(1000) is first
+    assert ws.get(5000).numel() >= 5000 and ws.get(1000).numel() >= 5000
+
+
+def test_scratch_that_a_capture_was_given_stays(streams):
+    """A graph's replays write there for as long as the graph lives, whatever is called in between."""
+    ws = hv.Workspace("cpu")
+    eager = ws.get(1000)
+    streams["capturing"] = True
+    buffers = [ws.get(1000), ws.get(3000)]
+    kept = [weakref.ref(b) for b in buffers]
+    addresses = [b.data_ptr() for b in buffers]
+    del buffers
+    streams["capturing"] = False
+    assert ws.get(1000) is eager and eager.data_ptr() not in addresses  # eager calls may run beside a replay
+    ws.get(1 << 20)
+    streams["capturing"] = True
+    ws.get(1 << 21)
+    gc.collect()
+    assert all(k() is not None for k in kept)
+
+
+@pytest.mark.parametrize("device", ["cpu", "cuda:0"])
+def test_scratch_elsewhere_is_refused(monkeypatch, device):
+    library = Library(monkeypatch, 1)
+    library.hv_fp8_matmul_workspace_bytes = lambda *args: 4096
+    monkeypatch.setattr(hv.Workspace, "get", lambda self, nbytes: torch.empty(nbytes, dtype=torch.uint8))
+    call, args = arguments()["matmul"]
+    with pytest.raises(ValueError, match="workspace"):
+        call(**args, workspace=hv.Workspace(device))
+    assert library.calls == []

@@ -32,3 +32,49 @@ def test_gated_by_a_closing_gate(dtype):
     assert (want > 2.0 ** -126).all()
     assert np.all(np.abs(got / want - 1) <= base.Y_ERROR)
     base.check_codes(base.bytes_of(codes), y, got, 1, 2 * base.Y_ERROR)
+
+
+def test_matmul_scratch_of_a_graph_survives_larger_calls():
+    """A product whose columns are split, captured; a larger one on the same workspace outgrows the scratch; what is
+    allocated then is not written by the graph's replays, and their results stay right."""
+    rng = np.random.default_rng(23)
+    small, large = base.operands(rng, 40, 300, 9000)[1], base.operands(rng, 100, 600, 20000)[1]
+    need = hv.lib.hv_fp8_matmul_workspace_bytes(hv.HV_BF16, 0, 40, 300, 9000)
+    more = hv.lib.hv_fp8_matmul_workspace_bytes(hv.HV_BF16, 1, 100, 600, 20000)  # 20000 is a multiple of 16
+    assert 0 < need < more
+    ws = hv.Workspace(DEV)
+    side = torch.cuda.Stream(DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = hv.hv_fp8_matmul(*small, workspace=ws).clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = hv.hv_fp8_matmul(*small, workspace=ws)
+        wanted_large = hv.hv_fp8_matmul(*large)
+        canaries = []
+        for _ in range(3):
+            assert torch.equal(hv.hv_fp8_matmul(*large, workspace=ws), wanted_large)
+            canaries += [torch.full((need,), 0x55, dtype=torch.uint8, device=DEV) for _ in range(8)]
+            got.zero_()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(got, want)
+            assert all(bool((c == 0x55).all()) for c in canaries)
+
+
+def test_matmul_on_two_streams_with_one_workspace():
+    """Each stream's calls have scratch of their own: products that run at once do not mix their parts' sums."""
+    rng = np.random.default_rng(24)
+    operands = [base.operands(rng, 40, 300, 9000)[1] for _ in range(2)]
+    want = [hv.hv_fp8_matmul(*o) for o in operands]
+    ws = hv.Workspace(DEV)
+    streams = [torch.cuda.Stream(DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(hv.hv_fp8_matmul(*operands[i], workspace=ws))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
