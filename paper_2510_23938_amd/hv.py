@@ -1146,7 +1146,9 @@ def verify(named_tensors, expected: bytes, chunk_bytes: int, alg: str = "sha256"
 # 8-bit operators (include/hv_fp8.h): codes are torch.float8_e4m3fn tensors
 # [..., cols], scales contiguous float32, one for every 128 columns of a row
 # ([..., ceil(cols / 128)]) or for every block of 128 x 128
-# ([ceil(rows / 128), ceil(cols / 128)]).
+# ([ceil(rows / 128), ceil(cols / 128)]).  There is no backward pass: what is
+# verified is a constant, and codes have no gradient.  A call that autograd
+# would record is refused.
 
 def _device_of(t, what: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -1162,6 +1164,9 @@ def _matrix(t, dtypes, what: str, device, shape=None) -> tuple:
         raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on {device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, and the 8-bit operators have no backward pass: call them "
+                         "under torch.no_grad(), or on detached tensors")
     s = t.shape
     if shape is not None and s != shape:
         raise ValueError(f"{what} has shape {tuple(s)}; the call needs {tuple(shape)}")

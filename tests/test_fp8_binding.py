@@ -124,3 +124,24 @@ def test_scratch_elsewhere_is_refused(monkeypatch, device):
     with pytest.raises(ValueError, match="workspace"):
         call(**args, workspace=hv.Workspace(device))
     assert library.calls == []
+
+
+# --------------------------------------------------------------------------
+# gradients
+
+@pytest.mark.parametrize("operator", OPERATORS)
+def test_gradients_are_refused_where_they_would_be_lost(monkeypatch, operator):
+    """No backward pass: a call that autograd records is refused, and runs where nothing is recorded."""
+    library = Library(monkeypatch, 1)
+    call, args = arguments()[operator]
+    wide = [k for k, v in args.items() if isinstance(v, torch.Tensor) and v.dtype in (torch.bfloat16, torch.float32)]
+    for name in wide:
+        args = arguments()[operator][1]
+        args[name].requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            call(**args)
+        assert library.calls == []
+        with torch.no_grad():
+            call(**args)
+        assert len(library.calls) == 1
+        library.calls.clear()
