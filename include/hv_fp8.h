@@ -107,8 +107,8 @@ size_t hv_fp8_matmul_workspace_bytes(hv_type type, int aligned, uint64_t m, uint
  * 32 bits.
  *   c: [m][n] of the type, with leading dimension ld_c.
  *   workspace: >= hv_fp8_matmul_workspace_bytes(...), 256-byte aligned; NULL where
- *              that is 0.  Scratch: calls that share one must share a
- *              stream.
+ *              that is 0, or where ld_a or ld_b is 2^23 or more.  Scratch: calls that
+ *              share one must share a stream.
  * Errors: HV_ERR_INVALID_ARG also for m or n above 2^27; HV_ERR_WORKSPACE for a
  * missing, short or misaligned workspace. */
 hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const float* a_scales, const uint8_t* b,

@@ -92,7 +92,7 @@ hv_status hv_set_handover_polls(uint32_t polls);
 hv_status hv_merkle_launches(hv_alg alg, const uint64_t* seg_offsets, uint32_t n_seg, uint32_t cus, int* launches,
                              int* kind, uint64_t* units, uint64_t* one_lane);
 
-/* The launches hv_fp8_matmul makes for these sizes and rows that are 16-byte
+/* The launches hv_fp8_matmul makes for these sizes and rows (less than 2^23 bytes apart) that are 16-byte
  * aligned or not, for tests and measurements: *launches (at most 3; 0 for an empty c), and per launch
  * kind[i] = 0 (no columns: zeros), 1 to 4 (up to 16 rows of A against 16, 32, 64 or
  * 112 rows of B, straight from memory), 5 to 8 (tiles of 256 x 256, 256 x 128, 192 x

@@ -914,7 +914,7 @@ bool rows_aligned(const MatmulArgs& x) {
 
 template <typename T>
 hipError_t launch(MatmulArgs x, hipStream_t s) {
-    const bool tiles = x.ld_a <= kMaxTileLd && x.ld_b <= kMaxTileLd;
+    const bool tiles = fp8_matmul_tiles(x.ld_a, x.ld_b);
     MatmulPart parts[kMatmulMostParts];
     const int count = fp8_matmul_parts(sizeof(T) == 4, rows_aligned(x), tiles, x.m, x.n, x.k, parts);
     const Scratch scratch = scratch_of(parts, count, x.m, x.n, x.k);
@@ -949,6 +949,8 @@ hipError_t launch(MatmulArgs x, hipStream_t s) {
 }
 
 }  // namespace
+
+bool fp8_matmul_tiles(uint64_t ld_a, uint64_t ld_b) { return ld_a <= kMaxTileLd && ld_b <= kMaxTileLd; }
 
 uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k) {
     MatmulPart parts[kMatmulMostParts];

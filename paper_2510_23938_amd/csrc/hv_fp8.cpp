@@ -133,7 +133,8 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
     }
     HV_TRY(check_matrix("c", c, size_of(type), ld_c, n));
     const bool aligned = ld_a % 16 == 0 && ld_b % 16 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0;
-    const size_t need = hv_fp8_matmul_workspace_bytes(type, aligned, m, n, k);
+    const bool tiles = hv::fp8_matmul_tiles(ld_a, ld_b);
+    const size_t need = tiles ? hv_fp8_matmul_workspace_bytes(type, aligned, m, n, k) : 0;
     if (need > 0) {
         if (workspace == nullptr || workspace_bytes < need)
             return fail(HV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu%s", need, workspace_bytes,

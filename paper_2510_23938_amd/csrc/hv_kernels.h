@@ -277,10 +277,12 @@ struct MatmulPart {
     uint32_t splits;
     uint64_t rows, cols;
 };
-// wide: a 32-bit result; aligned: 16-byte aligned rows; tiles: leading dimensions below 2^23.
+// Leading dimensions below 2^23, which tiles take; rows further apart go straight from memory and need no scratch.
+bool fp8_matmul_tiles(uint64_t ld_a, uint64_t ld_b);
+// wide: a 32-bit result; aligned: 16-byte aligned rows; tiles: fp8_matmul_tiles.
 int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n, uint64_t k,
                      MatmulPart parts[kMatmulMostParts]);
-// Scratch bytes (0 where leading dimensions are not below 2^23).
+// Scratch bytes of a product whose leading dimensions tiles take.
 uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 

@@ -78,3 +78,24 @@ def test_matmul_on_two_streams_with_one_workspace():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_matmul_of_rows_far_apart_needs_no_workspace(dtype):
+    """Rows of 2^23 bytes or more apart go straight from memory, whatever the sizes: no sums to join, no copies."""
+    m, n, k = 40, 300, 9000
+    host, gpu = base.operands(np.random.default_rng(22), m, n, k, near=dtype != "f32")
+    assert hv.lib.hv_fp8_matmul_workspace_bytes(hv.TYPES[TYPES[dtype]], 1, m, n, k) > 0  # for rows nearer by
+    ld = 1 << 23
+
+    def apart(t):
+        wide = torch.empty(t.shape[0], ld, dtype=torch.uint8, device=DEV)[:, :k].view(torch.float8_e4m3fn)
+        wide.view(torch.uint8).copy_(t.view(torch.uint8))
+        return wide
+
+    a, sa, b, sb = apart(gpu[0]), gpu[1], apart(gpu[2]), gpu[3]
+    out = torch.empty(m, n, dtype=TYPES[dtype], device=DEV)
+    st = hv.lib.hv_fp8_matmul(hv.TYPES[TYPES[dtype]], a.data_ptr(), ld, sa.data_ptr(), b.data_ptr(), ld, sb.data_ptr(),
+                              m, n, k, out.data_ptr(), n, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert st == hv.HV_OK, hv.lib.hv_last_error()
+    base.check_product(out.double().cpu().numpy(), host, dtype)
