@@ -29,6 +29,9 @@ class VerifiedMLP:
 
     def __init__(self, norm, gate_up, down, expected: bytes):
         """``gate_up`` [2 ffn, d] and ``down`` [d, ffn]: (codes, scales) by blocks; ``expected``: their root."""
+        for codes, _ in (gate_up, down):
+            if codes.stride(0) % 16 or codes.data_ptr() % 16:  # a product may copy such rows before it reads them
+                raise ValueError("rows that are not 16-byte aligned would not be multiplied where they were verified")
         self.norm, self.gate_up, self.down = norm, gate_up, down
         self.pipe = hv.Pipeline(self.messages(norm, gate_up, down), CHUNK)
         if not self.pipe.run(expected):

@@ -4,8 +4,10 @@
  * The paper's threat model asks that the bytes that were checked are the bytes
  * that are used (Problem Statement & Threat Model: the TOCTOU discussion), and
  * its loader runs the model it has verified.  These operators run a decoder's
- * projections on 8-bit weights exactly as they lie in memory when the calls of
- * hv.h hash them: codes and scales, with no second copy in another layout.
+ * projections on 8-bit weights as they lie in memory when the calls of hv.h hash
+ * them: codes and scales, with no second copy in another layout.  (That goes for
+ * weights whose rows are 16-byte aligned.  Rows at other addresses hv_fp8_matmul may
+ * copy to its workspace, anew in each call, and multiply from there.)
  * Held in 8 bits, a weight set also takes half the time to hash.
  *
  * Format.  A code is an 8-bit floating-point number, OCP E4M3 (1 sign, 4
@@ -92,7 +94,8 @@ hv_status hv_fp8_gated(hv_type type, const void* gate, uint64_t ld_gate, const v
 /* Scratch bytes hv_fp8_matmul needs for a result of the type and these sizes; 0
  * where it needs none, and for a type or sizes that the call refuses.
  *   aligned: nonzero where a and b are 16-byte aligned and ld_a and ld_b multiples
- *            of 16 (other rows may be copied to aligned ones first). */
+ *            of 16.  An operand for which that does not hold may be copied to
+ *            aligned rows there first. */
 size_t hv_fp8_matmul_workspace_bytes(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k);
 
 /* c [m][n] = A times the transpose of B, for A [m][k] with scales by rows and B

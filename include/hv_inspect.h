@@ -97,7 +97,7 @@ hv_status hv_merkle_launches(hv_alg alg, const uint64_t* seg_offsets, uint32_t n
  * kind[i] = 0 (no columns: zeros), 1 to 4 (up to 16 rows of A against 16, 32, 64 or
  * 112 rows of B, straight from memory), 5 to 8 (tiles of 256 x 256, 256 x 128, 192 x
  * 128 or 128 x 128 through LDS), 9 (128 x 128, rows at any address), 10 (before
- * the others: A's and B's rows copied to aligned ones, a launch each) or 11 to 13 (up to 32
+ * the others: A's or B's rows, where they are not aligned, copied to aligned ones, a launch each) or 11 to 13 (up to 32
  * rows of A against 16, 32 or 64 rows of B, straight from memory); rows[i] and
  * cols[i] of c, from its first ones for the first of the others and to its last ones
  * for the second; splits[i], the parts of A's and B's columns whose sums one more

@@ -908,15 +908,14 @@ hipError_t launch_pack(const uint8_t* from, uint64_t ld, uint64_t rows, uint64_t
     return hipGetLastError();
 }
 
-bool rows_aligned(const MatmulArgs& x) {
-    return x.ld_a % 16 == 0 && x.ld_b % 16 == 0 && (uintptr_t)x.a % 16 == 0 && (uintptr_t)x.b % 16 == 0;
-}
+bool rows_aligned(const uint8_t* p, uint64_t ld) { return ld % 16 == 0 && (uintptr_t)p % 16 == 0; }
 
 template <typename T>
 hipError_t launch(MatmulArgs x, hipStream_t s) {
     const bool tiles = fp8_matmul_tiles(x.ld_a, x.ld_b);
+    const bool a_aligned = rows_aligned(x.a, x.ld_a), b_aligned = rows_aligned(x.b, x.ld_b);
     MatmulPart parts[kMatmulMostParts];
-    const int count = fp8_matmul_parts(sizeof(T) == 4, rows_aligned(x), tiles, x.m, x.n, x.k, parts);
+    const int count = fp8_matmul_parts(sizeof(T) == 4, a_aligned && b_aligned, tiles, x.m, x.n, x.k, parts);
     const Scratch scratch = scratch_of(parts, count, x.m, x.n, x.k);
     uint8_t* const workspace = (uint8_t*)x.workspace;
     x.workspace = workspace + scratch.sums;
@@ -925,11 +924,19 @@ hipError_t launch(MatmulArgs x, hipStream_t s) {
     for (int i = 0; i < count; ++i) {
         hipError_t e;
         if (parts[i].kind == kMatmulPack) {
-            e = launch_pack(x.a, x.ld_a, x.m, x.k, workspace + scratch.a, scratch.ld, s);
-            if (e == hipSuccess) e = launch_pack(x.b, x.ld_b, x.n, x.k, workspace + scratch.b, scratch.ld, s);
-            x.a = workspace + scratch.a;
-            x.b = workspace + scratch.b;
-            x.ld_a = x.ld_b = scratch.ld;
+            // only an operand whose own rows are at odd addresses: aligned ones, such as verified
+            // weights, are read where they lie
+            e = hipSuccess;
+            if (!a_aligned) {
+                e = launch_pack(x.a, x.ld_a, x.m, x.k, workspace + scratch.a, scratch.ld, s);
+                x.a = workspace + scratch.a;
+                x.ld_a = scratch.ld;
+            }
+            if (e == hipSuccess && !b_aligned) {
+                e = launch_pack(x.b, x.ld_b, x.n, x.k, workspace + scratch.b, scratch.ld, s);
+                x.b = workspace + scratch.b;
+                x.ld_b = scratch.ld;
+            }
         } else {  // its first rows and columns, or (a second one) the last
             const bool last = i > 0 && parts[i - 1].kind != kMatmulPack;
             const uint64_t row = last ? whole.rows - parts[i].rows : 0, col = last ? whole.cols - parts[i].cols : 0;

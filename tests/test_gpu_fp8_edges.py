@@ -1,10 +1,14 @@
 """The 8-bit operators at the ends of their ranges, against their definitions in 64 bits (oracle/fp8.py), and
 their calls on other streams, with shared scratch and with rows far apart."""
+import importlib.util
+import os
+
 import numpy as np
 import pytest
 import torch
 
 import test_gpu_fp8 as base
+from conftest import ROOT
 from oracle import fp8
 from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
 
@@ -99,3 +103,49 @@ def test_matmul_of_rows_far_apart_needs_no_workspace(dtype):
                               m, n, k, out.data_ptr(), n, None, 0, torch.cuda.current_stream().cuda_stream)
     assert st == hv.HV_OK, hv.lib.hv_last_error()
     base.check_product(out.double().cpu().numpy(), host, dtype)
+
+
+@pytest.mark.parametrize("odd", ["a", "b", "both"])
+def test_matmul_copies_no_operand_whose_rows_are_aligned(odd):
+    """Where the rows of one operand are at odd addresses and copying them pays, the other one, such as verified
+    weights, is read where it lies: the workspace's place for its copy is not written."""
+    m, n, k = 333, 11008, 1024
+    assert [p[0] for p in hv.matmul_launches(m, n, k, torch.bfloat16, False)] == ["pack", "192x128"]
+    host, (a, sa, b, sb) = base.operands(np.random.default_rng(25), m, n, k, near=True)
+
+    def moved(t):  # its first code one byte past an aligned address
+        return base.codes_on_gpu(t.view(torch.uint8).cpu().numpy(), 0, 1)
+
+    a = moved(a) if odd != "b" else a
+    b = moved(b) if odd != "a" else b
+    out = torch.empty(m, n, dtype=torch.bfloat16, device=DEV)
+    size = hv.lib.hv_fp8_matmul_workspace_bytes(hv.HV_BF16, 0, m, n, k)
+    ws = torch.full((size,), 0x55, dtype=torch.uint8, device=DEV)
+    st = hv.lib.hv_fp8_matmul(hv.HV_BF16, a.data_ptr(), k, sa.data_ptr(), b.data_ptr(), k, sb.data_ptr(), m, n, k,
+                              out.data_ptr(), n, ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream)
+    assert st == hv.HV_OK, hv.lib.hv_last_error()
+    base.check_product(out.double().cpu().numpy(), host, "bf16")
+    place = {"a": ws[:m * k].view(m, k), "b": ws[m * k + -(m * k) % 256:][:n * k].view(n, k)}
+    for name, t in (("a", a), ("b", b)):
+        if odd in (name, "both"):
+            assert torch.equal(place[name], t.view(torch.uint8))
+        else:
+            assert bool((place[name] == 0x55).all())
+
+
+def test_verified_layer_refuses_weights_that_a_product_would_copy():
+    spec = importlib.util.spec_from_file_location("verified_mlp", os.path.join(ROOT, "examples", "verified_mlp.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    layer = example.weights(256, 384, DEV)
+    root = example.VerifiedMLP.root_of(*layer)
+    example.VerifiedMLP(*layer, root)
+    for d, ffn in ((250, 384), (256, 392)):  # rows of a length that is no multiple of 16
+        odd = example.weights(d, ffn, DEV)
+        with pytest.raises(ValueError, match="16-byte"):
+            example.VerifiedMLP(*odd, example.VerifiedMLP.root_of(*odd))
+    norm, (codes, scales), down = layer
+    moved = torch.empty(codes.numel() + 1, dtype=torch.uint8, device=DEV)[1:].view(codes.shape)
+    moved.copy_(codes.view(torch.uint8))
+    with pytest.raises(ValueError, match="16-byte"):
+        example.VerifiedMLP(norm, (moved.view(codes.dtype), scales), down, root)
