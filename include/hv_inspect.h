@@ -92,16 +92,20 @@ hv_status hv_set_handover_polls(uint32_t polls);
 hv_status hv_merkle_launches(hv_alg alg, const uint64_t* seg_offsets, uint32_t n_seg, uint32_t cus, int* launches,
                              int* kind, uint64_t* units, uint64_t* one_lane);
 
-/* The launches hv_fp8_matmul makes for these sizes and rows (less than 2^23 bytes apart) that are 16-byte
- * aligned or not, for tests and measurements: *launches (at most 3; 0 for an empty c), and per launch
- * kind[i] = 0 (no columns: zeros), 1 to 4 (up to 16 rows of A against 16, 32, 64 or
- * 112 rows of B, straight from memory), 5 to 8 (tiles of 256 x 256, 256 x 128, 192 x
- * 128 or 128 x 128 through LDS), 9 (128 x 128, rows at any address), 10 (before
- * the others: A's or B's rows, where they are not aligned, copied to aligned ones, a launch each) or 11 to 13 (up to 32
- * rows of A against 16, 32 or 64 rows of B, straight from memory); rows[i] and
- * cols[i] of c, from its first ones for the first of the others and to its last ones
- * for the second; splits[i], the parts of A's and B's columns whose sums one more
- * launch adds (1: none).  All host arrays of 3 entries.  Host only; no device is needed.
+/* The launches hv_fp8_matmul makes for these sizes and rows (less than 2^23 bytes
+ * apart) that are 16-byte aligned or not, for tests and measurements: *launches (at
+ * most 3; 0 for an empty c), and per launch kind[i] =
+ *   0         no columns: zeros
+ *   1 to 4    up to 16 rows of A against 16, 32, 64 or 112 rows of B, straight from memory
+ *   5 to 8    tiles of 256 x 256, 256 x 128, 192 x 128 or 128 x 128 through LDS
+ *   9         tiles of 128 x 128, rows at any address
+ *   10        before the others: A's or B's rows, where they are not aligned, copied to
+ *             aligned ones, a launch each
+ *   11 to 13  up to 32 rows of A against 16, 32 or 64 rows of B, straight from memory
+ *   14, 15    as 1 to 4, against 48 or 80 rows of B
+ * rows[i] and cols[i] of c, from its first ones for the first of the others and to its
+ * last ones for the second; splits[i], the parts of A's and B's columns whose sums one
+ * more launch adds (1: none).  All host arrays of 3 entries.  Host only; no device is needed.
  * Errors: HV_ERR_INVALID_ARG for an unknown type, sizes that hv_fp8_matmul
  * refuses or a NULL output. */
 hv_status hv_fp8_matmul_launches(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k, int* launches, int* kind,

@@ -781,10 +781,15 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
 // Up to 16 rows of A (or 32, as two fragments) straight from memory.  A workgroup's
 // fragments of B share those of A, whose rows take as many loads as theirs, and a unit
 // with one workgroup more than others is the last to end: the fewest loads of a unit
-// that has the most (8 x 28672 x 8192: 57 us by single fragments, 56 by 2, 50 by 4, 47 by
-// 7; 16 x 8192 x 28672 71, 56, 78 and 112).  Up to four rows of A take next to nothing (1 x
-// 28672 x 8192: 42, 56, 48, 48).  Two fragments of A only where one workgroup on each unit is
-// enough (17 x 28672 x 8192 58 us, 49 by tiles).
+// that has the most (8 x 20480 x 4096: 23.2 us by single fragments, 18.4 by 5; 8 x 11008 x
+// 4096 14.6, 11.7 by 3; 16 x 8192 x 28672 71, 57 by 2, 78 by 4).  Of up to five fragments a
+// unit holds two workgroups at once; more leave room for one, so seven only where each unit
+// has but one (16 x 28672 x 8192: 45.9 us by 7, 49.3 by 4; 8 x 28672 x 8192 45.2 and 46.7; but 8
+// x 57344 x 4096 49.1 and 46.0 by 5), and six and eight never: three and four then do as
+// much in two rounds (16 x 24576 x 4096 24.3 us by 6, 22.9 by 3; 16 x 32768 x 8192 56.4 by 8,
+// 51.5 by 4).  Up to four rows of A take next to nothing (2 x 28672 x 8192: 44.6 us by single
+// fragments, 55.9, 49.0 and 49.4 by 2, 4 and 7).  Two fragments of A only where one workgroup
+// on each unit is enough (17 x 28672 x 8192 58 us, 49 by tiles).
 //
 // The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory. Rows
 // that are not 16-byte aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x
@@ -794,17 +799,25 @@ struct Stream {
     float cost;
 };
 Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t groups) {
-    constexpr int kFragments[] = {1, 2, 4, 7};
+    struct Kind {
+        int kind;
+        uint32_t each;  // fragments of B
+        bool alone;     // only where a unit has one workgroup
+    };
+    constexpr Kind kFew[] = {{kMatmulStream1, 1, false}, {kMatmulStream2, 2, false}, {kMatmulStream3, 3, false},
+                             {kMatmulStream4, 4, false}, {kMatmulStream5, 5, false}, {kMatmulStream7, 7, true}};
+    constexpr Kind kTwo[] = {{kMatmulStreamTwo1, 1, true}, {kMatmulStreamTwo2, 2, true}, {kMatmulStreamTwo4, 4, true}};
     const bool two = m > 16 && m <= 32;
     const uint64_t fragments = (n + 15) / 16;
     Stream best = {kMatmulStream1, INFINITY};
     uint64_t least = 0;
-    for (int i = 0; i < (m <= 4 ? 1 : two ? 3 : 4); ++i) {
-        const uint64_t each = kFragments[i], workgroups = (fragments + each - 1) / each;
-        const uint64_t rounds = (workgroups + kUnits - 1) / kUnits, loads = rounds * (16 * each + m);
-        if ((two && rounds > 1) || (least > 0 && loads >= least)) continue;
+    for (int i = 0; i < (m <= 4 ? 1 : two ? 3 : 6); ++i) {
+        const Kind& c = two ? kTwo[i] : kFew[i];
+        const uint64_t workgroups = (fragments + c.each - 1) / c.each, rounds = (workgroups + kUnits - 1) / kUnits;
+        const uint64_t loads = rounds * (16 * c.each + m);
+        if ((c.alone && rounds > 1) || (least > 0 && loads >= least)) continue;
         least = loads;
-        best = {(two ? kMatmulStreamTwo1 : kMatmulStream1) + i,
+        best = {c.kind,
                 3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f), (float)n * (float)k / 3.9e6f)};
     }
     return best;
@@ -865,7 +878,9 @@ hipError_t launch_part(const MatmulPart& p, const MatmulArgs& x, hipStream_t s) 
         case kMatmulZeros: return launch_join<T>(nullptr, 0, x, s);
         case kMatmulStream1: return launch_stream<T, 1, 1, 2>(x, s);
         case kMatmulStream2: return launch_stream<T, 1, 2, 2>(x, s);
+        case kMatmulStream3: return launch_stream<T, 1, 3, 1>(x, s);
         case kMatmulStream4: return launch_stream<T, 1, 4, 1>(x, s);
+        case kMatmulStream5: return launch_stream<T, 1, 5, 1>(x, s);
         case kMatmulStream7: return launch_stream<T, 1, 7, 1>(x, s);
         case kMatmulStreamTwo1: return launch_stream<T, 2, 1, 1>(x, s);
         case kMatmulStreamTwo2: return launch_stream<T, 2, 2, 1>(x, s);

@@ -257,7 +257,7 @@ hipError_t launch_fp8_gated(int type, const void* gate, uint64_t ld_gate, const 
 // part has the last rows or the last columns.
 enum : int {
     kMatmulZeros = 0,    // no columns
-    kMatmulStream1 = 1,  // 16 rows, B straight from memory; 1, 2, 4 or 7 fragments a workgroup
+    kMatmulStream1 = 1,  // 16 rows, B straight from memory; 1 to 5 or 7 fragments a workgroup
     kMatmulStream2 = 2,
     kMatmulStream4 = 3,
     kMatmulStream7 = 4,
@@ -270,6 +270,8 @@ enum : int {
     kMatmulStreamTwo1 = 11,  // 32 rows, B straight from memory; 1, 2 or 4 fragments a workgroup
     kMatmulStreamTwo2 = 12,
     kMatmulStreamTwo4 = 13,
+    kMatmulStream3 = 14,
+    kMatmulStream5 = 15,
 };
 constexpr int kMatmulMostParts = 3;
 struct MatmulPart {

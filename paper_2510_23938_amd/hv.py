@@ -676,8 +676,9 @@ def merkle_launches(seg_offsets, alg: str = "sha256", cus: int = 0) -> list:
     return [({1: "group", 2: "tile"}[kind[k]], int(units[k]), int(one[k])) for k in range(n.value)]
 
 
-_MATMUL_KINDS = ("zeros", "stream16", "stream32", "stream64", "stream112", "256x256", "256x128", "192x128", "128x128",
-                 "128x128 unaligned", "pack", "stream 2x16", "stream 2x32", "stream 2x64")
+# by the launch's number; "stream" are those of up to 16 rows of A, which the numbers tell apart by B's rows
+_MATMUL_KINDS = ("zeros", *4 * ("stream",), "256x256", "256x128", "192x128", "128x128", "128x128 unaligned", "pack",
+                 "stream 2x16", "stream 2x32", "stream 2x64", *2 * ("stream",))
 
 
 def matmul_launches(m: int, n: int, k: int, dtype=torch.bfloat16, aligned: bool = True) -> list:

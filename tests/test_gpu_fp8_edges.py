@@ -1,5 +1,6 @@
 """The 8-bit operators at the ends of their ranges, against their definitions in 64 bits (oracle/fp8.py), and
 their calls on other streams, with shared scratch and with rows far apart."""
+import ctypes
 import importlib.util
 import os
 
@@ -149,3 +150,23 @@ def test_verified_layer_refuses_weights_that_a_product_would_copy():
     moved.copy_(codes.view(torch.uint8))
     with pytest.raises(ValueError, match="16-byte"):
         example.VerifiedMLP(norm, (moved.view(codes.dtype), scales), down, root)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fragments", [1, 2, 3, 4, 5, 7])
+def test_matmul_by_each_number_of_fragments(fragments, dtype):
+    """Up to 16 rows of A against each number of fragments of B a workgroup, the last workgroup's not all there."""
+    kind = {1: 1, 2: 2, 3: 14, 4: 3, 5: 15, 7: 4}[fragments]
+    for m, short, k, pad in ((16, 0, 300, 4), (16, 27, 1024, 0), (15, 19, 300, 20)):
+        n = 4096 * fragments - short
+        assert _kinds(m, n, k, dtype) == [kind]
+        base.product(m, n, k, dtype, pad)
+
+
+def _kinds(m, n, k, dtype):
+    count = ctypes.c_int(0)
+    kind, splits = (ctypes.c_int * 3)(), (ctypes.c_uint32 * 3)()
+    rows, cols = (ctypes.c_uint64 * 3)(), (ctypes.c_uint64 * 3)()
+    assert hv.lib.hv_fp8_matmul_launches(hv.TYPES[TYPES[dtype]], 1, m, n, k, ctypes.byref(count), kind, rows, cols,
+                                         splits) == hv.HV_OK
+    return list(kind[:count.value])
