@@ -787,7 +787,9 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
 // has but one (16 x 28672 x 8192: 45.9 us by 7, 49.3 by 4; 8 x 28672 x 8192 45.2 and 46.7; but 8
 // x 57344 x 4096 49.1 and 46.0 by 5), and six and eight never: three and four then do as
 // much in two rounds (16 x 24576 x 4096 24.3 us by 6, 22.9 by 3; 16 x 32768 x 8192 56.4 by 8,
-// 51.5 by 4).  Up to four rows of A take next to nothing (2 x 28672 x 8192: 44.6 us by single
+// 51.5 by 4).  Rows at odd addresses wait for their requests, however many workgroups there
+// are (11 x 57344 x 1023: 34.9 us by 7, 45.3 by 5), and of equal loads the higher count ends
+// sooner (16 x 36864 x 2047: 61.9 us by 3, 46.8 by 5).  Up to four rows of A take next to nothing (2 x 28672 x 8192: 44.6 us by single
 // fragments, 55.9, 49.0 and 49.4 by 2, 4 and 7).  Two fragments of A only where one workgroup
 // on each unit is enough (17 x 28672 x 8192 58 us, 49 by tiles).
 //
@@ -802,7 +804,7 @@ Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t grou
     struct Kind {
         int kind;
         uint32_t each;  // fragments of B
-        bool alone;     // only where a unit has one workgroup
+        bool alone;     // only where a unit has one workgroup (single fragments of A: of aligned rows)
     };
     constexpr Kind kFew[] = {{kMatmulStream1, 1, false}, {kMatmulStream2, 2, false}, {kMatmulStream3, 3, false},
                              {kMatmulStream4, 4, false}, {kMatmulStream5, 5, false}, {kMatmulStream7, 7, true}};
@@ -815,7 +817,7 @@ Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t grou
         const Kind& c = two ? kTwo[i] : kFew[i];
         const uint64_t workgroups = (fragments + c.each - 1) / c.each, rounds = (workgroups + kUnits - 1) / kUnits;
         const uint64_t loads = rounds * (16 * c.each + m);
-        if ((c.alone && rounds > 1) || (least > 0 && loads >= least)) continue;
+        if ((c.alone && rounds > 1 && (two || aligned)) || (least > 0 && loads + aligned > least)) continue;
         least = loads;
         best = {c.kind,
                 3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f), (float)n * (float)k / 3.9e6f)};

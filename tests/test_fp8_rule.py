@@ -43,3 +43,15 @@ def test_up_to_four_rows_take_single_fragments():
     for m in (1, 4):
         for n in (16, 5000, 28672, 57344):
             assert kinds(m, n, 4096) == [1]
+
+
+@pytest.mark.parametrize("m", [5, 16])
+def test_few_rows_at_odd_addresses_take_the_fragments_that_load_least(m):
+    """Seven fragments in any number of rounds: their units hold as many requests whatever else they hold."""
+    taken = set()
+    for n in [16 * UNITS * e - short for e in range(1, 17) for short in (0, 100, 2000)] + [1000, 5001, 57344]:
+        kind, = kinds(m, n, 250, aligned=0)
+        loads = {e: busiest(m, n, e)[1] for e in (1, 2, 3, 4, 5, 7)}
+        assert loads[FRAGMENTS[kind]] == min(loads.values()), n
+        taken.add(FRAGMENTS[kind])
+    assert taken == {1, 2, 3, 4, 5, 7}
