@@ -793,9 +793,10 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
 // fragments, 55.9, 49.0 and 49.4 by 2, 4 and 7).  Two fragments of A only where one workgroup
 // on each unit is enough (17 x 28672 x 8192 58 us, 49 by tiles).
 //
-// The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory. Rows
-// that are not 16-byte aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x
-// 1025 x 1023 5.9 and 14.1; aligned 17 x 4096 x 4096 7.4 and 11.1, 32 x 8192 x 8192 21.3 and 16.9).
+// The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory (two
+// fragments, 17 x 16384 x 8192 31.1 us, 17 x 8192 x 4096 10.1).  Rows that are not 16-byte
+// aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x 1025 x 1023
+// 5.9 and 14.1).
 struct Stream {
     int kind;
     float cost;
@@ -820,9 +821,21 @@ Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t grou
         if ((c.alone && rounds > 1 && (two || aligned)) || (least > 0 && loads + aligned > least)) continue;
         least = loads;
         best = {c.kind,
-                3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f), (float)n * (float)k / 3.9e6f)};
+                3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f),
+                             (float)n * (float)k / (two ? 4.4e6f : 3.9e6f))};
     }
     return best;
+}
+
+// What tiles take for 17 to 32 rows of A, in us, where `cost` is what full ones take: less
+// for the rows that are not there, which at odd addresses are a request each, but all of B from
+// memory, by workgroups that mostly wait.  By tiles and by two fragments of A: 17 x 16384 x 4096
+// 23.5 and 17.5 us, x 2047 19.3 and 22.0, 24 x 4096 x 4095 in 32 bits 19.7 and 22.6, 32 x 8192 x 1023
+// 17.3 and 10.7; over 420 sizes from 17 x 500 x 259 to 32 x 16384 x 8192 the choice by these costs is
+// within 5% of the faster one (without this correction 20 of them lost 5% to 34%).
+float two_rows_cost(float cost, bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k) {
+    const float absent = !aligned ? 1.0f + 0.15f * (float)(32 - m) : wide ? 4.0f : 1.0f;
+    return fmaxf(cost - absent, 6.0f + (float)n * (float)k / 4.2e6f);
 }
 
 // Copying rows to aligned ones, in us: two launches (a small product waits for the
@@ -861,6 +874,7 @@ int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n
             plan = direct;
         }
     }
+    if (m > 16 && m <= 32) cost = two_rows_cost(cost, wide, aligned, m, n, k);
     if (m <= 32 && stream.cost < cost) {
         parts[0] = {stream.kind, 1, m, n};
         return 1;

@@ -55,3 +55,18 @@ def test_few_rows_at_odd_addresses_take_the_fragments_that_load_least(m):
         assert loads[FRAGMENTS[kind]] == min(loads.values()), n
         taken.add(FRAGMENTS[kind])
     assert taken == {1, 2, 3, 4, 5, 7}
+
+
+# (m, n, k, type, rows aligned): what is faster by a tenth or more, measured
+STREAM, TILES = True, False
+MEASURED = [(17, 16384, 4096, hv.HV_BF16, 1, STREAM), (24, 16384, 4096, hv.HV_BF16, 1, STREAM),
+            (32, 16384, 8192, hv.HV_BF16, 1, STREAM), (17, 16384, 8192, hv.HV_BF16, 1, STREAM),
+            (32, 8192, 1023, hv.HV_BF16, 0, STREAM), (24, 11008, 4096, hv.HV_F32, 1, STREAM),
+            (17, 16384, 2047, hv.HV_BF16, 0, TILES), (24, 500, 8192, hv.HV_F32, 1, TILES),
+            (17, 500, 4095, hv.HV_F32, 0, TILES), (24, 2000, 4095, hv.HV_F32, 0, TILES),
+            (24, 4096, 4095, hv.HV_F32, 0, TILES), (32, 16384, 4095, hv.HV_BF16, 0, TILES)]
+
+
+@pytest.mark.parametrize("m,n,k,type,aligned,stream", MEASURED)
+def test_two_fragments_of_rows_only_where_they_are_faster(m, n, k, type, aligned, stream):
+    assert (kinds(m, n, k, type, aligned)[0] in (11, 12, 13)) == stream
