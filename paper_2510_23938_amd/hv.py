@@ -1157,12 +1157,12 @@ def _device_of(t, what: str):
     return t.device
 
 
-def _matrix(t, dtypes, what: str, device, shape=None) -> tuple:
+def _matrix(t, dtypes, what: str, index: int, shape=None) -> tuple:
     """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
     lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
     what it is given, so anything it would overrun or misread is refused here."""
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on {device}")
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:  # half the time of comparing devices
+        raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on cuda:{index}")
     if t.dtype not in dtypes:
         raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
     if t.requires_grad and torch.is_grad_enabled():
@@ -1195,8 +1195,8 @@ _CODES = (torch.float8_e4m3fn,)
 _SCALES = (torch.float32,)
 
 
-def _scales(t, what: str, device, shape) -> int:
-    ptr, ld, rows, cols = _matrix(t, _SCALES, what, device, shape)
+def _scales(t, what: str, index: int, shape) -> int:
+    ptr, ld, rows, cols = _matrix(t, _SCALES, what, index, shape)
     if rows > 1 and ld != cols:
         raise ValueError(f"{what} must be contiguous")
     return ptr
@@ -1213,12 +1213,12 @@ def _coded(x, scales_shape, device, out, scales) -> tuple:
         out = _like(x, torch.float8_e4m3fn)
         ptr, ld = out.data_ptr(), x.shape[-1]
     else:
-        ptr, ld, _, _ = _matrix(out, _CODES, "out", device, x.shape)
+        ptr, ld, _, _ = _matrix(out, _CODES, "out", device.index, x.shape)
     if scales is None:
         scales = torch.empty(*scales_shape, dtype=torch.float32, device=device)
         scales_ptr = scales.data_ptr()
     else:
-        scales_ptr = _scales(scales, "scales", device, scales_shape)
+        scales_ptr = _scales(scales, "scales", device.index, scales_shape)
     return out, scales, ptr, ld, scales_ptr
 
 
@@ -1229,10 +1229,11 @@ def hv_fp8_quantize(x: torch.Tensor, tile: str = "rows", out=None, scales=None):
     if tile not in ("rows", "blocks"):
         raise ValueError(f"unknown tile {tile!r}; expected 'rows' or 'blocks'")
     dev = _device_of(x, "x")
-    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+    index = dev.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
         with torch.cuda.device(dev):
             return hv_fp8_quantize(x, tile, out, scales)
-    ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
+    ptr, ld, rows, cols = _matrix(x, TYPES, "x", index)
     if tile == "blocks":
         if x.dim() != 2:
             raise ValueError("quantisation by blocks takes a two-dimensional x")
@@ -1241,7 +1242,7 @@ def hv_fp8_quantize(x: torch.Tensor, tile: str = "rows", out=None, scales=None):
         scales_shape = (*x.shape[:-1], _groups(cols))
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x, scales_shape, dev, out, scales)
     _check(lib.hv_fp8_quantize(TYPES[x.dtype], ptr, ld, rows, cols, 1 if tile == "rows" else HV_FP8_GROUP, codes_ptr,
-                               ld_codes, scales_ptr, _current_stream(dev.index)))
+                               ld_codes, scales_ptr, _current_stream(index)))
     return out, scales
 
 
@@ -1251,25 +1252,26 @@ def hv_fp8_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual=
     ``weight``, quantised by rows.  h comes back in x's type, for the next layer (``residual_out``
     may be ``x`` or ``residual``, for the addition in place); without a residual it is None."""
     dev = _device_of(x, "x")
-    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+    index = dev.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
         with torch.cuda.device(dev):
             return hv_fp8_rms_norm(x, weight, eps, residual, out, scales, residual_out)
-    ptr, ld, rows, cols = _matrix(x, TYPES, "x", dev)
+    ptr, ld, rows, cols = _matrix(x, TYPES, "x", index)
     same = (x.dtype,)
-    weight_ptr = _matrix(weight, same, "weight", dev, (cols,))[0]
+    weight_ptr = _matrix(weight, same, "weight", index, (cols,))[0]
     res_ptr, ld_res, h_ptr, ld_h = None, 0, None, 0
     if residual is not None:
-        res_ptr, ld_res, _, _ = _matrix(residual, same, "residual", dev, x.shape)
+        res_ptr, ld_res, _, _ = _matrix(residual, same, "residual", index, x.shape)
         if residual_out is None:
             residual_out = _like(x, x.dtype)
             h_ptr, ld_h = residual_out.data_ptr(), cols
         else:
-            h_ptr, ld_h, _, _ = _matrix(residual_out, same, "residual_out", dev, x.shape)
+            h_ptr, ld_h, _, _ = _matrix(residual_out, same, "residual_out", index, x.shape)
     elif residual_out is not None:
         raise ValueError("residual_out without a residual")
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(x, (*x.shape[:-1], _groups(cols)), dev, out, scales)
     _check(lib.hv_fp8_rms_norm(TYPES[x.dtype], ptr, ld, res_ptr, ld_res, weight_ptr, eps, rows, cols, h_ptr, ld_h,
-                               codes_ptr, ld_codes, scales_ptr, _current_stream(dev.index)))
+                               codes_ptr, ld_codes, scales_ptr, _current_stream(index)))
     return out, scales, residual_out
 
 
@@ -1277,14 +1279,15 @@ def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
     """(codes, scales) of silu(gate) * up, quantised by rows.  ``gate`` and ``up`` may be the halves
     of one product's columns."""
     dev = _device_of(gate, "gate")
-    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+    index = dev.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
         with torch.cuda.device(dev):
             return hv_fp8_gated(gate, up, out, scales)
-    ptr, ld, rows, cols = _matrix(gate, TYPES, "gate", dev)
-    up_ptr, ld_up, _, _ = _matrix(up, (gate.dtype,), "up", dev, gate.shape)
+    ptr, ld, rows, cols = _matrix(gate, TYPES, "gate", index)
+    up_ptr, ld_up, _, _ = _matrix(up, (gate.dtype,), "up", index, gate.shape)
     out, scales, codes_ptr, ld_codes, scales_ptr = _coded(gate, (*gate.shape[:-1], _groups(cols)), dev, out, scales)
     _check(lib.hv_fp8_gated(TYPES[gate.dtype], ptr, ld, up_ptr, ld_up, rows, cols, codes_ptr, ld_codes, scales_ptr,
-                            _current_stream(dev.index)))
+                            _current_stream(index)))
     return out, scales
 
 
@@ -1296,28 +1299,29 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
     if dtype not in TYPES:
         raise ValueError(f"dtype is {dtype}; expected one of {[str(d) for d in TYPES]}")
     dev = _device_of(a, "a")
-    if dev.index != _current_device():  # a stream's handle of zero is the current device's default stream
+    index = dev.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
         with torch.cuda.device(dev):
             return hv_fp8_matmul(a, a_scales, b, b_scales, dtype, out, workspace)
-    a_ptr, ld_a, _, k = _matrix(a, _CODES, "a", dev)
-    b_ptr, ld_b, _, _ = _matrix(b, _CODES, "b", dev)
+    a_ptr, ld_a, _, k = _matrix(a, _CODES, "a", index)
+    b_ptr, ld_b, _, _ = _matrix(b, _CODES, "b", index)
     if b.dim() != 2 or b.shape[1] != k:
         raise ValueError(f"b has shape {tuple(b.shape)}; the call needs [n, {k}]")
     n = b.shape[0]
     lead = a.shape[:-1]
     m = lead.numel()
-    sa_ptr = _scales(a_scales, "a_scales", dev, (*lead, _groups(k)))
-    sb_ptr = _scales(b_scales, "b_scales", dev, (_groups(n), _groups(k)))
+    sa_ptr = _scales(a_scales, "a_scales", index, (*lead, _groups(k)))
+    sb_ptr = _scales(b_scales, "b_scales", index, (_groups(n), _groups(k)))
     if out is None:
         out = torch.empty(*lead, n, dtype=dtype, device=dev)
         out_ptr, ld_out = out.data_ptr(), n
     else:
-        out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", dev, (*lead, n))
+        out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", index, (*lead, n))
     aligned = not (ld_a % 16 or ld_b % 16 or a_ptr % 16 or b_ptr % 16)
     need = lib.hv_fp8_matmul_workspace_bytes(TYPES[dtype], aligned, m, n, k)
-    if workspace is not None and (workspace.device.type != "cuda" or workspace.device.index not in (None, dev.index)):
+    if workspace is not None and (workspace.device.type != "cuda" or workspace.device.index not in (None, index)):
         raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {dev}")
     ws = (workspace or Workspace(dev)).get(need) if need else None
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
-                             ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(dev.index)))
+                             ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(index)))
     return out
