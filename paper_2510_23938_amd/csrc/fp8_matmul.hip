@@ -796,7 +796,7 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
 // on each unit is enough (17 x 28672 x 8192 58 us, 49 by tiles).
 //
 // The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory (two
-// fragments, 17 x 16384 x 8192 31.1 us, 17 x 8192 x 4096 10.1).  Rows that are not 16-byte
+// fragments of A, by four of B 17 x 16384 x 8192 31.1 us, by two 17 x 8192 x 8192 20.5).  Rows that are not 16-byte
 // aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x 1025 x 1023
 // 5.9 and 14.1).
 struct Stream {
@@ -824,7 +824,7 @@ Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t grou
         least = loads;
         best = {c.kind,
                 3.0f + fmaxf((float)(loads * groups) * (aligned ? 0.0043f : 0.014f),
-                             (float)n * (float)k / (two ? 4.4e6f : 3.9e6f))};
+                             (float)n * (float)k / (two && c.each == 4 ? 4.7e6f : 3.9e6f))};
     }
     return best;
 }
@@ -833,11 +833,12 @@ Stream stream_of(bool aligned, uint64_t m, uint64_t n, uint64_t k, uint64_t grou
 // for the rows that are not there, which at odd addresses are a request each, but all of B from
 // memory, by workgroups that mostly wait.  By tiles and by two fragments of A: 17 x 16384 x 4096
 // 23.5 and 17.5 us, x 2047 19.3 and 22.0, 24 x 4096 x 4095 in 32 bits 19.7 and 22.6, 32 x 8192 x 1023
-// 17.3 and 10.7; over 420 sizes from 17 x 500 x 259 to 32 x 16384 x 8192 the choice by these costs is
-// within 5% of the faster one (without this correction 20 of them lost 5% to 34%).
+// 17.3 and 10.7.  Over 465 sizes from 17 x 500 x 259 to 32 x 8192 x 28672 the choice by these costs
+// is within 6% of the faster one, but for 8192 x 8192 of B, which tiles take 18.5 us for or 23.6,
+// from one run to another, and fragments 20.5; without this correction 20 of them lost 5% to 34%.
 float two_rows_cost(float cost, bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k) {
     const float absent = !aligned ? 1.0f + 0.15f * (float)(32 - m) : wide ? 4.0f : 1.0f;
-    return fmaxf(cost - absent, 6.0f + (float)n * (float)k / 4.2e6f);
+    return fmaxf(cost - absent, 6.0f + (float)n * (float)k / 5.0e6f);
 }
 
 // Copying rows to aligned ones, in us: two launches (a small product waits for the
