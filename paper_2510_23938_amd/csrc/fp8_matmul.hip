@@ -11,9 +11,9 @@
 //
 // Two kinds of kernels share the work, by the rows of A:
 //   up to 16   (small products: 32) bound by reading B: stream_kernel.  1 x 8192 x 8192 13.7 us (4.9
-//              TB/s), 8 x 28672 x 8192 47 us (5.0 TB/s, where a copy reaches 5.1).
+//              TB/s), 8 x 28672 x 8192 45 to 48 us (5.0 TB/s, where a copy reaches 5.1).
 //   more       bound by the matrix unit and its power: tile_kernel.  2048 x 28672 x
-//              8192 415 us (2.3 PFLOP/s; a library's product of the same codes
+//              8192 404 us (2.4 PFLOP/s; a library's product of the same codes
 //              without group scales 392).  A loop of this mix alone, products and four
 //              additions each from registers, reaches 3.1 PFLOP/s on ordinary codes and
 //              4.1 on equal ones: the chip lowers its clock to 1.7 GHz under it.
@@ -254,8 +254,8 @@ constexpr int scale_run(int stages) { return stages == 3 ? 3 : 4; }
 // rows are not 16-byte aligned (kDirect = false) through registers.
 //
 // Sizes and stages as they fit 160 KB of LDS and 256 registers a lane: 256 x 256 with
-// 2 (the least LDS traffic and loads for a product: 61% of the cycles have the matrix
-// unit busy, 1.73 GHz), 256 x 128 and 192 x 128 with 3, 128 x 128 with 4.  LDS reads
+// 2 (the least LDS traffic and loads for a product: 63% of the cycles have the matrix
+// unit busy, 1.86 GHz), 256 x 128 and 192 x 128 with 3, 128 x 128 with 4.  LDS reads
 // meet no bank conflicts; what is left is waiting at the meetings (30%) and for issue (34%).
 template <typename T, int TM, int TN, int WM, int WN, int S, bool kDirect>
 __global__ void __launch_bounds__(WM* WN * 64) tile_kernel(MatmulArgs x, Tiles tiles) {
@@ -791,14 +791,15 @@ Plan plan_of(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t groups) {
 // much in two rounds (16 x 24576 x 4096 24.3 us by 6, 22.9 by 3; 16 x 32768 x 8192 56.4 by 8,
 // 51.5 by 4).  Rows at odd addresses wait for their requests, however many workgroups there
 // are (11 x 57344 x 1023: 34.9 us by 7, 45.3 by 5), and of equal loads the higher count ends
-// sooner (16 x 36864 x 2047: 61.9 us by 3, 46.8 by 5).  Up to four rows of A take next to nothing (2 x 28672 x 8192: 44.6 us by single
-// fragments, 55.9, 49.0 and 49.4 by 2, 4 and 7).  Two fragments of A only where one workgroup
-// on each unit is enough (17 x 28672 x 8192 58 us, 49 by tiles).
+// sooner (16 x 36864 x 2047: 61.9 us by 3, 46.8 by 5).  Up to four rows of A take next to
+// nothing (2 x 28672 x 8192: 44.6 us by single fragments, 55.9, 49.0 and 49.4 by 2, 4 and 7).
+// Two fragments of A only where one workgroup on each unit is enough (17 x 28672 x 8192 58
+// us, 49 by tiles).
 //
 // The cost, in us: a launch, and a row of 128 bytes at a time or all of B from memory (two
-// fragments of A, by four of B 17 x 16384 x 8192 31.1 us, by two 17 x 8192 x 8192 20.5).  Rows that are not 16-byte
-// aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by tiles; 16 x 1025 x 1023
-// 5.9 and 14.1).
+// fragments of A, by four of B 17 x 16384 x 8192 31.1 us, by two 17 x 8192 x 8192 20.5).
+// Rows that are not 16-byte aligned take three times as long (16 x 1000 x 8191 32 us, 17.5 by
+// tiles; 16 x 1025 x 1023 5.9 and 14.1).
 struct Stream {
     int kind;
     float cost;

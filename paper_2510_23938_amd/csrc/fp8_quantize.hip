@@ -4,7 +4,7 @@
 //
 // All of them read and write each element once and are bound by HBM, where a copy
 // reaches 5.1 TB/s (bfloat16): norm with residual of 16384 x 8192 182 us (5.2 TB/s), gate of
-// 2048 x 28672 52 us (5.6), quantisation of 28672 x 8192 by blocks 150 us (4.7); one
+// 2048 x 28672 51 us (5.7), quantisation of 28672 x 8192 by blocks 150 us (4.7); one
 // row of 8192 takes 4 us, a launch and two trips to memory.  A lane holds 8
 // consecutive columns (16 bytes of a 16-bit type), so 16 lanes, one DPP row, hold a
 // group of 128: its largest magnitude is four rotations of the row away, without LDS.
@@ -67,7 +67,7 @@ struct GatedOf {  // gate / (1 + exp(-gate)) * up
         }
     }
     // For gates from -87 on: the reciprocal instruction is within one unit in the last place of a normal
-    // result; a division takes ten instructions more (2048 x 28672: 67 us instead of 54).
+    // result; a division takes ten instructions more (2048 x 28672: a quarter more time).
     static __device__ __forceinline__ float ordinary(float gate, float up) {
         return gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up;
     }
