@@ -244,18 +244,19 @@ class Workspace:
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)
+        self.index = self.device.index
         self.bufs = {}      # (device, stream, whether it is being captured) -> buffer
         self.captured = []  # every buffer that a capture was given
 
     def get(self, nbytes: int) -> torch.Tensor:
-        nbytes = max(int(nbytes), 256)
         if not self.bufs and self.device.type == "cuda":
             torch.cuda.init()
-        index = self.device.index if self.device.index is not None else _current_device()
-        key = (index, _current_stream(index), _capturing())
+        index = self.index if self.index is not None else _current_device()
+        stream = _current_stream(index)
+        key = (index, stream, stream != 0 and _capturing())  # the default stream cannot be captured
         buf = self.bufs.get(key)
         if buf is None or buf.numel() < nbytes:
-            buf = self.bufs[key] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            buf = self.bufs[key] = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
             if key[2]:
                 self.captured.append(buf)
         return buf
