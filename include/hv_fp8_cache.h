@@ -1,0 +1,95 @@
+/*
+ * hv_fp8_cache.h -- a cache of keys and values held in 8 bits.
+ *
+ * What stands between a decoder's projections on verified 8-bit weights (hv_fp8.h):
+ * new tokens' keys and values go to pages of a cache.
+ *
+ * Format.  A cache is a pool of pages of `page_tokens` tokens each, for every key
+ * head.  Codes are OCP E4M3 as in hv_fp8.h.  16 consecutive tokens of a page
+ * and head are a block and share a scale, one for their keys and one for their
+ * values.  A scale is a power of two from 2^-126 to 2^127 (a 32-bit number of which
+ * only the exponent is read); the value of a code is the code's number times it.
+ * Keys lie token by token, values of a block dimension by dimension, as the matrix
+ * unit reads them:
+ *   k_codes [pages][kv_heads][page_tokens][head_dim]
+ *   v_codes [pages][kv_heads][page_tokens / 16][head_dim][16]
+ *   k_scales, v_scales [pages][kv_heads][page_tokens / 16]
+ * Pages and heads of the codes may lie any multiple of 16 bytes apart that keeps
+ * them from overlapping; the rest is contiguous.  Codes are 16-byte aligned.
+ *
+ * Batches.  A call serves `count` sequences.  Sequence i has, with this call's new
+ * tokens, lengths[i] tokens; the new ones are the last of them and take the rows
+ * starts[i] to starts[i + 1] - 1 of the call's matrices, so a token in row t has
+ * the position lengths[i] - starts[i + 1] + t.  The token at position p of sequence
+ * i lies in page pages[i][p / page_tokens].  All three are device memory that the
+ * call's kernels read, so a captured call takes what they hold when it is replayed.
+ * What they may not hold is dealt with as follows, and nothing out of bounds is read
+ * or written: a sequence of no rows, and one whose rows are not within the
+ * call's, is left out (its rows, like those that belong to no sequence, are neither read nor
+ * written); tokens at negative positions, behind the table's last column or in a page that
+ * does not exist (any negative number may stand for none) are not in the cache: they are
+ * neither written nor seen.
+ *
+ * Every call is asynchronous on `stream` and queues kernels only, so it may be
+ * captured in a HIP graph.  All pointers but those to the two descriptions are
+ * device pointers of the device that is current; the descriptions are read before the call
+ * returns.  Strides count elements.  Rows of the wider
+ * matrices need no alignment beyond that of their element type; 16-byte aligned ones
+ * are read faster.  Inputs and outputs must not overlap.  A call with no elements to write
+ * does nothing.  Results do not depend on the stream or on what runs beside, and are equal
+ * bit for bit from call to call.
+ *
+ * Common errors: HV_ERR_INVALID_ARG for an unknown type, a NULL or misaligned pointer,
+ * strides that overlap, a head_dim that is no multiple of 16 from 16 to 256, a
+ * page_tokens that is no multiple of 16 from 16 to 65536, or sizes past the limits (pages
+ * 2^31 - 1, kv_heads 65535, sequences 65536, columns * page_tokens 2^30, tokens * heads
+ * 2^30, strides 2^40); HV_ERR_HIP.
+ */
+#ifndef HV_FP8_CACHE_H
+#define HV_FP8_CACHE_H
+
+#include "hv_fp8.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define HV_FP8_CACHE_BLOCK 16 /* tokens of a head that share a scale */
+
+typedef struct {
+    uint8_t* k_codes;
+    float* k_scales;
+    uint8_t* v_codes;
+    float* v_scales;
+    uint64_t pages, kv_heads, page_tokens, head_dim;
+    uint64_t k_page, k_head; /* bytes between the keys of neighbouring pages, and heads */
+    uint64_t v_page, v_head;
+} hv_fp8_cache;
+
+typedef struct {
+    const int32_t* starts;  /* [count + 1] */
+    const int32_t* lengths; /* [count] */
+    const int32_t* pages;   /* [count][columns], rows ld_pages apart */
+    uint64_t count, columns, ld_pages;
+} hv_fp8_batch;
+
+/* Writes the new tokens' keys and values.
+ * A block's scale is the smallest power of two (at least 2^-126) under which the finite
+ * new values written to it have codes of at most 448, or the scale that it had if that is
+ * larger and the block holds earlier tokens of the sequence.  Where it grows, the
+ * earlier tokens' codes are rounded to it.  (The scale being a power of two, that
+ * changes only codes that get below 2^-6, by at most half of the new scale's 2^-9.)
+ * A new value's code is value / scale rounded to the nearest E4M3 number, ties to
+ * even; a NaN or an infinity becomes a NaN code and leaves the rest of its block alone.
+ * Slots of a block behind its last new token stay as they are and hold nothing.
+ * No page may be written by two sequences in one call.
+ *   k, v: [tokens][kv_heads][head_dim] of the type, the dimensions of a head adjacent. */
+hv_status hv_fp8_cache_write(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* k,
+                             uint64_t k_token, uint64_t k_head, const void* v, uint64_t v_token, uint64_t v_head,
+                             uint64_t tokens, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* HV_FP8_CACHE_H */

@@ -1,6 +1,5 @@
 // hv_fp8.cpp -- C ABI of the 8-bit operators: argument checks and launches.
-#include "hv_fp8.h"
-#include "hv_host.h"
+#include "fp8_host.h"
 #include "hv_inspect.h"
 
 using namespace hvh;
@@ -11,15 +10,6 @@ constexpr uint64_t kMaxRows = ((uint64_t)1 << 31) - 1;
 constexpr uint64_t kMaxCols = (uint64_t)1 << 24;
 constexpr uint64_t kMaxSide = (uint64_t)1 << 27;  // of a product: rows and columns, rounded up to tiles, count in 32 bits
 constexpr uint64_t kMaxLd = (uint64_t)1 << 31;
-
-static_assert(HV_BF16 == hv::kTypeBf16 && HV_F16 == hv::kTypeF16 && HV_F32 == hv::kTypeF32, "element types");
-
-hv_status check_type(hv_type type) {
-    if (type == HV_BF16 || type == HV_F16 || type == HV_F32) return HV_OK;
-    return fail(HV_ERR_INVALID_ARG, "unknown element type %d", (int)type);
-}
-
-size_t size_of(hv_type type) { return type == HV_F32 ? 4 : 2; }
 
 hv_status check_size(uint64_t rows, uint64_t cols) {
     if (rows > kMaxRows || cols > kMaxCols)
@@ -38,22 +28,12 @@ hv_status check_product(uint64_t m, uint64_t n, uint64_t k) {
 
 // A matrix operand that is read or written: present, at its element's alignment, rows apart.
 hv_status check_matrix(const char* what, const void* p, size_t element, uint64_t ld, uint64_t cols) {
-    if (p == nullptr) return fail(HV_ERR_INVALID_ARG, "%s is NULL", what);
-    if ((uintptr_t)p % element != 0)
-        return fail(HV_ERR_INVALID_ARG, "%s is not %zu-byte aligned", what, element);
+    HV_TRY(check_pointer(what, p, element));
     if (ld < cols || ld > kMaxLd)
         return fail(HV_ERR_INVALID_ARG, "%s: leading dimension %llu is below its %llu columns or above the limit of %llu",
                     what, (unsigned long long)ld, (unsigned long long)cols, (unsigned long long)kMaxLd);
     return HV_OK;
 }
-
-#define HV_TRY(call)                     \
-    do {                                 \
-        const hv_status st_ = (call);    \
-        if (st_ != HV_OK) return st_;    \
-    } while (0)
-
-hv_status done(hipError_t e, const char* what) { return e == hipSuccess ? HV_OK : hip_fail(e, what); }
 
 }  // namespace
 
@@ -135,12 +115,7 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
     const bool aligned = ld_a % 16 == 0 && ld_b % 16 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0;
     const bool tiles = hv::fp8_matmul_tiles(ld_a, ld_b);
     const size_t need = tiles ? hv_fp8_matmul_workspace_bytes(type, aligned, m, n, k) : 0;
-    if (need > 0) {
-        if (workspace == nullptr || workspace_bytes < need)
-            return fail(HV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu%s", need, workspace_bytes,
-                        workspace ? "" : " (NULL)");
-        if ((uintptr_t)workspace % kAlign != 0) return fail(HV_ERR_WORKSPACE, "workspace is not 256-byte aligned");
-    }
+    HV_TRY(check_workspace(workspace, workspace_bytes, need));
     const hv::MatmulArgs args = {a, ld_a, a_scales, b, ld_b, b_scales, m, n, k, c, ld_c, workspace};
     return done(hv::launch_fp8_matmul(type, args, stream), "product kernel");
 }

@@ -288,4 +288,33 @@ int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n
 uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 
+// The 8-bit cache (fp8_cache.hip, fp8_attention.hip); as in hv_fp8_cache.h, checked.
+struct CacheArgs {
+    uint8_t* k_codes;
+    float* k_scales;
+    uint8_t* v_codes;
+    float* v_scales;
+    uint64_t k_page, k_head, v_page, v_head;  // bytes
+    uint32_t pages, heads, page_blocks, head_dim;
+    uint64_t divide;  // ceil(2^40 / page_blocks)
+};
+struct BatchArgs {
+    const int32_t* starts;
+    const int32_t* lengths;
+    const int32_t* table;
+    uint64_t ld_table;
+    uint32_t count;
+    int32_t capacity;  // tokens that a row of the table has pages for
+    int32_t tokens;    // rows of the call's matrices
+};
+struct WriteArgs {
+    CacheArgs cache;
+    BatchArgs batch;
+    const void* k;
+    uint64_t k_token, k_head;
+    const void* v;
+    uint64_t v_token, v_head;
+};
+hipError_t launch_fp8_cache_write(int type, const WriteArgs& a, hipStream_t s);
+
 }  // namespace hv

@@ -23,7 +23,8 @@ one root over them in the given order -- the paper's hierarchical roots) and
 ``verify`` (raises ``VerificationError`` on a mismatch, as the paper's
 loader does when a model fails its check), and the operators on matrices held
 in 8 bits (``include/hv_fp8.h``): ``hv_fp8_quantize``, ``hv_fp8_rms_norm``,
-``hv_fp8_gated`` and ``hv_fp8_matmul``.
+``hv_fp8_gated`` and ``hv_fp8_matmul``, and on a cache of keys and values in 8 bits
+(``include/hv_fp8_cache.h``): ``Fp8Cache`` and ``hv_fp8_cache_write``.
 """
 from __future__ import annotations
 
@@ -46,6 +47,7 @@ ALGS = {"sha256": (HV_SHA256, 32), "sha384": (HV_SHA384, 48)}
 HV_BF16, HV_F16, HV_F32 = 0, 1, 2
 # element type -> its hv_type code
 TYPES = {torch.bfloat16: HV_BF16, torch.float16: HV_F16, torch.float32: HV_F32}
+HV_FP8_CACHE_BLOCK = 16  # tokens of a head of an 8-bit cache that share a scale
 HV_FP8_GROUP = 128  # columns (and, for weights, rows) of an 8-bit matrix that share a scale
 _STATUS = {1: "HV_ERR_INVALID_ARG", 2: "HV_ERR_WORKSPACE", 3: "HV_ERR_HIP"}
 
@@ -70,6 +72,7 @@ EXPORTS = (
     "hv_verify_model",  # include/hv_plan.h
     "hv_fp8_quantize", "hv_fp8_rms_norm", "hv_fp8_gated", "hv_fp8_matmul_workspace_bytes",
     "hv_fp8_matmul",  # include/hv_fp8.h
+    "hv_fp8_cache_write",  # include/hv_fp8_cache.h
 )
 
 
@@ -107,6 +110,18 @@ class hv_result(ctypes.Structure):
 class hv_monitor_plan(ctypes.Structure):
     _fields_ = [("device", ctypes.c_void_p), ("alg", ctypes.c_int), ("n_msgs", ctypes.c_uint32),
                 ("chunk_bytes", ctypes.c_uint64), ("n_leaves", ctypes.c_uint64)]
+
+
+class hv_fp8_cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_uint64), ("kv_heads", ctypes.c_uint64),
+                ("page_tokens", ctypes.c_uint64), ("head_dim", ctypes.c_uint64), ("k_page", ctypes.c_uint64),
+                ("k_head", ctypes.c_uint64), ("v_page", ctypes.c_uint64), ("v_head", ctypes.c_uint64)]
+
+
+class hv_fp8_batch(ctypes.Structure):
+    _fields_ = [("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+                ("count", ctypes.c_uint64), ("columns", ctypes.c_uint64), ("ld_pages", ctypes.c_uint64)]
 
 
 def _load():
@@ -179,6 +194,7 @@ def _load():
         "hv_fp8_matmul_workspace_bytes": ([ctypes.c_int32, ctypes.c_int, u64, u64, u64], sz),
         "hv_fp8_matmul": ([ctypes.c_int32, vp, u64, vp, vp, u64, vp, u64, u64, u64, vp, u64, vp, sz, vp],
                           ctypes.c_int),
+        "hv_fp8_cache_write": ([vp, vp, ctypes.c_int32, vp, u64, u64, vp, u64, u64, u64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -1326,3 +1342,141 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
                              ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(index)))
     return out
+
+
+# --------------------------------------------------------------------------
+# the 8-bit cache of keys and values (include/hv_fp8_cache.h)
+
+_I32 = torch.int32
+
+
+def _strides(t) -> list:
+    """A tensor's strides, with those of dimensions of one element, which mean nothing, as if it were contiguous."""
+    strides, inner = list(t.stride()), 1
+    for i in range(t.dim() - 1, -1, -1):
+        if t.shape[i] <= 1:
+            strides[i] = inner
+        inner = strides[i] * max(t.shape[i], 1)
+    return strides
+
+
+def _on(t, dtypes, what: str, index: int):
+    """``t`` once it is known to be a tensor of one of the types on the call's GPU."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on cuda:{index}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, and the 8-bit operators have no backward pass: call them "
+                         "under torch.no_grad(), or on detached tensors")
+    return t
+
+
+def _heads(t, dtypes, what: str, index: int, shape=None) -> tuple:
+    """(data pointer, token stride, head stride) of [tokens, heads, head_dim], the dimensions of a head adjacent."""
+    _on(t, dtypes, what, index)
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}; the call needs "
+                         f"{'[tokens, heads, head_dim]' if shape is None else tuple(shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[1] * t.shape[2], t.shape[2]
+    token, head, one = _strides(t)
+    if one != 1:
+        raise ValueError(f"{what}: the elements of a head must be adjacent")
+    return t.data_ptr(), token, head
+
+
+class Fp8Cache:
+    """Keys and values in 8 bits, by pages: codes ``k_codes`` [pages, kv_heads, page_tokens, head_dim] and ``v_codes``
+    [pages, kv_heads, page_tokens // 16, head_dim, 16] (float8_e4m3fn) and a power of two for each 16 tokens of
+    a head, ``k_scales`` and ``v_scales`` [pages, kv_heads, page_tokens // 16] (float32).  Pages and heads of the
+    codes may lie apart, a multiple of 16 bytes each; the rest is contiguous."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        device = _device_of(k_codes, "k_codes")
+        index = device.index
+        if k_codes.dim() != 4:
+            raise ValueError(f"k_codes has shape {tuple(k_codes.shape)}; expected [pages, kv_heads, page_tokens, head_dim]")
+        pages, heads, tokens, dim = k_codes.shape
+        blocks = tokens // HV_FP8_CACHE_BLOCK
+        shapes = {"k_codes": k_codes.shape, "v_codes": (pages, heads, blocks, dim, HV_FP8_CACHE_BLOCK)}
+        for what, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+            _on(t, _CODES, what, index)
+            if t.shape != shapes[what]:
+                raise ValueError(f"{what} has shape {tuple(t.shape)}; it needs {shapes[what]}")
+            inner = (dim, 1) if what == "k_codes" else (dim * HV_FP8_CACHE_BLOCK, HV_FP8_CACHE_BLOCK, 1)
+            if tuple(_strides(t)[2:]) != inner:
+                raise ValueError(f"{what}: the codes of a page and head must be contiguous")
+        for what, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+            _on(t, _SCALES, what, index)
+            if t.shape != (pages, heads, blocks) or not t.is_contiguous():
+                raise ValueError(f"{what} must be contiguous, with shape {(pages, heads, blocks)}")
+        if heads == 0 or tokens == 0 or tokens % HV_FP8_CACHE_BLOCK or tokens > 65536 or not 16 <= dim <= 256 or dim % 16:
+            raise ValueError(f"a cache of {heads} heads, pages of {tokens} tokens and {dim} dimensions: heads are at "
+                             "least 1, page_tokens a multiple of 16 up to 65536, head_dim a multiple of 16 up to 256")
+        for what, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+            if t.data_ptr() % 16 or t.stride(0) % 16 and pages > 1 or t.stride(1) % 16 and heads > 1:
+                raise ValueError(f"{what}: pages and heads must be 16-byte aligned")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.pages, self.kv_heads, self.page_tokens, self.head_dim = pages, heads, tokens, dim
+        self.device = device
+        (k_page, k_head), (v_page, v_head) = _strides(k_codes)[:2], _strides(v_codes)[:2]
+        self._struct = hv_fp8_cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
+                                    pages, heads, tokens, dim, k_page, k_head, v_page, v_head)
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page_tokens: int, head_dim: int, device="cuda") -> Fp8Cache:
+        """A cache that holds nothing yet (all codes zero)."""
+        if page_tokens % HV_FP8_CACHE_BLOCK:
+            raise ValueError(f"page_tokens = {page_tokens} is no multiple of {HV_FP8_CACHE_BLOCK}")
+        blocks = page_tokens // HV_FP8_CACHE_BLOCK
+        codes = [torch.zeros(shape, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                 for shape in ((pages, kv_heads, page_tokens, head_dim),
+                               (pages, kv_heads, blocks, head_dim, HV_FP8_CACHE_BLOCK))]
+        scales = [torch.zeros(pages, kv_heads, blocks, dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(codes[0], scales[0], codes[1], scales[1])
+
+    def tensors(self) -> tuple:
+        """(k_codes, k_scales, v_codes, v_scales)."""
+        return self.k_codes, self.k_scales, self.v_codes, self.v_scales
+
+
+def _batch(starts, lengths, pages, index: int) -> hv_fp8_batch:
+    """The description of a batch: ``starts`` [count + 1], ``lengths`` [count], ``pages`` [count, columns], int32."""
+    for t, what in ((starts, "starts"), (lengths, "lengths"), (pages, "pages")):
+        if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype != _I32:
+            _on(t, (_I32,), what, index)
+    if lengths.dim() != 1 or not lengths.is_contiguous():
+        raise ValueError("lengths must be one-dimensional and contiguous")
+    count = lengths.shape[0]
+    if starts.shape != (count + 1,) or not starts.is_contiguous():
+        raise ValueError(f"starts must be contiguous, with {count + 1} elements: one more than lengths")
+    if pages.dim() != 2 or pages.shape[0] != count:
+        raise ValueError(f"pages has shape {tuple(pages.shape)}; the call needs [{count}, columns]")
+    columns = pages.shape[1]
+    if pages.is_contiguous():
+        ld = columns
+    else:
+        ld, one = _strides(pages)
+        if one != 1 or ld < columns:
+            raise ValueError("pages: the columns of a row must be adjacent and rows must not overlap")
+    return hv_fp8_batch(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), count, columns, ld)
+
+
+def hv_fp8_cache_write(cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, starts, lengths, pages) -> None:
+    """Writes new tokens' keys and values [tokens, kv_heads, head_dim] (bfloat16, float16 or float32) to the cache.
+    Sequence i's new tokens are the rows ``starts[i]`` to ``starts[i + 1]`` and the last of its ``lengths[i]`` tokens;
+    its token at position p goes to page ``pages[i, p // page_tokens]``.  All three are int32 tensors on the GPU.
+    No page may be written by two sequences of one call."""
+    index = cache.device.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(cache.device):
+            return hv_fp8_cache_write(cache, k, v, starts, lengths, pages)
+    k_ptr, k_token, k_head = _heads(k, TYPES, "k", index)
+    if k.shape[1] != cache.kv_heads or k.shape[2] != cache.head_dim:
+        raise ValueError(f"k has shape {tuple(k.shape)}; the cache needs [tokens, {cache.kv_heads}, {cache.head_dim}]")
+    v_ptr, v_token, v_head = _heads(v, (k.dtype,), "v", index, k.shape)
+    batch = _batch(starts, lengths, pages, index)
+    _check(lib.hv_fp8_cache_write(cache._ref, ctypes.byref(batch), TYPES[k.dtype], k_ptr, k_token, k_head, v_ptr,
+                                  v_token, v_head, k.shape[0], _current_stream(index)))
