@@ -1,8 +1,9 @@
 /*
- * hv_fp8_cache.h -- a cache of keys and values held in 8 bits.
+ * hv_fp8_cache.h -- a cache of keys and values held in 8 bits, and attention over it.
  *
  * What stands between a decoder's projections on verified 8-bit weights (hv_fp8.h):
- * new tokens' keys and values go to pages of a cache.
+ * new tokens' keys and values go to pages of a cache, and the tokens' queries are
+ * answered from there, one at a time or whole prompts.
  *
  * Format.  A cache is a pool of pages of `page_tokens` tokens each, for every key
  * head.  Codes are OCP E4M3 as in hv_fp8.h.  16 consecutive tokens of a page
@@ -87,6 +88,38 @@ typedef struct {
 hv_status hv_fp8_cache_write(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* k,
                              uint64_t k_token, uint64_t k_head, const void* v, uint64_t v_token, uint64_t v_head,
                              uint64_t tokens, hipStream_t stream);
+
+/* Scratch bytes hv_fp8_attention needs; 0 where it needs none, and for sizes that it refuses.
+ * `capacity`: columns * page_tokens of the batch. */
+size_t hv_fp8_attention_workspace_bytes(uint64_t sequences, uint64_t capacity, uint64_t tokens, uint64_t heads,
+                                        uint64_t kv_heads, uint64_t head_dim, uint32_t window, uint32_t sinks);
+
+/* Attention of the batch's new tokens over the cache, in which they are already:
+ *   out[t][h] = sum over visible positions j of w_j v_j,
+ *   w = softmax over them of scale * (q[t][h] . k_j),
+ * with the keys and values of key head h / (heads / kv_heads).  A token at position
+ * p sees the positions j <= p that are in the cache; with a window, of these only the
+ * last `window` (p - j < window) and the first `sinks` (j < sinks).  A token that sees
+ * nothing gets zeros.  What a token does not see does not change its output, whatever it
+ * holds (NaN included).
+ * Products of q and codes and of weights and codes are added in 32 bits, the softmax
+ * is in 32 bits; a weight is rounded to the type before its product, relative to its row's
+ * largest, and the result once.  Scores beyond 32 bits give NaN or, where all
+ * of a token's are minus infinity, zeros.
+ *   type: HV_BF16 or HV_F16, of q and out.
+ *   q, out: [tokens][heads][head_dim], the dimensions of a head adjacent; kv_heads divides heads.
+ *   scale: positive and finite.
+ *   window: 0 for none; sinks count only beside a window.
+ *   workspace: >= hv_fp8_attention_workspace_bytes(...), 256-byte aligned; NULL where that is 0.
+ *              Scratch: calls that share one must share a stream.
+ * For HV_F16, value codes are widened relative to the largest value scale met: a block whose scale
+ * is 2^-14 of it loses bits, and from 2^-24 on all of them.
+ * Errors: HV_ERR_INVALID_ARG also for another type, heads that are no multiple of kv_heads, or another
+ * scale; HV_ERR_WORKSPACE for a missing, short or misaligned workspace. */
+hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* q,
+                           uint64_t q_token, uint64_t q_head, uint64_t tokens, uint64_t heads, float scale,
+                           uint32_t window, uint32_t sinks, void* out, uint64_t out_token, uint64_t out_head,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

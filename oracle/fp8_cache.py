@@ -82,33 +82,36 @@ def write(cache, k, v, starts, lengths, table):
 
 
 def attention(cache, q, starts, lengths, table, scale, window=0, sinks=0):
-    """(out, spread): the attention of q [tokens, heads, dim] (64 bits), and the sum of weights times values' magnitudes,
-    which bounds what rounding weights can move; rows of no sequence are NaN."""
+    """Attention of q [tokens, heads, dim] (64 bits), (out, size, root, steep): the outputs, and what bounds their
+    rounding: size = sum of w |v|, root = the root of the sum of (w v)^2, and steep [tokens, heads], the largest sum of
+    |q k| * scale of a visible key.  Rows of no sequence are NaN."""
     tokens, heads, dim = q.shape
-    out, spread = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
+    out, size, root = (np.full(q.shape, np.nan) for _ in range(3))
+    steep = np.zeros((tokens, heads))
     share = heads // cache.heads
     for i, rows, position in sequences(starts, lengths, tokens):
         spots = [(j, place(cache, table, i, j)) for j in range(max(position + len(rows), 0))]
         spots = [(j, p) for j, p in spots if p is not None]
         at = np.array([j for j, _ in spots], dtype=np.int64)
-        where = np.array([p for _, p in spots], dtype=np.int64).reshape(-1, 3)
+        page, block, slot = np.array([p for _, p in spots], dtype=np.int64).reshape(-1, 3).T
         pos = position + np.arange(len(rows))[:, None]
         seen = at[None, :] <= pos
         if window:
             seen &= (pos - at[None, :] < window) | (at[None, :] < sinks)
         for head in range(cache.heads):
-            page, block, slot = where[:, 0], where[:, 1], where[:, 2]
             keys = VALUES[cache.k[page, head, block * BLOCK + slot]] * cache.ks[page, head, block].astype(np.float64)[:, None]
             vals = VALUES[cache.v[page, head, block, :, slot]] * cache.vs[page, head, block].astype(np.float64)[:, None]
             for h in range(head * share, (head + 1) * share):
                 for n, row in enumerate(rows):
                     vis = seen[n]
                     if not vis.any():
-                        out[row, h] = spread[row, h] = 0.0
+                        out[row, h] = size[row, h] = root[row, h] = 0.0
                         continue
-                    s = (keys[vis] @ q[row, h].astype(np.float64)) * scale
+                    k, v = keys[vis], vals[vis]
+                    s = (k @ q[row, h]) * scale
                     w = np.exp(s - s.max()) if np.isfinite(s).all() else np.full(s.shape, math.nan)
                     w /= w.sum()
-                    out[row, h] = w @ vals[vis]
-                    spread[row, h] = w @ np.abs(vals[vis])
-    return out, spread
+                    out[row, h], size[row, h] = w @ v, w @ np.abs(v)
+                    root[row, h] = np.sqrt((w * w) @ (v * v))
+                    steep[row, h] = (np.abs(k) @ np.abs(q[row, h])).max() * scale
+    return out, size, root, steep

@@ -2,6 +2,7 @@
 #pragma once
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include <hip/hip_runtime.h>
@@ -60,6 +61,13 @@ __device__ __forceinline__ Sequence sequence_in_lane(const Sequence& s, uint32_t
     return {__builtin_amdgcn_readlane(s.row, lane), __builtin_amdgcn_readlane(s.rows, lane),
             __builtin_amdgcn_readlane(s.position, lane)};
 }
+
+// A workgroup for each of more items than a launch's first dimension holds (2^32 threads): the rest in the third.
+constexpr uint32_t kRowOfItems = 1u << 20;
+inline dim3 item_grid(uint32_t items, uint32_t y = 1) {
+    return dim3(std::min(items, kRowOfItems), y, (items + kRowOfItems - 1) / kRowOfItems);
+}
+__device__ __forceinline__ uint32_t item_of_block() { return blockIdx.z * kRowOfItems + blockIdx.x; }
 
 // Which sequence an item belongs to, where sequence i has items(sequence) of them, and the item's
 // number there.  Every wave looks for itself; all its lanes take part.

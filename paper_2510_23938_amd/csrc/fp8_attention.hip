@@ -1,0 +1,908 @@
+// fp8_attention.hip -- attention of new tokens over the 8-bit cache:
+//   out = sum_j w_j v_j,  w = softmax_j(scale * q . k_j) over the positions that a token sees.
+//
+// One pass over the keys, 64 at a time, with the running maximum m and sum l of
+// each row's weights: p = exp2(s - m), l = sum p, o = sum p v, and where m grows by more
+// than 2^8 the sums so far are scaled down.  A "row" is one head of one new token; the
+// heads that share a key head and the tokens of a sequence are rows of one problem,
+// so each key is read once for all of them.
+//
+// Codes are widened to the 16-bit type, which holds them exactly, and multiplied by
+// its matrix instruction, whose sums are in 32 bits.  The product of keys and queries
+// is made transposed (keys down, rows across): its result leaves a lane with
+// weights of one row only, and the keys are taken in such an order that they are
+// those of one block of 16 tokens (or of two), all of them, in order.  That is the layout in which
+// the second product wants its weights, so they never leave the lane; a lane has one key
+// scale, which joins the softmax's own multiplication, and one value scale,
+// which the conversion of codes applies; and values lie in the cache by dimensions so that
+// their 16 bytes are those 16 tokens.
+//
+// Two kernels: few rows (a token or a few each of many sequences), bound by reading
+// the cache, take it from memory to registers; many rows, bound by the matrix and vector
+// units, share it in LDS.  In both, a sequence's keys are cut into segments where
+// there are too few rows to fill the chip; the parts' sums are joined by another kernel.
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "cache_device.h"
+
+namespace hv {
+namespace {
+
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using float4x = __attribute__((ext_vector_type(4))) float;
+using float16x = __attribute__((ext_vector_type(16))) float;
+
+constexpr int kTile = 64;         // keys of a step
+constexpr float kLazy = 8.0f;     // binary orders that a row's weights may grow before its sums are scaled
+constexpr float kNothing = -FLT_MAX;  // the maximum of a row that has seen nothing
+
+// ---------------------------------------------------------------------------
+// the 16-bit types
+
+template <typename T>
+struct Wide;
+
+template <>
+struct Wide<__bf16> {
+    using Eight = bf16x8;
+    // The exponents are those of 32 bits: a block's scale goes into its values as it is.
+    static constexpr bool kRelative = false;
+    template <bool kHigh>
+    static __device__ __forceinline__ bf16x2 two(uint32_t w, float scale) {
+        return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, kHigh);
+    }
+    static __device__ __forceinline__ Eight codes(uint32_t lo, uint32_t hi, float scale) {
+        const bf16x2 a = two<false>(lo, scale), b = two<true>(lo, scale), c = two<false>(hi, scale), d = two<true>(hi, scale);
+        return Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+    static __device__ __forceinline__ float4x mul16(Eight a, Eight b, float4x c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float16x mul32(Eight a, Eight b, float16x c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <>
+struct Wide<_Float16> {
+    using Eight = f16x8;
+    // Values times their scale may leave the type: they are taken relative to the largest scale met.
+    static constexpr bool kRelative = true;
+    template <bool kHigh>
+    static __device__ __forceinline__ f16x2 two(uint32_t w, float scale) {
+        return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, kHigh);
+    }
+    static __device__ __forceinline__ Eight codes(uint32_t lo, uint32_t hi, float scale) {
+        const f16x2 a = two<false>(lo, scale), b = two<true>(lo, scale), c = two<false>(hi, scale), d = two<true>(hi, scale);
+        return Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+    static __device__ __forceinline__ float4x mul16(Eight a, Eight b, float4x c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float16x mul32(Eight a, Eight b, float16x c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 2^e as the conversions' scale, at least 2^-126.
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)max(e + 127, 1) << 23); }
+__device__ __forceinline__ int exponent_of(float power) { return (int)(__float_as_uint(power) >> 23) - 127; }
+
+// The high bit of each byte that is a NaN code.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7f) + 0x01010101) & 0x80808080; }
+// Zero codes in their place.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+    const uint32_t m = nan_bytes(w);
+    return w & ~(m | (m - (m >> 7)));
+}
+// The code of 1 in their place, and of zero elsewhere.
+__device__ __forceinline__ uint32_t ones_at_nan(uint32_t w) {
+    const uint32_t m = nan_bytes(w);
+    return m >> 2 | m >> 3 | m >> 4;
+}
+
+// ---------------------------------------------------------------------------
+// which keys, and who takes them
+
+// Tiles of 64 keys that the positions p_min to p_max see: the first `sinks` of them from 0 on, the others from `first`.
+struct Range {
+    int first, sinks, count;
+    __device__ __forceinline__ int tile(int t) const { return t < sinks ? t : first + t - sinks; }
+};
+
+__device__ __forceinline__ Range range_of(const AttentionArgs& x, int p_min, int p_max) {
+    const int hi = min(p_max, x.batch.capacity - 1);
+    if (hi < 0) return {0, 0, 0};
+    const int lo = x.window ? max(p_min - x.window + 1, 0) : 0;
+    const int lo_tile = lo / kTile, hi_tile = hi / kTile;
+    const int sinks = x.window ? min(lo_tile, (min(x.sinks, hi + 1) + kTile - 1) / kTile) : 0;
+    return {lo_tile, sinks, sinks + max(hi_tile - lo_tile + 1, 0)};
+}
+
+// How a sequence's work is cut: row tiles of R rows, and the segments of each one's keys.
+struct Cut {
+    uint32_t units, segments;  // row tiles times key heads
+};
+
+template <int R>
+__device__ __forceinline__ uint32_t units_of(const AttentionArgs& x, const Sequence& s) {
+    return ((uint32_t)s.rows * x.share + R - 1) / R * x.cache.heads;
+}
+
+// A workgroup's work.
+struct Job {
+    bool found;
+    Sequence sequence;
+    uint32_t index, row_tile, head, segment, segments, part;
+};
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) v += __shfl_xor((unsigned long long)v, step);
+    return v;
+}
+
+// Tiles of a segment: an even share of all for each of `slots` workgroups, at least `least`.
+template <int R>
+__device__ __forceinline__ uint32_t segment_tiles(const AttentionArgs& x, uint32_t lane) {
+    if (x.slots == 0) return ~0u;
+    uint64_t total = 0;
+    for (uint32_t i = lane; i < x.batch.count; i += 64) {
+        const Sequence s = sequence_at(x.batch, i);
+        if (s.rows > 0)
+            total += (uint64_t)units_of<R>(x, s) * range_of(x, s.position, s.position + s.rows - 1).count;
+    }
+    const uint64_t share = (wave_sum(total) + x.slots - 1) / x.slots;
+    return (uint32_t)min(max(share, (uint64_t)x.least), (uint64_t)1 << 30);
+}
+
+// Segments of a sequence's row tiles.  A quarter of a segment more does not cost another, so the tiles of all that are
+// cut in two or more take fewer than 2 * slots: s < c / share + 3/4 with c / share > 5/4.
+__device__ __forceinline__ uint32_t segments_of(uint32_t tiles, uint32_t share) {
+    const uint32_t slack = share / 4;
+    return tiles <= share + slack ? 1 : (tiles - slack + share - 1) / share;
+}
+
+// The job of number `item`; or, for the join, that of the item-th unit which is cut (its first segment's).
+template <int R, bool kJoin>
+__device__ __forceinline__ Job find_job(const AttentionArgs& x, uint32_t item) {
+    const uint32_t lane = lane_id();
+    const uint32_t share = segment_tiles<R>(x, lane);
+    uint32_t part = 0;
+    for (uint32_t base = 0; base < x.batch.count; base += 64) {
+        const Sequence s = base + lane < x.batch.count ? sequence_at(x.batch, base + lane) : Sequence{0, 0, 0};
+        uint32_t units = 0, segments = 1;
+        if (s.rows > 0) {
+            units = units_of<R>(x, s);
+            segments = segments_of(range_of(x, s.position, s.position + s.rows - 1).count, share);
+        }
+        const uint32_t parts = segments > 1 ? units * segments : 0;
+        const uint32_t items = kJoin ? (segments > 1 ? units : 0) : units * segments;
+        const uint32_t upto = wave_scan(items), parts_upto = wave_scan(parts);
+        const uint64_t at = __ballot(upto > item);
+        if (at != 0) {
+            const uint32_t l = __builtin_ctzll(at);
+            const uint32_t within = item - __builtin_amdgcn_readlane(upto - items, l);
+            const uint32_t n = __builtin_amdgcn_readlane(segments, l), all = __builtin_amdgcn_readlane(items, l);
+            const uint32_t unit = kJoin ? within : within / n, segment = kJoin ? 0 : within - unit * n;
+            const uint32_t row_tiles = __builtin_amdgcn_readlane(units, l) / x.cache.heads;
+            const uint32_t row_tile = unit / x.cache.heads;
+            part += __builtin_amdgcn_readlane(parts_upto - parts, l) + unit * n + segment;
+            // the last rows, which see the most, first; what a batch without order may ask for stays in bounds
+            const bool ok = within < all && (n == 1 || part < x.parts_limit);
+            return {ok, sequence_in_lane(s, l), base + l, row_tiles - 1 - row_tile, unit - row_tile * x.cache.heads,
+                    segment, n, part};
+        }
+        item -= __builtin_amdgcn_readlane(upto, 63);
+        part += __builtin_amdgcn_readlane(parts_upto, 63);
+    }
+    return {};
+}
+
+// Whether some of the positions p_min to p_max sees some of the block's 16 tokens from `key` on.
+__device__ __forceinline__ bool block_seen(const AttentionArgs& x, int key, int p_min, int p_max) {
+    return key <= p_max && (!x.window || key + (int)kCacheBlock > p_min - x.window + 1 || key < x.sinks);
+}
+
+// The pages of a sequence's blocks of 16 tokens: a page and a block in it, or none.
+struct Places {
+    const int32_t* table;
+    uint32_t columns_end;  // blocks that the table has columns for
+    uint32_t pages, page_blocks;
+    uint64_t divide;
+    __device__ __forceinline__ Places(const AttentionArgs& x, uint32_t sequence)
+        : table(x.batch.table + sequence * x.batch.ld_table), columns_end((uint32_t)x.batch.capacity / kCacheBlock),
+          pages(x.cache.pages), page_blocks(x.cache.page_blocks), divide(x.cache.divide) {}
+    // page << 32 | block in it; -1 for none
+    __device__ __forceinline__ int64_t of(uint32_t block) const {
+        if (block >= columns_end) return -1;
+        const uint32_t column = page_column(block, divide);
+        const int32_t page = table[column];
+        return (uint32_t)page < pages ? (int64_t)page << 32 | (block - column * page_blocks) : -1;
+    }
+};
+
+// Parts' sums: [part][R][DP] sums, then [part][R] pairs of maximum and sum of weights.
+template <int R, int DP>
+__device__ __forceinline__ float* part_rows(const AttentionArgs& x, uint32_t part) {
+    return x.parts + (uint64_t)part * R * DP;
+}
+template <int R, int DP>
+__device__ __forceinline__ float2* part_weights(const AttentionArgs& x, uint32_t part) {
+    return (float2*)(x.parts + (uint64_t)x.parts_limit * R * DP) + (uint64_t)part * R;
+}
+
+// Four neighbouring dimensions of a row's output.
+template <typename T>
+__device__ __forceinline__ void store_four(T* p, float4x v) {
+    struct Four {
+        T v[4];
+    } four = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+    __builtin_memcpy(p, &four, sizeof four);
+}
+
+template <typename T>
+__device__ __forceinline__ T* out_at(const AttentionArgs& x, const Job& job, uint32_t row) {
+    const uint32_t token = row / x.share;
+    return (T*)x.out + (uint64_t)(job.sequence.row + token) * x.out_token +
+           (uint64_t)(job.head * x.share + (row - token * x.share)) * x.out_head;
+}
+
+// 16 neighbouring dimensions of a row's query; zeros where there are none.
+template <typename T>
+__device__ __forceinline__ void load_query(const AttentionArgs& x, const Job& job, uint32_t row, uint32_t rows, uint32_t d,
+                                           typename Wide<T>::Eight (&q)[2]) {
+    uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row < rows && d < x.cache.head_dim) {
+        const uint32_t token = row / x.share;
+        const T* const p = (const T*)x.q + (uint64_t)(job.sequence.row + token) * x.q_token +
+                           (uint64_t)(job.head * x.share + (row - token * x.share)) * x.q_head + d;
+        __builtin_memcpy(zero, p, 32);
+    }
+    __builtin_memcpy(&q[0], zero, 16);
+    __builtin_memcpy(&q[1], zero + 4, 16);
+}
+
+// ---------------------------------------------------------------------------
+// few rows: the cache from memory to registers
+
+// A workgroup takes 16 * F rows and one segment of their keys, its NW waves a tile of 64 keys in turn.  In a
+// tile, a lane (row n = lane % 16, group g = lane / 16) has the weights of block g.  For that, fragment f of four has
+// as its key m the token 4 f + m % 4 of block m / 4.
+template <typename T, int DP, int F, int NW>
+__global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
+    constexpr int R = 16 * F, NC = DP / 64, ND = DP / 16;
+    constexpr int CE = std::min(ND, 64 / (NW * F));  // 16 dimensions each of all waves' sums that LDS holds at once
+    static_assert(CE >= 1, "LDS holds a fragment of each wave");
+    using W = Wide<T>;
+    using Eight = typename W::Eight;
+    __shared__ float4x sums[NW][F][CE][64];
+    __shared__ float2 weights[NW][R];
+    const Job job = find_job<R, false>(x, item_of_block());
+    if (!job.found) return;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t n = lane % 16, g = lane / 16, dims = x.cache.head_dim;
+    const uint32_t rows_all = job.sequence.rows * x.share, row0 = job.row_tile * R, rows = min(rows_all - row0, (uint32_t)R);
+
+    Eight q[F][NC][2];
+    int pos[F];
+#pragma unroll
+    for (int fr = 0; fr < F; ++fr) {
+        const uint32_t row = 16 * fr + n;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) load_query<T>(x, job, row0 + row, row0 + rows, 64 * c + 16 * g, q[fr][c]);
+        pos[fr] = job.sequence.position + (int)((row0 + min(row, rows - 1)) / x.share);
+    }
+    const int p_min = job.sequence.position + (int)(row0 / x.share);
+    const int p_max = job.sequence.position + (int)((row0 + rows - 1) / x.share);
+    const Range range = range_of(x, p_min, p_max);
+    const int first = (int)((int64_t)range.count * job.segment / job.segments);
+    const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
+
+    const Places places(x, job.index);
+    const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head + (n % 4) * dims + 16 * g;
+    const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head + n * 16;
+    const uint64_t block_bytes = 16 * dims;
+
+    float4x o[F][ND];
+    float m[F], l[F];
+#pragma unroll
+    for (int fr = 0; fr < F; ++fr) {
+        m[fr] = kNothing;
+        l[fr] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < ND; ++e) o[fr][e] = float4x{0, 0, 0, 0};
+    }
+    int v_most = -126;  // kRelative: the exponent of the largest value scale met
+
+    uint4 k[4][NC], v[ND];
+    float k_scale = 0.0f, v_scale = 0.0f;
+    // a tile's places: of the block that a lane reads keys of, and of the one that it has values and weights of
+    int64_t k_place = -1, v_place = -1, k_next = -1, v_next = -1;
+    auto look = [&](int t, int64_t& kp, int64_t& vp) {
+        const uint32_t block = (uint32_t)range.tile(t) * 4;
+        kp = places.of(block + n / 4);
+        vp = places.of(block + g);
+    };
+    auto load_keys = [&](int64_t place) {
+        const uint8_t* const p = k_head + (place < 0 ? 0 : (place >> 32) * x.cache.k_page + (uint32_t)place * block_bytes);
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                k[f][c] = uint4{0, 0, 0, 0};
+                if (place >= 0 && 64 * c + 16 * g < dims) k[f][c] = *(const uint4*)(p + 4 * f * dims + 64 * c);
+            }
+    };
+    auto load_values = [&](int64_t place) {
+        const uint8_t* const p = v_head + (place < 0 ? 0 : (place >> 32) * x.cache.v_page + (uint32_t)place * block_bytes);
+#pragma unroll
+        for (int e = 0; e < ND; ++e) {
+            v[e] = uint4{0, 0, 0, 0};
+            if (place >= 0 && 16 * e + n < dims) v[e] = *(const uint4*)(p + 256 * e);
+        }
+    };
+    auto load_scales = [&](int64_t place) {
+        k_scale = v_scale = 0.0f;
+        if (place < 0) return;
+        const uint64_t at = ((place >> 32) * x.cache.heads + job.head) * x.cache.page_blocks + (uint32_t)place;
+        k_scale = x.cache.k_scales[at];
+        v_scale = x.cache.v_scales[at];
+    };
+
+    int t = first + (int)wave;
+    if (t < end) {
+        look(t, k_place, v_place);
+        if (t + NW < end) look(t + NW, k_next, v_next);
+        load_keys(k_place);
+        load_scales(v_place);
+        load_values(v_place);
+    }
+    for (; t < end; t += NW) {
+        const int tile = range.tile(t), key0 = tile * kTile;
+        const bool more = t + NW < end;
+        int64_t k_then = -1, v_then = -1;
+        if (t + 2 * NW < end) look(t + 2 * NW, k_then, v_then);
+
+        float4x s[F][4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+#pragma unroll
+            for (int fr = 0; fr < F; ++fr) s[fr][f] = float4x{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const Eight a = W::codes(k[f][c].x, k[f][c].y, 1.0f), b = W::codes(k[f][c].z, k[f][c].w, 1.0f);
+#pragma unroll
+                for (int fr = 0; fr < F; ++fr) {
+                    s[fr][f] = W::mul16(a, q[fr][c][0], s[fr][f]);
+                    s[fr][f] = W::mul16(b, q[fr][c][1], s[fr][f]);
+                }
+            }
+        }
+        const float to_log2 = fmaxf(cache_scale(k_scale) * x.scale, 0x1p-126f);
+        const float v_power = cache_scale(v_scale);
+        const bool here = v_place >= 0;
+        if (more) load_keys(k_next);
+
+        // whether some row does not see some key of the tile
+        const bool edge = key0 + kTile - 1 > p_min || __ballot(!here) != 0 ||
+                          (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
+        uint32_t seen[F];  // bit 4 f + r: the token 4 f + r of block g
+        if (edge) {
+#pragma unroll
+            for (int fr = 0; fr < F; ++fr) {
+                seen[fr] = 0;
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = key0 + 16 * (int)g + 4 * f + r;
+                        const bool sees = here && key <= pos[fr] && (!x.window || pos[fr] - key < x.window || key < x.sinks);
+                        seen[fr] |= (uint32_t)sees << (4 * f + r);
+                        s[fr][f][r] = sees ? s[fr][f][r] : -__builtin_inff();
+                    }
+            }
+        }
+        float widen_by = v_power;
+        if constexpr (W::kRelative) {
+            const int e = here && block_seen(x, key0 + 16 * (int)g, p_min, p_max) ? exponent_of(v_power) : -126;
+            int most = max(e, __shfl_xor(e, 16));
+            most = __builtin_amdgcn_readfirstlane(max(most, __shfl_xor(most, 32)));
+            if (most > v_most) {
+                const float down = exp2_fast((float)(v_most - most));
+#pragma unroll
+                for (int fr = 0; fr < F; ++fr)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) o[fr][d] *= down;
+                v_most = most;
+            }
+            widen_by = power_of(e - v_most);
+        }
+        Eight p[F][2];
+#pragma unroll
+        for (int fr = 0; fr < F; ++fr) {
+            float top = s[fr][0][0];
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, s[fr][f][r]);
+            top *= to_log2;
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__ballot(top > m[fr] + kLazy) != 0) {
+                const float grown = fmaxf(m[fr], top), down = exp2_fast(m[fr] - grown);
+                m[fr] = grown;
+                l[fr] *= down;
+#pragma unroll
+                for (int e = 0; e < ND; ++e) o[fr][e] *= down;
+            }
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float w = exp2_fast(fmaf(s[fr][f][r], to_log2, -m[fr]));
+                    l[fr] += w;
+                    p[fr][f / 2][f % 2 * 4 + r] = (T)w;
+                }
+        }
+        if (edge) {  // a NaN among the values reaches the rows that see it, and no others
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < ND; ++e) any |= nan_bytes(v[e].x) | nan_bytes(v[e].y) | nan_bytes(v[e].z) | nan_bytes(v[e].w);
+            if (__ballot(any != 0) != 0) {
+#pragma unroll
+                for (int fr = 0; fr < F; ++fr) {
+                    Eight sees[2];
+#pragma unroll
+                    for (int b = 0; b < 16; ++b) sees[b / 8][b % 8] = (T)(float)(seen[fr] >> b & 1);
+#pragma unroll
+                    for (int e = 0; e < ND; ++e) {
+                        float4x hits = {0, 0, 0, 0};
+                        hits = W::mul16(W::codes(ones_at_nan(v[e].x), ones_at_nan(v[e].y), 1.0f), sees[0], hits);
+                        hits = W::mul16(W::codes(ones_at_nan(v[e].z), ones_at_nan(v[e].w), 1.0f), sees[1], hits);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[fr][e][r] = hits[r] > 0 ? __builtin_nanf("") : o[fr][e][r];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < ND; ++e)
+                    v[e] = uint4{without_nan(v[e].x), without_nan(v[e].y), without_nan(v[e].z), without_nan(v[e].w)};
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < ND; ++e) {
+            const Eight a = W::codes(v[e].x, v[e].y, widen_by), b = W::codes(v[e].z, v[e].w, widen_by);
+#pragma unroll
+            for (int fr = 0; fr < F; ++fr) {
+                o[fr][e] = W::mul16(a, p[fr][0], o[fr][e]);
+                o[fr][e] = W::mul16(b, p[fr][1], o[fr][e]);
+            }
+        }
+        if (more) {
+            load_scales(v_next);
+            load_values(v_next);
+        }
+        k_place = k_next, v_place = v_next, k_next = k_then, v_next = v_then;
+    }
+
+    // the waves' sums, to their common maximum
+#pragma unroll
+    for (int fr = 0; fr < F; ++fr) {
+        l[fr] += __shfl_xor(l[fr], 16);
+        l[fr] += __shfl_xor(l[fr], 32);
+        if (g == 0) weights[wave][16 * fr + n] = float2{m[fr], l[fr]};
+    }
+    __syncthreads();
+    float down[F];
+#pragma unroll
+    for (int fr = 0; fr < F; ++fr) {
+        float most = kNothing;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = fmaxf(most, weights[w][16 * fr + n].x);
+        l[fr] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) l[fr] += exp2_fast(weights[w][16 * fr + n].x - most) * weights[w][16 * fr + n].y;
+        down[fr] = exp2_fast(m[fr] - most);
+        if constexpr (W::kRelative) down[fr] *= power_of(v_most);
+        m[fr] = most;
+    }
+    const bool whole = job.segments == 1;
+    if (!whole && wave == 0 && g == 0) {
+#pragma unroll
+        for (int fr = 0; fr < F; ++fr) part_weights<R, DP>(x, job.part)[16 * fr + n] = float2{m[fr], l[fr]};
+    }
+#pragma unroll
+    for (int e0 = 0; e0 < ND; e0 += CE) {
+        if (16u * e0 >= dims) break;
+        if (e0 > 0) __syncthreads();
+#pragma unroll
+        for (int fr = 0; fr < F; ++fr)
+#pragma unroll
+            for (int e = 0; e < CE; ++e)
+                if (e0 + e < ND) sums[wave][fr][e][lane] = o[fr][e0 + e < ND ? e0 + e : 0] * down[fr];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < (F * CE + NW - 1) / NW; ++i) {
+            const uint32_t at = i * NW + wave;  // uniform
+            const uint32_t fr = at / CE, e = at % CE, d = 16 * (e0 + e) + 4 * g, row = 16 * fr + n;
+            if (at >= F * CE || d >= dims || row >= rows) continue;
+            float4x sum = sums[0][fr][e][lane];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) sum += sums[w][fr][e][lane];
+            if (!whole) {
+                *(float4x*)(part_rows<R, DP>(x, job.part) + row * DP + d) = sum;
+                continue;
+            }
+            float total = 0.0f;
+#pragma unroll
+            for (int k = 0; k < F; ++k) total = (uint32_t)k == fr ? l[k] : total;
+            store_four(out_at<T>(x, job, row0 + row) + d, total == 0.0f ? float4x{0, 0, 0, 0} : sum / total);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// many rows: tiles of keys and values in LDS
+
+constexpr int kManyRows = 128;  // of a workgroup: four waves of 32
+
+// Where LDS has the 16-byte chunk of a key's row: an order in which eight lanes with neighbouring rows read
+// from different banks.
+template <int DP>
+__device__ __forceinline__ uint32_t chunk_place(uint32_t row, uint32_t chunk) {
+    return DP % 128 == 0 ? chunk ^ (row & 7) : chunk ^ (row >> 1 & 3);
+}
+
+// Lane (row n = lane % 32, half h = lane / 32) of a wave has the weights of the blocks h and 2 + h of a tile.  For
+// that, fragment f of two has as its key m the token 4 (m / 8) + m % 4 of block 2 f + m / 4 % 2, and LDS holds the keys in
+// that order.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(AttentionArgs x) {
+    constexpr int R = kManyRows, NC = DP / 32, CP = DP / 16;
+    constexpr int KL = 64 * CP / 256, VL = 4 * DP / 256;  // 16-byte loads of a thread
+    using W = Wide<T>;
+    using Eight = typename W::Eight;
+    __shared__ uint4 keys[2][64 * CP];
+    __shared__ uint4 vals[2][4 * DP];
+    const Job job = find_job<R, false>(x, item_of_block());
+    if (!job.found) return;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t n = lane % 32, h = lane / 32, dims = x.cache.head_dim;
+    const uint32_t rows_all = job.sequence.rows * x.share, row0 = job.row_tile * R, rows = min(rows_all - row0, (uint32_t)R);
+    const uint32_t my_row0 = row0 + wave * 32;
+    const bool idle = wave * 32 >= rows;  // a wave without rows loads and meets the others, no more
+    const uint32_t my_rows = idle ? 1 : min(rows - wave * 32, 32u);
+
+    Eight q[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) load_query<T>(x, job, my_row0 + n, row0 + rows, 32 * c + 16 * h, q[c]);
+    const int base = job.sequence.position;
+    const int pos = base + (int)(min(my_row0 + n, row0 + rows - 1) / x.share);
+    const int p_min = base + (int)(min(my_row0, row0 + rows - 1) / x.share);
+    const int p_max = base + (int)(min(my_row0 + my_rows - 1, row0 + rows - 1) / x.share);
+    const Range range = range_of(x, base + (int)(row0 / x.share), base + (int)((row0 + rows - 1) / x.share));
+    const int first = (int)((int64_t)range.count * job.segment / job.segments);
+    const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
+
+    const Places places(x, job.index);
+    const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head;
+    const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head;
+    const uint32_t block_bytes = 16 * dims;
+
+    float16x o[DP / 32];
+#pragma unroll
+    for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[e][i] = 0.0f;
+    float m = kNothing, l = 0.0f;
+    int v_most = -126;
+
+    // of the tile that loads are under way for
+    uint4 k_in[KL], v_in[VL];
+    float k_scale[2], v_scale[2];
+    int64_t place[4];
+    auto look = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) place[j] = places.of((uint32_t)range.tile(t) * 4 + j);
+    };
+    auto load = [&]() {
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+            const uint32_t id = i * 256 + threadIdx.x, row = id / CP, chunk = chunk_place<DP>(row, id % CP);
+            const uint32_t km = row % 32, token = 4 * (km / 8) + km % 4, j = 2 * (row / 32) + km / 4 % 2;
+            const int64_t p = j == 0 ? place[0] : j == 1 ? place[1] : j == 2 ? place[2] : place[3];
+            k_in[i] = uint4{0, 0, 0, 0};
+            if (p >= 0 && 16 * chunk < dims)
+                k_in[i] = *(const uint4*)(k_head + (p >> 32) * x.cache.k_page + (uint64_t)(uint32_t)p * block_bytes +
+                                          token * dims + 16 * chunk);
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const uint32_t id = i * 256 + threadIdx.x, j = id / DP, d = id % DP;
+            const int64_t p = j == 0 ? place[0] : j == 1 ? place[1] : j == 2 ? place[2] : place[3];
+            v_in[i] = uint4{0, 0, 0, 0};
+            if (p >= 0 && d < dims)
+                v_in[i] = *(const uint4*)(v_head + (p >> 32) * x.cache.v_page + (uint64_t)(uint32_t)p * block_bytes + 16 * d);
+        }
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int64_t p = h == 0 ? place[2 * f] : place[2 * f + 1];
+            k_scale[f] = v_scale[f] = 0.0f;
+            if (p >= 0) {
+                const uint64_t at = ((p >> 32) * x.cache.heads + job.head) * x.cache.page_blocks + (uint32_t)p;
+                k_scale[f] = x.cache.k_scales[at];
+                v_scale[f] = x.cache.v_scales[at];
+            }
+        }
+    };
+    auto hand_over = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < KL; ++i) keys[stage][i * 256 + threadIdx.x] = k_in[i];
+#pragma unroll
+        for (int i = 0; i < VL; ++i) vals[stage][i * 256 + threadIdx.x] = v_in[i];
+    };
+
+    if (first < end) {
+        look(first);
+        load();
+        hand_over(0);
+    }
+    __syncthreads();
+    for (int t = first; t < end; ++t) {
+        const int stage = (t - first) & 1, key0 = range.tile(t) * kTile;
+        float to_log2[2], v_power[2];
+        bool here[2];
+        bool gaps = false;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            to_log2[f] = fmaxf(cache_scale(k_scale[f]) * x.scale, 0x1p-126f);
+            v_power[f] = cache_scale(v_scale[f]);
+            here[f] = (h == 0 ? place[2 * f] : place[2 * f + 1]) >= 0;
+            gaps |= place[2 * f] < 0 || place[2 * f + 1] < 0;
+        }
+        if (t + 1 < end) {
+            look(t + 1);
+            load();
+        }
+        if (!idle && key0 <= p_max) {
+            float16x s[2];
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[f][i] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const uint4 w = keys[stage][(32 * f + n) * CP + chunk_place<DP>(n, 2 * c + h)];
+                    s[f] = W::mul32(W::codes(w.x, w.y, 1.0f), q[c][0], s[f]);
+                    s[f] = W::mul32(W::codes(w.z, w.w, 1.0f), q[c][1], s[f]);
+                }
+            }
+            const bool edge = key0 + kTile - 1 > p_min || gaps ||
+                              (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
+            uint32_t seen[2];
+            if (edge) {
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    seen[f] = 0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = key0 + 32 * f + 16 * (int)h + i;
+                        const bool sees = here[f] && key <= pos && (!x.window || pos - key < x.window || key < x.sinks);
+                        seen[f] |= (uint32_t)sees << i;
+                        s[f][i] = sees ? s[f][i] : -__builtin_inff();
+                    }
+                }
+            }
+            float widen_by[2] = {v_power[0], v_power[1]};
+            if constexpr (W::kRelative) {
+                int e[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+                    e[f] = here[f] && block_seen(x, key0 + 32 * f + 16 * (int)h, p_min, p_max) ? exponent_of(v_power[f]) : -126;
+                int most = max(e[0], e[1]);
+                most = __builtin_amdgcn_readfirstlane(max(most, __shfl_xor(most, 32)));
+                if (most > v_most) {
+                    const float down = exp2_fast((float)(v_most - most));
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) o[d] *= down;
+                    v_most = most;
+                }
+                widen_by[0] = power_of(e[0] - v_most);
+                widen_by[1] = power_of(e[1] - v_most);
+            }
+            float top[2];
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                top[f] = s[f][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top[f] = fmaxf(top[f], s[f][i]);
+            }
+            float most = fmaxf(top[0] * to_log2[0], top[1] * to_log2[1]);
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (__ballot(most > m + kLazy) != 0) {
+                const float grown = fmaxf(m, most), down = exp2_fast(m - grown);
+                m = grown;
+                l *= down;
+#pragma unroll
+                for (int e = 0; e < DP / 32; ++e) o[e] *= down;
+            }
+            Eight p[2][2];
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
+                    l += w;
+                    p[f][i / 8][i % 8] = (T)w;
+                }
+            bool mend = false;
+            if (edge) {  // a NaN among the values reaches the rows that see it, and no others
+                uint32_t any = 0;
+#pragma unroll
+                for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
+                        any |= nan_bytes(w.x) | nan_bytes(w.y) | nan_bytes(w.z) | nan_bytes(w.w);
+                    }
+                mend = __ballot(any != 0) != 0;
+                if (mend) {
+                    Eight sees[2][2];
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sees[f][i / 8][i % 8] = (T)(float)(seen[f] >> i & 1);
+#pragma unroll
+                    for (int e = 0; e < DP / 32; ++e) {
+                        float16x hits;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) hits[i] = 0.0f;
+#pragma unroll
+                        for (int f = 0; f < 2; ++f) {
+                            const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
+                            hits = W::mul32(W::codes(ones_at_nan(w.x), ones_at_nan(w.y), 1.0f), sees[f][0], hits);
+                            hits = W::mul32(W::codes(ones_at_nan(w.z), ones_at_nan(w.w), 1.0f), sees[f][1], hits);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[e][i] = hits[i] > 0 ? __builtin_nanf("") : o[e][i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
+                    if (mend) w = uint4{without_nan(w.x), without_nan(w.y), without_nan(w.z), without_nan(w.w)};
+                    o[e] = W::mul32(W::codes(w.x, w.y, widen_by[f]), p[f][0], o[e]);
+                    o[e] = W::mul32(W::codes(w.z, w.w, widen_by[f]), p[f][1], o[e]);
+                }
+        }
+        if (t + 1 < end) hand_over(stage ^ 1);
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32);
+    if constexpr (W::kRelative) {
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) o[e] *= power_of(v_most);
+    }
+    if (idle || n >= my_rows) return;
+    const uint32_t row = wave * 32 + n;
+    if (job.segments > 1 && h == 0) part_weights<R, DP>(x, job.part)[row] = float2{m, l};
+    const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const uint32_t d = 32 * e + 8 * a + 4 * h;
+            if (d >= dims) continue;
+            const float4x four = {o[e][4 * a], o[e][4 * a + 1], o[e][4 * a + 2], o[e][4 * a + 3]};
+            if (job.segments > 1)
+                *(float4x*)(part_rows<R, DP>(x, job.part) + row * DP + d) = four;
+            else
+                store_four(out_at<T>(x, job, row0 + row) + d, l == 0.0f ? float4x{0, 0, 0, 0} : four * inverse);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// the parts' sums joined, in order: workgroups of 16 rows of each unit that is cut
+
+template <typename T, int DP, int R>
+__global__ void __launch_bounds__(4 * DP) join_attention(AttentionArgs x) {
+    constexpr uint32_t kLanes = DP / 4;
+    const Job job = find_job<R, true>(x, blockIdx.x);
+    if (!job.found) return;
+    const uint32_t rows = min(job.sequence.rows * x.share - job.row_tile * R, (uint32_t)R);
+    const uint32_t row = blockIdx.y * 16 + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+    if (row >= rows || d >= x.cache.head_dim) return;
+    const float2* const weights = part_weights<R, DP>(x, job.part) + row;
+    float most = kNothing;
+    for (uint32_t i = 0; i < job.segments; ++i) most = fmaxf(most, weights[i * R].x);
+    float total = 0.0f;
+    float4x sum = {0, 0, 0, 0};
+    const float* const from = part_rows<R, DP>(x, job.part) + row * DP + d;
+#pragma unroll 4
+    for (uint32_t i = 0; i < job.segments; ++i) {
+        const float2 w = weights[i * R];
+        const float up = exp2_fast(w.x - most);
+        total += up * w.y;
+        sum += up * *(const float4x*)(from + (uint64_t)i * R * DP);
+    }
+    store_four(out_at<T>(x, job, job.row_tile * R + row) + d, total == 0.0f ? float4x{0, 0, 0, 0} : sum / total);
+}
+
+// ---------------------------------------------------------------------------
+// launches
+
+template <typename T, int DP, int R, typename Main>
+hipError_t run(const AttentionArgs& a, const AttentionPlan& plan, uint32_t threads, Main main, hipStream_t s) {
+    main<<<item_grid(plan.jobs), threads, 0, s>>>(a);
+    if (plan.join == 0) return hipGetLastError();
+    join_attention<T, DP, R><<<dim3(plan.join, R / 16), 4 * DP, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch(const AttentionArgs& a, const AttentionPlan& plan, hipStream_t s) {
+    switch (plan.rows) {
+        case 16: return run<T, DP, 16>(a, plan, 512, stream_attention<T, DP, 1, 8>, s);
+        case 32: {
+            constexpr int NW = DP <= 128 ? 8 : 4;
+            return run<T, DP, 32>(a, plan, NW * 64, stream_attention<T, DP, 2, NW>, s);
+        }
+        case 64:
+            if constexpr (DP <= 128) return run<T, DP, 64>(a, plan, 256, stream_attention<T, DP, 4, 4>, s);
+            [[fallthrough]];
+        default: return run<T, DP, kManyRows>(a, plan, 256, tile_attention<T, DP>, s);
+    }
+}
+
+template <typename T>
+hipError_t launch(const AttentionArgs& a, const AttentionPlan& plan, hipStream_t s) {
+    switch (plan.dims) {
+        case 64: return launch<T, 64>(a, plan, s);
+        case 128: return launch<T, 128>(a, plan, s);
+        case 192: return launch<T, 192>(a, plan, s);
+        default: return launch<T, 256>(a, plan, s);
+    }
+}
+
+}  // namespace
+
+AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t tokens, uint64_t heads, uint64_t kv_heads,
+                                 uint64_t head_dim, uint64_t window, uint64_t sinks) {
+    AttentionPlan plan = {};
+    plan.dims = (uint32_t)((head_dim + 63) / 64 * 64);
+    const uint64_t share = heads / kv_heads;
+    const uint64_t rows = (tokens + sequences - 1) / sequences * share;  // of a sequence, on the average
+    plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && plan.dims <= 128 ? 64 : kManyRows;
+    const uint64_t units = kv_heads * (tokens * share / plan.rows + std::min(sequences, tokens));
+    // tiles that one row tile may see at most
+    const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
+    const uint64_t tiles = (reach + kTile - 1) / kTile;
+    plan.least = 8;
+    plan.slots = 512;
+    if (tiles <= plan.least + plan.least / 4) plan.slots = 0;  // segments_of gives one
+    plan.jobs = (uint32_t)(units + 2 * plan.slots);
+    plan.join = (uint32_t)std::min<uint64_t>(units, plan.slots);
+    plan.parts = 2 * plan.slots;
+    plan.workspace = (uint64_t)plan.parts * plan.rows * (plan.dims + 2) * sizeof(float);
+    return plan;
+}
+
+hipError_t launch_fp8_attention(int type, AttentionArgs a, const AttentionPlan& plan, hipStream_t s) {
+    a.slots = plan.slots;
+    a.least = plan.least;
+    a.parts_limit = plan.parts;
+    return type == kTypeBf16 ? launch<__bf16>(a, plan, s) : launch<_Float16>(a, plan, s);
+}
+
+}  // namespace hv

@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kWaves * 64) write_kernel(WriteArgs x) {
     if (head >= x.cache.heads) return;
     auto first_written = [&](const Sequence& s) { return max(s.position, 0); };
     auto end_written = [&](const Sequence& s) { return min(s.position + s.rows, x.batch.capacity); };
-    const ItemPlace place = find_item(x.batch, blockIdx.x, [&](const Sequence& s) -> uint32_t {
+    const ItemPlace place = find_item(x.batch, item_of_block(), [&](const Sequence& s) -> uint32_t {
         const int p0 = first_written(s), p1 = end_written(s);
         return s.rows > 0 && p1 > p0 ? (p1 - 1) / 16 - p0 / 16 + 1 : 0;
     });
@@ -189,7 +189,7 @@ hipError_t launch(const WriteArgs& a, hipStream_t s) {
     // Blocks that new tokens touch: a sequence of n rows touches (n + 14) / 16 + 1 at most and n at most.
     const uint64_t tokens = a.batch.tokens;
     const uint64_t blocks = std::min<uint64_t>(tokens, tokens / 16 + 2 * std::min<uint64_t>(a.batch.count, tokens));
-    const dim3 grid((uint32_t)blocks, (a.cache.heads + kWaves - 1) / kWaves);
+    const dim3 grid = item_grid((uint32_t)blocks, (a.cache.heads + kWaves - 1) / kWaves);
     const uint32_t d = a.cache.head_dim;
     auto run = [&](auto ki, auto vi) {
         write_kernel<T, decltype(ki)::value, decltype(vi)::value><<<grid, kWaves * 64, 0, s>>>(a);

@@ -2,6 +2,7 @@
 #include "hv_fp8_cache.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "fp8_host.h"
@@ -92,6 +93,20 @@ hv_status check_rows(const char* what, const void* p, size_t element, uint64_t t
     return HV_OK;
 }
 
+hv_status check_attention(uint64_t sequences, uint64_t capacity, uint64_t tokens, uint64_t heads, uint64_t kv_heads,
+                          uint64_t head_dim) {
+    HV_LIMIT("sequences", sequences, kMaxCount);
+    HV_LIMIT("capacity", capacity, kMaxCapacity);
+    HV_LIMIT("kv_heads", kv_heads, kMaxHeads);
+    HV_TRY(check_head_dim(head_dim));
+    if (kv_heads == 0 || heads == 0 || heads % kv_heads != 0)
+        return fail(HV_ERR_INVALID_ARG, "heads = %llu is no multiple of the %llu key heads", (unsigned long long)heads,
+                    (unsigned long long)kv_heads);
+    HV_LIMIT("heads", heads, kMaxRows);
+    HV_LIMIT("tokens * heads", tokens, kMaxRows / heads);
+    return HV_OK;
+}
+
 hv::CacheArgs cache_args(const hv_fp8_cache& c) {
     const uint64_t blocks = c.page_tokens / 16;
     return {c.k_codes, c.k_scales, c.v_codes, c.v_scales, c.k_page, c.k_head, c.v_page, c.v_head,
@@ -121,6 +136,47 @@ hv_status hv_fp8_cache_write(const hv_fp8_cache* cache, const hv_fp8_batch* batc
     const hv::WriteArgs args = {cache_args(*cache), batch_args(*batch, cache->page_tokens, tokens), k, k_token, k_head, v,
                                 v_token, v_head};
     return done(hv::launch_fp8_cache_write(type, args, stream), "cache write kernel");
+}
+
+size_t hv_fp8_attention_workspace_bytes(uint64_t sequences, uint64_t capacity, uint64_t tokens, uint64_t heads,
+                                        uint64_t kv_heads, uint64_t head_dim, uint32_t window, uint32_t sinks) {
+    if (sequences == 0 || capacity == 0 || tokens == 0 ||
+        check_attention(sequences, capacity, tokens, heads, kv_heads, head_dim) != HV_OK)
+        return 0;
+    return round_up(hv::fp8_attention_plan(sequences, capacity, tokens, heads, kv_heads, head_dim, window, sinks).workspace);
+}
+
+hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* q,
+                           uint64_t q_token, uint64_t q_head, uint64_t tokens, uint64_t heads, float scale,
+                           uint32_t window, uint32_t sinks, void* out, uint64_t out_token, uint64_t out_head,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (type != HV_BF16 && type != HV_F16)
+        return fail(HV_ERR_INVALID_ARG, "element type %d is neither HV_BF16 nor HV_F16", (int)type);
+    HV_TRY(check_cache(cache));
+    HV_TRY(check_batch(batch, cache->page_tokens));
+    const uint64_t capacity = batch->columns * cache->page_tokens;
+    HV_TRY(check_attention(batch->count, capacity, tokens, heads, cache->kv_heads, cache->head_dim));
+    const float log2_scale = scale * 1.44269504088896341f;
+    if (!(scale > 0.0f) || !std::isfinite(log2_scale) || log2_scale < FLT_MIN)
+        return fail(HV_ERR_INVALID_ARG, "scale = %g is not positive and finite", (double)scale);
+    if (tokens == 0 || batch->count == 0) return HV_OK;
+    HV_TRY(check_rows("q", q, 2, tokens, q_token, heads, q_head, cache->head_dim));
+    HV_TRY(check_rows("out", out, 2, tokens, out_token, heads, out_head, cache->head_dim));
+    const hv::AttentionPlan plan = hv::fp8_attention_plan(batch->count, capacity, tokens, heads, cache->kv_heads,
+                                                          cache->head_dim, window, sinks);
+    HV_TRY(check_workspace(workspace, workspace_bytes, round_up(plan.workspace)));
+    constexpr uint32_t kFar = 1u << 30;  // more than any position
+    hv::AttentionArgs args = {};
+    args.cache = cache_args(*cache);
+    args.batch = batch_args(*batch, cache->page_tokens, tokens);
+    args.q = q, args.q_token = q_token, args.q_head = q_head;
+    args.out = out, args.out_token = out_token, args.out_head = out_head;
+    args.share = (uint32_t)(heads / cache->kv_heads);
+    args.scale = log2_scale;
+    args.window = (int)std::min(window, kFar);
+    args.sinks = (int)std::min(sinks, kFar);
+    args.parts = static_cast<float*>(workspace);
+    return done(hv::launch_fp8_attention(type, args, plan, stream), "attention kernels");
 }
 
 }  // extern "C"

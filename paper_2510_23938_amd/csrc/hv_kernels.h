@@ -317,4 +317,33 @@ struct WriteArgs {
 };
 hipError_t launch_fp8_cache_write(int type, const WriteArgs& a, hipStream_t s);
 
+struct AttentionArgs {
+    CacheArgs cache;
+    BatchArgs batch;
+    const void* q;
+    uint64_t q_token, q_head;
+    void* out;
+    uint64_t out_token, out_head;
+    uint32_t share;     // heads that share a key head
+    float scale;        // of scores, times log2(e)
+    int window, sinks;  // window 0: none
+    float* parts;       // workspace
+    uint32_t slots, least, parts_limit;  // of the plan, set by the launcher
+};
+// What a call is made by, from sizes alone; the kernels cut the keys by the lengths that they find.
+struct AttentionPlan {
+    uint32_t dims;   // of a head, rounded up to what the kernels are made for
+    uint32_t rows;   // of a workgroup: 16, 32 or 64 straight from memory, 128 through LDS
+    uint32_t jobs;   // workgroups, at most
+    uint32_t slots;  // shares that the keys' tiles are cut into where there are few rows; 0 where they never are
+    uint32_t least;  // tiles of a share, at least
+    uint32_t join;   // units that are cut, at most
+    uint32_t parts;  // that have sums to be joined, at most
+    uint64_t workspace;
+};
+// At least one sequence, token and page.
+AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t tokens, uint64_t heads, uint64_t kv_heads,
+                                 uint64_t head_dim, uint64_t window, uint64_t sinks);
+hipError_t launch_fp8_attention(int type, AttentionArgs a, const AttentionPlan& plan, hipStream_t s);
+
 }  // namespace hv

@@ -24,7 +24,7 @@ one root over them in the given order -- the paper's hierarchical roots) and
 loader does when a model fails its check), and the operators on matrices held
 in 8 bits (``include/hv_fp8.h``): ``hv_fp8_quantize``, ``hv_fp8_rms_norm``,
 ``hv_fp8_gated`` and ``hv_fp8_matmul``, and on a cache of keys and values in 8 bits
-(``include/hv_fp8_cache.h``): ``Fp8Cache`` and ``hv_fp8_cache_write``.
+(``include/hv_fp8_cache.h``): ``Fp8Cache``, ``hv_fp8_cache_write`` and ``hv_fp8_attention``.
 """
 from __future__ import annotations
 
@@ -72,7 +72,7 @@ EXPORTS = (
     "hv_verify_model",  # include/hv_plan.h
     "hv_fp8_quantize", "hv_fp8_rms_norm", "hv_fp8_gated", "hv_fp8_matmul_workspace_bytes",
     "hv_fp8_matmul",  # include/hv_fp8.h
-    "hv_fp8_cache_write",  # include/hv_fp8_cache.h
+    "hv_fp8_cache_write", "hv_fp8_attention_workspace_bytes", "hv_fp8_attention",  # include/hv_fp8_cache.h
 )
 
 
@@ -195,6 +195,9 @@ def _load():
         "hv_fp8_matmul": ([ctypes.c_int32, vp, u64, vp, vp, u64, vp, u64, u64, u64, vp, u64, vp, sz, vp],
                           ctypes.c_int),
         "hv_fp8_cache_write": ([vp, vp, ctypes.c_int32, vp, u64, u64, vp, u64, u64, u64, vp], ctypes.c_int),
+        "hv_fp8_attention_workspace_bytes": ([u64, u64, u64, u64, u64, u64, u32, u32], sz),
+        "hv_fp8_attention": ([vp, vp, ctypes.c_int32, vp, u64, u64, u64, u64, ctypes.c_float, u32, u32, vp, u64, u64, vp,
+                              sz, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -1480,3 +1483,50 @@ def hv_fp8_cache_write(cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, starts
     batch = _batch(starts, lengths, pages, index)
     _check(lib.hv_fp8_cache_write(cache._ref, ctypes.byref(batch), TYPES[k.dtype], k_ptr, k_token, k_head, v_ptr,
                                   v_token, v_head, k.shape[0], _current_stream(index)))
+
+
+_SIXTEEN_BITS = (torch.bfloat16, torch.float16)
+
+
+def _scratch(workspace, need: int, device):
+    """The buffer of a call that needs scratch, of the workspace given or of one of its own."""
+    if workspace is None:
+        workspace = Workspace(device)
+    elif workspace.device.type != "cuda" or workspace.device.index not in (None, device.index):
+        raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {device}")
+    return workspace.get(need) if need else None
+
+
+def hv_fp8_attention(q: torch.Tensor, cache: Fp8Cache, starts, lengths, pages, scale: float | None = None,
+                     window: int = 0, sinks: int = 0, out=None, workspace: Workspace | None = None):
+    """Attention of new tokens' queries ``q`` [tokens, heads, head_dim] (bfloat16 or float16) over the cache, which has
+    their keys and values already: [tokens, heads, head_dim].  ``starts``, ``lengths`` and ``pages`` as in
+    ``hv_fp8_cache_write``; ``heads`` is a multiple of the cache's, and neighbouring ones share a key head.  A token
+    sees those up to itself; with a ``window``, only the last that many of them and the first ``sinks``.  ``scale``
+    is 1 / sqrt(head_dim) unless given.  Rows of ``out`` that belong to no sequence are not written.  A ``workspace``
+    given has to outlive the HIP graphs that are captured with it."""
+    dev = cache.device
+    index = dev.index
+    if index != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_attention(q, cache, starts, lengths, pages, scale, window, sinks, out, workspace)
+    q_ptr, q_token, q_head = _heads(q, _SIXTEEN_BITS, "q", index)
+    tokens, heads, dim = q.shape
+    if dim != cache.head_dim or heads == 0 or heads % cache.kv_heads:
+        raise ValueError(f"q has shape {tuple(q.shape)}; the cache needs [tokens, a multiple of {cache.kv_heads}, "
+                         f"{cache.head_dim}]")
+    if not 0 <= window < 1 << 32 or not 0 <= sinks < 1 << 32:
+        raise ValueError(f"window = {window} and sinks = {sinks} must be from 0 to 2^32 - 1")
+    batch = _batch(starts, lengths, pages, index)
+    if out is None:
+        out = _like(q, q.dtype)
+        out_ptr, out_token, out_head = out.data_ptr(), heads * dim, dim
+    else:
+        out_ptr, out_token, out_head = _heads(out, (q.dtype,), "out", index, q.shape)
+    need = lib.hv_fp8_attention_workspace_bytes(batch.count, batch.columns * cache.page_tokens, tokens, heads,
+                                                cache.kv_heads, dim, window, sinks)
+    ws = _scratch(workspace, need, dev)
+    _check(lib.hv_fp8_attention(cache._ref, ctypes.byref(batch), TYPES[q.dtype], q_ptr, q_token, q_head, tokens, heads,
+                                dim ** -0.5 if scale is None else scale, window, sinks, out_ptr, out_token, out_head,
+                                ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(index)))
+    return out

@@ -1,0 +1,218 @@
+"""Attention over the 8-bit cache against its definition in 64 bits (oracle/fp8_cache.py), within what its arithmetic
+may lose (cache_bounds.py)."""
+import numpy as np
+import pytest
+import torch
+
+import cache_bounds
+from cache_cases import TYPES, Batch, on_gpu, random_cache
+from oracle import fp8_cache
+from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda")
+
+
+def framed(tokens, heads, dim, dtype, pad):
+    """([tokens, heads, dim] view, whole buffer): an output whose surroundings are known."""
+    raw = torch.full((tokens + 2, heads, dim + pad), 7.0, dtype=dtype, device=DEV)
+    return raw[1:-1, :, :dim], raw
+
+
+def check(rng, sequences, heads, kv_heads, dim, page, dtype="bf16", window=0, sinks=0, pad=0, scale=None, steep=1.0,
+          change=None, spread=3.0):
+    """One call against the oracle; ``change(cache, batch)`` alters both before it."""
+    batch = Batch(rng, sequences, page)
+    host = random_cache(rng, batch.pool, kv_heads, page, dim, spread)
+    if change:
+        change(host, batch)
+    gpu = on_gpu(host, pad * 16, pad * 32)
+    q = torch.from_numpy(rng.standard_normal((batch.tokens, heads, dim)) * steep).to(TYPES[dtype])
+    wide = torch.full((batch.tokens, heads, dim + pad), float("nan"), dtype=TYPES[dtype], device=DEV)
+    wide[:, :, :dim] = q.to(DEV)
+    out, raw = framed(batch.tokens, heads, dim, TYPES[dtype], pad)
+    ws = hv.Workspace(DEV)
+    hv.hv_fp8_attention(wide[:, :, :dim], gpu, *batch.gpu(), scale=scale, window=window, sinks=sinks, out=out, workspace=ws)
+    want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table,
+                               dim ** -0.5 if scale is None else scale, window, sinks)
+    cache_bounds.check(out.double().cpu().numpy(), want, dtype, int(batch.lengths.max(initial=0)))
+    frame = raw.clone()
+    frame[1:-1, :, :dim] = 7.0
+    assert bool((frame == 7.0).all())
+    none = np.isnan(want[0]).all((1, 2))
+    assert bool((out.cpu()[torch.from_numpy(none)] == 7.0).all())
+    again, _ = framed(batch.tokens, heads, dim, TYPES[dtype], pad)
+    hv.hv_fp8_attention(wide[:, :, :dim], gpu, *batch.gpu(), scale=scale, window=window, sinks=sinks, out=again, workspace=ws)
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))
+    return out, want
+
+
+def rng_of(*numbers):
+    return np.random.default_rng([abs(int(n)) for n in numbers])
+
+
+# one token: lengths around tiles, blocks and segments
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 500, 513, 777, 2000, 5000])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_token(dtype, length):
+    check(rng_of(length), [(1, length)], 8, 2, 128, 64, dtype)
+
+
+@pytest.mark.parametrize("dim", range(16, 257, 16))
+def test_each_width(dim):
+    rng = rng_of(dim)
+    check(rng, [(1, 100), (1, 1500)], 4, 2, dim, 32, "bf16")
+    check(rng, [(3, 70), (2, 900)], 12, 2, dim, 48, "f16", pad=1)
+    check(rng, [(9, 70), (30, 400)], 12, 2, dim, 48, "bf16", pad=1)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 5), (7, 1), (16, 1), (17, 1), (32, 2), (48, 1), (64, 1), (70, 1),
+                                            (130, 1), (24, 3), (300, 1)])
+def test_shared_heads(heads, kv_heads):
+    rng = rng_of(heads, kv_heads)
+    check(rng, [(1, 333)], heads, kv_heads, 64, 32)
+    check(rng, [(1, 40), (2, 130), (1, 1)], heads, kv_heads, 128, 64, "f16")
+
+
+@pytest.mark.parametrize("new", [1, 2, 3, 4, 5, 8, 16, 17, 31, 64, 65, 128, 130, 300])
+def test_new_tokens(new):
+    rng = rng_of(new)
+    check(rng, [(new, new)], 4, 2, 64, 16)
+    check(rng, [(new, new + 777), (max(new // 2, 1), new)], 4, 2, 128, 64, "f16")
+
+
+@pytest.mark.parametrize("page", [16, 48, 96, 128, 1024])
+def test_pages(page):
+    rng = rng_of(page)
+    check(rng, [(1, 700), (1, 33)], 4, 1, 128, page)
+    check(rng, [(40, 300), (25, 25)], 4, 1, 64, page)
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (63, 0), (64, 1), (65, 64), (100, 200), (500, 4),
+                                          (1 << 31, 5), (4, 1 << 31), ((1 << 32) - 1, (1 << 32) - 1)])
+def test_windows(window, sinks, new):
+    rng = rng_of(window, sinks, new)
+    check(rng, [(new, 1000), (new, new), (new, 230)], 4, 2, 64, 32, "bf16", window, sinks)
+    check(rng, [(new, 2500)], 8, 1, 128, 64, "f16", window, sinks, pad=8)
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_ragged_batches(new):
+    rng = rng_of(new, 9)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, 7, 90))]
+    check(rng, [(min(int(rng.integers(0, new + 1)), n), n) for n in lengths], 4, 2, 64, 16)
+
+
+def test_one_long_among_many():
+    """Segments of one sequence beside sequences that are not cut, for each kernel."""
+    rng = rng_of(10)
+    check(rng, [(1, 50)] * 20 + [(1, 20000)] + [(1, 3)] * 5, 8, 2, 64, 64)
+    check(rng, [(6, 50)] * 5 + [(6, 9000)] + [(6, 7)], 8, 2, 64, 64)
+    check(rng, [(40, 50)] * 5 + [(40, 4000)] + [(40, 77)], 8, 1, 64, 64)
+
+
+def test_mixed_prompts_and_tokens():
+    rng = rng_of(11)
+    check(rng, [(1, 400), (150, 150), (1, 90), (33, 500), (1, 1), (0, 9)], 4, 2, 64, 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("steep", [0.0, 1e-4, 8.0, 60.0])
+def test_flat_and_steep_scores(dtype, steep):
+    rng = rng_of(steep * 10)
+    check(rng, [(1, 600), (1, 40)], 8, 2, 128, 64, dtype, steep=steep)
+    check(rng, [(20, 300)], 8, 2, 128, 64, dtype, steep=steep)
+
+
+@pytest.mark.parametrize("scale", [1e-3, 1.0, 30.0])
+def test_scale(scale):
+    rng = rng_of(scale * 1000)
+    check(rng, [(1, 500), (1, 2)], 8, 2, 64, 64, scale=scale)
+    check(rng, [(50, 200)], 4, 2, 64, 64, "f16", scale=scale)
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_what_is_not_seen_changes_nothing(new, dtype):
+    """NaN codes and wild scales behind the last token, at pages of no sequence, and a page that does not exist."""
+    def change(cache, batch):
+        used = np.zeros((cache.pages, cache.page_tokens), dtype=bool)
+        for i, n in enumerate(batch.lengths):
+            for p in range(n):
+                used[batch.table[i, p // cache.page_tokens], p % cache.page_tokens] = True
+        for page in range(cache.pages):
+            for slot in np.flatnonzero(~used[page]):
+                cache.k[page, :, slot] = 0x7f
+                cache.v[page, :, slot // 16, :, slot % 16] = 0xff
+            for block in np.flatnonzero(~used[page].reshape(-1, 16).any(1)):
+                cache.ks[page, :, block], cache.vs[page, :, block] = np.nan, np.inf
+        batch.table[0, 1] = -1
+        batch.table[1, 0] = cache.pages
+
+    rng = rng_of(new)
+    check(rng, [(new, 200), (new, 130), (new, new + 1), (new, 1000)], 8, 2, 64, 32, dtype, change=change)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,heads", [(5, 4), (12, 4), (30, 4), (100, 2)])
+def test_nan_reaches_who_sees_it(new, heads, dtype):
+    """A NaN in a new token's value or key: the tokens before it and those whose window has passed it do not get it."""
+    def change(cache, batch):
+        n = int(batch.lengths[0])
+        for back, what in ((3, "v"), (new + 70, "v"), (1, "k")):
+            p = n - back
+            page, at = batch.table[0, p // cache.page_tokens], p % cache.page_tokens
+            if what == "v":
+                cache.v[page, 0, at // 16, 5, at % 16] = 0x7f
+            else:
+                cache.k[page, 1, at, 9] = 0xff
+
+    rng = rng_of(new)
+    for window in (0, 71 + new // 2):
+        _, want = check(rng, [(new, new + 300), (new, 40 + new)], heads, 2, 64, 16, dtype, window, 3, change=change)
+        assert np.isnan(want[0]).any() and not np.isnan(want[0]).all((0, 2)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_values_of_zero_and_scales_far_apart(dtype):
+    """A block of zeros has the smallest scale; its tokens' weights count all the same.  Half precision keeps blocks
+    whose scales are 2^-12 of the largest."""
+    def zeros(cache, batch):
+        for page in range(0, cache.pages, 2):
+            cache.v[page, :, 0], cache.vs[page, :, 0] = 0, 2.0 ** -126
+            cache.k[page, :, :16], cache.ks[page, :, 0] = 0, 2.0 ** -126
+
+    rng = rng_of(12)
+    for new in (1, 40):
+        check(rng, [(new, 500), (new, 60)], 8, 2, 64, 32, dtype, change=zeros)
+        check(rng, [(new, 500), (new, 60)], 8, 2, 64, 32, dtype, spread=6.0)
+
+
+def test_tokens_without_a_place():
+    """Tokens at negative positions see nothing and get zeros; rows of no sequence are not written."""
+    rng = rng_of(13)
+    for heads in (4, 40):
+        batch = Batch(rng, [(3, 10), (5, 50), (7, 7), (2, 90)], 16)
+        host = random_cache(rng, batch.pool, 2, 16, 64)
+        batch.lengths[:] = [1, 50, 0, 300]  # two, seven tokens ahead of the first; tokens past the table
+        starts = batch.starts + 2
+        starts[3] = starts[2]  # no rows: those of the third are left out with the fourth's first ones
+        q = torch.from_numpy(rng.standard_normal((25, heads, 64))).to(torch.bfloat16)
+        out = torch.full_like(q, 7.0, device=DEV)
+        args = [torch.from_numpy(a).to(DEV) for a in (starts, batch.lengths, batch.table)]
+        hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *args, out=out)
+        want = fp8_cache.attention(host, q.double().numpy(), starts, batch.lengths, batch.table, 0.125)
+        cache_bounds.check(out.double().cpu().numpy(), want, "bf16", 300)
+        none = torch.from_numpy(np.isnan(want[0]).all((1, 2)))
+        assert none.sum() >= 8 and bool((out.cpu()[none] == 7.0).all())
+        assert bool((out.cpu()[2:4] == 0).all())
+
+
+def test_an_empty_cache_gives_zeros():
+    q = torch.randn(3, 4, 64, device=DEV).to(torch.bfloat16)
+    for pages, columns in ((0, 2), (4, 0)):
+        cache = hv.Fp8Cache.empty(pages, 2, 16, 64)
+        args = [torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([0, 1, 3], [1, 2])]
+        out = hv.hv_fp8_attention(q, cache, *args, torch.zeros(2, columns, dtype=torch.int32, device=DEV))
+        assert bool((out == 0).all())
