@@ -125,6 +125,32 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
                         uint64_t ld_b, const float* b_scales, uint64_t m, uint64_t n, uint64_t k, void* c,
                         uint64_t ld_c, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* Scratch bytes hv_fp8_adapters needs; 0 where it needs none, and for sizes that it refuses. */
+size_t hv_fp8_adapters_workspace_bytes(uint64_t adapters, uint64_t rank, uint64_t m, uint64_t k);
+
+/* Low-rank adapters of many requests at once, beside a product of the same x:
+ *   out[t] = y[t] + factors[a] * (x[t] times the transpose of down[a]) times the transpose of up[a], a = index[t],
+ * and out[t] = y[t] for a token whose index is no adapter's number (-1, say).
+ * Products of codes and `down` are exact in 32 bits, their sums, the inner rows, the second product and
+ * the sum with y are in 32 bits, and out is rounded once, to the type.  A token's output depends on
+ * its own adapter alone.
+ *   type: of y and out; adapter_type: HV_BF16 or HV_F16, of down and up.
+ *   y, out: [m][n]; out may be y (same address and leading dimension).
+ *   x: [m][k] codes with scales by rows, as hv_fp8_matmul takes them.
+ *   down: [adapters][rank][k], up: [adapters][n][rank], both contiguous; adapters of a lower
+ *         rank have zeros in the place of the others.
+ *   factors: [adapters], NULL for ones; index: [m].
+ *   workspace: >= hv_fp8_adapters_workspace_bytes(...), 256-byte aligned; NULL where that is 0.
+ *              Scratch: calls that share one must share a stream.
+ * k = 0 or no adapters: out = y.
+ * Errors: HV_ERR_INVALID_ARG also for another adapter_type, a rank of 0 or above 1024, m or n above 2^27, m * n above
+ * 2^40, more than 2^31 - 1 adapters, or an out that is y with another leading dimension; HV_ERR_WORKSPACE for a
+ * missing, short or misaligned workspace. */
+hv_status hv_fp8_adapters(hv_type type, hv_type adapter_type, const void* y, uint64_t ld_y, const uint8_t* x,
+                          uint64_t ld_x, const float* x_scales, const void* down, const void* up, const float* factors,
+                          const int32_t* index, uint64_t adapters, uint64_t rank, uint64_t m, uint64_t n, uint64_t k,
+                          void* out, uint64_t ld_out, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

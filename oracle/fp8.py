@@ -79,3 +79,15 @@ def matmul(a, a_scales, b, b_scales):
     x = VALUES[a] * spread(a_scales, 1, *a.shape)
     y = VALUES[b] * spread(b_scales, GROUP, *b.shape)
     return x @ y.T, np.abs(x) @ np.abs(y).T
+
+
+def adapters(y, x, x_scales, down, up, index, factors):
+    """(out, size): y with each token's adapter in 64 bits, and the sum of its terms' magnitudes."""
+    out, size = np.array(y, dtype=np.float64), np.abs(np.asarray(y, dtype=np.float64))
+    numbers = VALUES[x] * spread(x_scales, 1, *x.shape)
+    for t, a in enumerate(index):
+        if 0 <= a < len(down):
+            inner = down[a] @ numbers[t]
+            out[t] += factors[a] * (up[a] @ inner)
+            size[t] += abs(factors[a]) * (np.abs(up[a]) @ (np.abs(down[a]) @ np.abs(numbers[t])))
+    return out, size

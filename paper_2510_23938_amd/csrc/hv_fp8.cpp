@@ -26,6 +26,17 @@ hv_status check_product(uint64_t m, uint64_t n, uint64_t k) {
     return HV_OK;
 }
 
+hv_status check_adapters(uint64_t adapters, uint64_t rank, uint64_t m, uint64_t n, uint64_t k) {
+    HV_TRY(check_product(m, n, k));
+    if (rank == 0 || rank > 1024) return fail(HV_ERR_INVALID_ARG, "rank = %llu is not from 1 to 1024", (unsigned long long)rank);
+    if (adapters >= (uint64_t)1 << 31)
+        return fail(HV_ERR_INVALID_ARG, "adapters = %llu exceeds the limit of 2^31 - 1", (unsigned long long)adapters);
+    if (m * n > (uint64_t)1 << 40)
+        return fail(HV_ERR_INVALID_ARG, "m = %llu, n = %llu: more than 2^40 outputs", (unsigned long long)m,
+                    (unsigned long long)n);
+    return HV_OK;
+}
+
 // A matrix operand that is read or written: present, at its element's alignment, rows apart.
 hv_status check_matrix(const char* what, const void* p, size_t element, uint64_t ld, uint64_t cols) {
     HV_TRY(check_pointer(what, p, element));
@@ -118,6 +129,39 @@ hv_status hv_fp8_matmul(hv_type type, const uint8_t* a, uint64_t ld_a, const flo
     HV_TRY(check_workspace(workspace, workspace_bytes, need));
     const hv::MatmulArgs args = {a, ld_a, a_scales, b, ld_b, b_scales, m, n, k, c, ld_c, workspace};
     return done(hv::launch_fp8_matmul(type, args, stream), "product kernel");
+}
+
+size_t hv_fp8_adapters_workspace_bytes(uint64_t adapters, uint64_t rank, uint64_t m, uint64_t k) {
+    if (check_adapters(adapters, rank, m, 1, k) != HV_OK || m == 0) return 0;
+    return round_up(hv::fp8_adapter_plan(m, k, rank, adapters).workspace);
+}
+
+hv_status hv_fp8_adapters(hv_type type, hv_type adapter_type, const void* y, uint64_t ld_y, const uint8_t* x,
+                          uint64_t ld_x, const float* x_scales, const void* down, const void* up, const float* factors,
+                          const int32_t* index, uint64_t adapters, uint64_t rank, uint64_t m, uint64_t n, uint64_t k,
+                          void* out, uint64_t ld_out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    HV_TRY(check_type(type));
+    if (adapter_type != HV_BF16 && adapter_type != HV_F16)
+        return fail(HV_ERR_INVALID_ARG, "adapter type %d is neither HV_BF16 nor HV_F16", (int)adapter_type);
+    HV_TRY(check_adapters(adapters, rank, m, n, k));
+    if (m == 0 || n == 0) return HV_OK;
+    HV_TRY(check_matrix("y", y, size_of(type), ld_y, n));
+    HV_TRY(check_matrix("out", out, size_of(type), ld_out, n));
+    if (out == y && ld_out != ld_y)
+        return fail(HV_ERR_INVALID_ARG, "out overlaps y with another leading dimension");
+    HV_TRY(check_pointer("index", index, sizeof(int32_t)));
+    if (adapters > 0 && k > 0) {
+        HV_TRY(check_matrix("x", x, 1, ld_x, k));
+        HV_TRY(check_pointer("x_scales", x_scales, sizeof(float)));
+        HV_TRY(check_pointer("down", down, 2));
+        HV_TRY(check_pointer("up", up, 2));
+        if (factors != nullptr) HV_TRY(check_pointer("factors", factors, sizeof(float)));
+    }
+    const hv::AdapterPlan plan = hv::fp8_adapter_plan(m, k, rank, adapters);
+    HV_TRY(check_workspace(workspace, workspace_bytes, round_up(plan.workspace)));
+    const hv::AdapterArgs args = {y,    ld_y, x, ld_x, x_scales, down, up,     factors,
+                                  index, adapters, rank, m, n, k, out, ld_out, static_cast<float*>(workspace)};
+    return done(hv::launch_fp8_adapters(type, adapter_type, args, plan, stream), "adapter kernels");
 }
 
 hv_status hv_fp8_matmul_launches(hv_type type, int aligned, uint64_t m, uint64_t n, uint64_t k, int* launches, int* kind,

@@ -288,6 +288,34 @@ int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n
 uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 
+// Adapters beside a product (fp8_adapters.hip); as in hv_fp8.h, checked.
+struct AdapterArgs {
+    const void* y;
+    uint64_t ld_y;
+    const uint8_t* x;
+    uint64_t ld_x;
+    const float* x_scales;
+    const void* down;
+    const void* up;
+    const float* factors;  // NULL: ones
+    const int32_t* index;
+    uint64_t adapters, rank, m, n, k;
+    void* out;
+    uint64_t ld_out;
+    float* inner;  // workspace
+    uint32_t distinct, splits, split_groups, tiles, inner_ld, token_rows;  // of the plan, set by the launcher
+};
+struct AdapterPlan {
+    uint32_t distinct;              // adapters among 16 tokens, at most
+    uint32_t splits, split_groups;  // parts of x's columns, and groups of 128 of each
+    uint32_t tiles;                 // of 16 tokens that a workgroup makes outputs of
+    uint32_t inner_ld;              // ranks, rounded up to whole vectors
+    uint32_t token_rows;            // of a launch's third dimension
+    uint64_t workspace;             // [splits][m][inner_ld] inner rows
+};
+AdapterPlan fp8_adapter_plan(uint64_t m, uint64_t k, uint64_t rank, uint64_t adapters);
+hipError_t launch_fp8_adapters(int type, int adapter_type, AdapterArgs a, const AdapterPlan& p, hipStream_t s);
+
 // The 8-bit cache (fp8_cache.hip, fp8_attention.hip); as in hv_fp8_cache.h, checked.
 struct CacheArgs {
     uint8_t* k_codes;

@@ -23,7 +23,7 @@ one root over them in the given order -- the paper's hierarchical roots) and
 ``verify`` (raises ``VerificationError`` on a mismatch, as the paper's
 loader does when a model fails its check), and the operators on matrices held
 in 8 bits (``include/hv_fp8.h``): ``hv_fp8_quantize``, ``hv_fp8_rms_norm``,
-``hv_fp8_gated`` and ``hv_fp8_matmul``, and on a cache of keys and values in 8 bits
+``hv_fp8_gated``, ``hv_fp8_matmul`` and ``hv_fp8_adapters``, and on a cache of keys and values in 8 bits
 (``include/hv_fp8_cache.h``): ``Fp8Cache``, ``hv_fp8_cache_write`` and ``hv_fp8_attention``.
 """
 from __future__ import annotations
@@ -71,7 +71,7 @@ EXPORTS = (
     "hv_plan_bytes", "hv_plan_init", "hv_plan_run", "hv_verify_model_workspace_bytes",
     "hv_verify_model",  # include/hv_plan.h
     "hv_fp8_quantize", "hv_fp8_rms_norm", "hv_fp8_gated", "hv_fp8_matmul_workspace_bytes",
-    "hv_fp8_matmul",  # include/hv_fp8.h
+    "hv_fp8_matmul", "hv_fp8_adapters_workspace_bytes", "hv_fp8_adapters",  # include/hv_fp8.h
     "hv_fp8_cache_write", "hv_fp8_attention_workspace_bytes", "hv_fp8_attention",  # include/hv_fp8_cache.h
 )
 
@@ -194,6 +194,9 @@ def _load():
         "hv_fp8_matmul_workspace_bytes": ([ctypes.c_int32, ctypes.c_int, u64, u64, u64], sz),
         "hv_fp8_matmul": ([ctypes.c_int32, vp, u64, vp, vp, u64, vp, u64, u64, u64, vp, u64, vp, sz, vp],
                           ctypes.c_int),
+        "hv_fp8_adapters_workspace_bytes": ([u64, u64, u64, u64], sz),
+        "hv_fp8_adapters": ([ctypes.c_int32, ctypes.c_int32, vp, u64, vp, u64, vp, vp, vp, vp, vp, u64, u64, u64, u64, u64,
+                             vp, u64, vp, sz, vp], ctypes.c_int),
         "hv_fp8_cache_write": ([vp, vp, ctypes.c_int32, vp, u64, u64, vp, u64, u64, u64, vp], ctypes.c_int),
         "hv_fp8_attention_workspace_bytes": ([u64, u64, u64, u64, u64, u64, u32, u32], sz),
         "hv_fp8_attention": ([vp, vp, ctypes.c_int32, vp, u64, u64, u64, u64, ctypes.c_float, u32, u32, vp, u64, u64, vp,
@@ -1177,10 +1180,8 @@ def _device_of(t, what: str):
     return t.device
 
 
-def _matrix(t, dtypes, what: str, index: int, shape=None) -> tuple:
-    """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
-    lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
-    what it is given, so anything it would overrun or misread is refused here."""
+def _on(t, dtypes, what: str, index: int):
+    """``t`` once it is known to be a tensor of one of the types on the call's GPU."""
     if not isinstance(t, torch.Tensor) or t.get_device() != index:  # half the time of comparing devices
         raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on cuda:{index}")
     if t.dtype not in dtypes:
@@ -1188,7 +1189,14 @@ def _matrix(t, dtypes, what: str, index: int, shape=None) -> tuple:
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient, and the 8-bit operators have no backward pass: call them "
                          "under torch.no_grad(), or on detached tensors")
-    s = t.shape
+    return t
+
+
+def _matrix(t, dtypes, what: str, index: int, shape=None) -> tuple:
+    """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
+    lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
+    what it is given, so anything it would overrun or misread is refused here."""
+    s = _on(t, dtypes, what, index).shape
     if shape is not None and s != shape:
         raise ValueError(f"{what} has shape {tuple(s)}; the call needs {tuple(shape)}")
     if len(s) == 0:
@@ -1212,6 +1220,8 @@ def _groups(n: int) -> int:
 
 
 _CODES = (torch.float8_e4m3fn,)
+_SIXTEEN_BITS = (torch.bfloat16, torch.float16)
+_I32 = (torch.int32,)
 _SCALES = (torch.float32,)
 
 
@@ -1311,6 +1321,13 @@ def hv_fp8_gated(gate: torch.Tensor, up: torch.Tensor, out=None, scales=None):
     return out, scales
 
 
+def _scratch(workspace, need: int, device):
+    """The buffer of a call that needs scratch, of the workspace given or of one of its own."""
+    if workspace is not None and (workspace.device.type != "cuda" or workspace.device.index not in (None, device.index)):
+        raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {device}")
+    return (workspace or Workspace(device)).get(need) if need else None
+
+
 def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
                   dtype=torch.bfloat16, out=None, workspace: Workspace | None = None):
     """a [..., k] times the transpose of b [n, k], both in codes, in ``dtype``: ``a_scales`` by rows
@@ -1339,18 +1356,63 @@ def hv_fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sc
         out_ptr, ld_out, _, _ = _matrix(out, (dtype,), "out", index, (*lead, n))
     aligned = not (ld_a % 16 or ld_b % 16 or a_ptr % 16 or b_ptr % 16)
     need = lib.hv_fp8_matmul_workspace_bytes(TYPES[dtype], aligned, m, n, k)
-    if workspace is not None and (workspace.device.type != "cuda" or workspace.device.index not in (None, index)):
-        raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {dev}")
-    ws = (workspace or Workspace(dev)).get(need) if need else None
+    ws = _scratch(workspace, need, dev)
     _check(lib.hv_fp8_matmul(TYPES[dtype], a_ptr, ld_a, sa_ptr, b_ptr, ld_b, sb_ptr, m, n, k, out_ptr, ld_out,
                              ws.data_ptr() if need else None, ws.numel() if need else 0, _current_stream(index)))
     return out
 
 
+def hv_fp8_adapters(y: torch.Tensor, x: torch.Tensor, x_scales: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
+                    index: torch.Tensor, factors=None, out=None, workspace: Workspace | None = None):
+    """Low-rank adapters of many requests beside a product: y[t] + factors[a] * (x[t] down[a]^T) up[a]^T for the
+    adapter a = index[t] of each token, and y[t] where index[t] is no adapter's number (-1).  ``y`` [..., n] is the
+    product's output, ``x`` [..., k] and ``x_scales`` its first operand in codes and scales by rows, ``down``
+    [adapters, rank, k] and ``up`` [adapters, n, rank] are bfloat16 or float16, ``index`` [...] int32,
+    ``factors`` [adapters] float32 (ones unless given).  ``out`` may be ``y``.  A ``workspace`` given has to outlive
+    the HIP graphs that are captured with it."""
+    dev = _device_of(y, "y")
+    gpu = dev.index
+    if gpu != _current_device():  # a stream's handle of zero is the current device's default stream
+        with torch.cuda.device(dev):
+            return hv_fp8_adapters(y, x, x_scales, down, up, index, factors, out, workspace)
+    y_ptr, ld_y, m, n = _matrix(y, TYPES, "y", gpu)
+    lead = y.shape[:-1]
+    m = lead.numel()
+    x_ptr, ld_x, _, k = _matrix(x, _CODES, "x", gpu)
+    if x.shape[:-1] != lead:
+        raise ValueError(f"x has shape {tuple(x.shape)}; the call needs {(*lead, k)}")
+    s_ptr = _scales(x_scales, "x_scales", gpu, (*lead, _groups(k)))
+    for t, what in ((down, "down"), (up, "up")):
+        _on(t, _SIXTEEN_BITS, what, gpu)
+        if t.dim() != 3 or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous, with three dimensions")
+    adapters, rank, _ = down.shape
+    if down.shape[2] != k or up.shape != (adapters, n, rank) or up.dtype != down.dtype:
+        raise ValueError(f"down {tuple(down.shape)} ({down.dtype}) and up {tuple(up.shape)} ({up.dtype}); the call needs "
+                         f"[adapters, rank, {k}] and [adapters, {n}, rank] of one type")
+    _on(index, _I32, "index", gpu)
+    if index.shape != lead or not index.is_contiguous():
+        raise ValueError(f"index must be contiguous, with shape {tuple(lead)}")
+    if factors is not None:
+        _on(factors, _SCALES, "factors", gpu)
+        if factors.shape != (adapters,) or not factors.is_contiguous():
+            raise ValueError(f"factors must be contiguous, with {adapters} elements")
+    if out is None:
+        out = _like(y, y.dtype)
+        out_ptr, ld_out = out.data_ptr(), n
+    else:
+        out_ptr, ld_out, _, _ = _matrix(out, (y.dtype,), "out", gpu, y.shape)
+    need = lib.hv_fp8_adapters_workspace_bytes(adapters, rank, m, k)
+    ws = _scratch(workspace, need, dev)
+    _check(lib.hv_fp8_adapters(TYPES[y.dtype], TYPES[down.dtype], y_ptr, ld_y, x_ptr, ld_x, s_ptr, down.data_ptr(),
+                               up.data_ptr(), factors.data_ptr() if factors is not None else None, index.data_ptr(),
+                               adapters, rank, m, n, k, out_ptr, ld_out, ws.data_ptr() if need else None,
+                               ws.numel() if need else 0, _current_stream(gpu)))
+    return out
+
+
 # --------------------------------------------------------------------------
 # the 8-bit cache of keys and values (include/hv_fp8_cache.h)
-
-_I32 = torch.int32
 
 
 def _strides(t) -> list:
@@ -1361,18 +1423,6 @@ def _strides(t) -> list:
             strides[i] = inner
         inner = strides[i] * max(t.shape[i], 1)
     return strides
-
-
-def _on(t, dtypes, what: str, index: int):
-    """``t`` once it is known to be a tensor of one of the types on the call's GPU."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != index:
-        raise ValueError(f"{what} is on {_device_of(t, what)}, but the call runs on cuda:{index}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} is {t.dtype}; expected one of {[str(d) for d in dtypes]}")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{what} requires a gradient, and the 8-bit operators have no backward pass: call them "
-                         "under torch.no_grad(), or on detached tensors")
-    return t
 
 
 def _heads(t, dtypes, what: str, index: int, shape=None) -> tuple:
@@ -1448,8 +1498,8 @@ class Fp8Cache:
 def _batch(starts, lengths, pages, index: int) -> hv_fp8_batch:
     """The description of a batch: ``starts`` [count + 1], ``lengths`` [count], ``pages`` [count, columns], int32."""
     for t, what in ((starts, "starts"), (lengths, "lengths"), (pages, "pages")):
-        if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype != _I32:
-            _on(t, (_I32,), what, index)
+        if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype != torch.int32:
+            _on(t, _I32, what, index)
     if lengths.dim() != 1 or not lengths.is_contiguous():
         raise ValueError("lengths must be one-dimensional and contiguous")
     count = lengths.shape[0]
@@ -1483,18 +1533,6 @@ def hv_fp8_cache_write(cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, starts
     batch = _batch(starts, lengths, pages, index)
     _check(lib.hv_fp8_cache_write(cache._ref, ctypes.byref(batch), TYPES[k.dtype], k_ptr, k_token, k_head, v_ptr,
                                   v_token, v_head, k.shape[0], _current_stream(index)))
-
-
-_SIXTEEN_BITS = (torch.bfloat16, torch.float16)
-
-
-def _scratch(workspace, need: int, device):
-    """The buffer of a call that needs scratch, of the workspace given or of one of its own."""
-    if workspace is None:
-        workspace = Workspace(device)
-    elif workspace.device.type != "cuda" or workspace.device.index not in (None, device.index):
-        raise ValueError(f"the workspace is on {workspace.device}, but the call runs on {device}")
-    return workspace.get(need) if need else None
 
 
 def hv_fp8_attention(q: torch.Tensor, cache: Fp8Cache, starts, lengths, pages, scale: float | None = None,
