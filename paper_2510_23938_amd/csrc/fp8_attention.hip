@@ -97,10 +97,14 @@ __device__ __forceinline__ int exponent_of(float power) { return (int)(__float_a
 
 // The high bit of each byte that is a NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7f) + 0x01010101) & 0x80808080; }
-// Zero codes in their place.
-__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+// Zero codes in their place; whether there were any.
+__device__ __forceinline__ uint32_t take_nan(uint32_t& w) {
     const uint32_t m = nan_bytes(w);
-    return w & ~(m | (m - (m >> 7)));
+    w &= ~(m | (m - (m >> 7)));
+    return m;
+}
+__device__ __forceinline__ uint32_t take_nan(uint4& w) {
+    return take_nan(w.x) | take_nan(w.y) | take_nan(w.z) | take_nan(w.w);
 }
 // The code of 1 in their place, and of zero elsewhere.
 __device__ __forceinline__ uint32_t ones_at_nan(uint32_t w) {
@@ -211,6 +215,20 @@ __device__ __forceinline__ bool block_seen(const AttentionArgs& x, int key, int 
     return key <= p_max && (!x.window || key + (int)kCacheBlock > p_min - x.window + 1 || key < x.sinks);
 }
 
+// `from`: the first key that a position's window has.
+__device__ __forceinline__ bool sees(const AttentionArgs& x, int position, int from, int key) {
+    return (key <= position) & ((key >= from) | (key < x.sinks));
+}
+__device__ __forceinline__ int window_from(const AttentionArgs& x, int position) {
+    return x.window ? position - x.window + 1 : 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Whether some of the positions p_min to p_max does not see some key of the tile from key0 on.
+__device__ __forceinline__ bool is_edge(const AttentionArgs& x, int key0, int p_min, int p_max) {
+    return key0 + kTile - 1 > p_min || (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
+}
+
 // The pages of a sequence's blocks of 16 tokens: a page and a block in it, or none.
 struct Places {
     const int32_t* table;
@@ -292,16 +310,17 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
     const uint32_t rows_all = job.sequence.rows * x.share, row0 = job.row_tile * R, rows = min(rows_all - row0, (uint32_t)R);
 
     Eight q[F][NC][2];
-    int pos[F];
+    int pos[F], from[F];
 #pragma unroll
     for (int fr = 0; fr < F; ++fr) {
         const uint32_t row = 16 * fr + n;
 #pragma unroll
         for (int c = 0; c < NC; ++c) load_query<T>(x, job, row0 + row, row0 + rows, 64 * c + 16 * g, q[fr][c]);
         pos[fr] = job.sequence.position + (int)((row0 + min(row, rows - 1)) / x.share);
+        from[fr] = window_from(x, pos[fr]);
     }
-    const int p_min = job.sequence.position + (int)(row0 / x.share);
-    const int p_max = job.sequence.position + (int)((row0 + rows - 1) / x.share);
+    const int p_min = uniform(job.sequence.position + (int)(row0 / x.share));
+    const int p_max = uniform(job.sequence.position + (int)((row0 + rows - 1) / x.share));
     const Range range = range_of(x, p_min, p_max);
     const int first = (int)((int64_t)range.count * job.segment / job.segments);
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
@@ -320,7 +339,8 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
 #pragma unroll
         for (int e = 0; e < ND; ++e) o[fr][e] = float4x{0, 0, 0, 0};
     }
-    int v_most = -126;  // kRelative: the exponent of the largest value scale met
+    int v_most = -126;      // kRelative: the exponent of the largest value scale met
+    bool poisoned = false;  // whether a tile that some row does not see all of had a NaN among its values
 
     uint4 k[4][NC], v[ND];
     float k_scale = 0.0f, v_scale = 0.0f;
@@ -391,24 +411,20 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
         const bool here = v_place >= 0;
         if (more) load_keys(k_next);
 
-        // whether some row does not see some key of the tile
-        const bool edge = key0 + kTile - 1 > p_min || __ballot(!here) != 0 ||
-                          (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
-        uint32_t seen[F];  // bit 4 f + r: the token 4 f + r of block g
+        const bool edge = is_edge(x, key0, p_min, p_max) || __ballot(!here) != 0;
         if (edge) {
+            asm volatile("");  // a branch: the comparisons are not made for other tiles
 #pragma unroll
-            for (int fr = 0; fr < F; ++fr) {
-                seen[fr] = 0;
+            for (int fr = 0; fr < F; ++fr)
 #pragma unroll
                 for (int f = 0; f < 4; ++f)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int key = key0 + 16 * (int)g + 4 * f + r;
-                        const bool sees = here && key <= pos[fr] && (!x.window || pos[fr] - key < x.window || key < x.sinks);
-                        seen[fr] |= (uint32_t)sees << (4 * f + r);
-                        s[fr][f][r] = sees ? s[fr][f][r] : -__builtin_inff();
-                    }
-            }
+                    for (int r = 0; r < 4; ++r)
+                        s[fr][f][r] = (here & sees(x, pos[fr], from[fr], key0 + 16 * (int)g + 4 * f + r)) ? s[fr][f][r] : -__builtin_inff();
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < ND; ++e) any |= take_nan(v[e]);
+            poisoned |= __ballot(any != 0) != 0;
         }
         float widen_by = v_power;
         if constexpr (W::kRelative) {
@@ -452,30 +468,6 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                     p[fr][f / 2][f % 2 * 4 + r] = (T)w;
                 }
         }
-        if (edge) {  // a NaN among the values reaches the rows that see it, and no others
-            uint32_t any = 0;
-#pragma unroll
-            for (int e = 0; e < ND; ++e) any |= nan_bytes(v[e].x) | nan_bytes(v[e].y) | nan_bytes(v[e].z) | nan_bytes(v[e].w);
-            if (__ballot(any != 0) != 0) {
-#pragma unroll
-                for (int fr = 0; fr < F; ++fr) {
-                    Eight sees[2];
-#pragma unroll
-                    for (int b = 0; b < 16; ++b) sees[b / 8][b % 8] = (T)(float)(seen[fr] >> b & 1);
-#pragma unroll
-                    for (int e = 0; e < ND; ++e) {
-                        float4x hits = {0, 0, 0, 0};
-                        hits = W::mul16(W::codes(ones_at_nan(v[e].x), ones_at_nan(v[e].y), 1.0f), sees[0], hits);
-                        hits = W::mul16(W::codes(ones_at_nan(v[e].z), ones_at_nan(v[e].w), 1.0f), sees[1], hits);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[fr][e][r] = hits[r] > 0 ? __builtin_nanf("") : o[fr][e][r];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < ND; ++e)
-                    v[e] = uint4{without_nan(v[e].x), without_nan(v[e].y), without_nan(v[e].z), without_nan(v[e].w)};
-            }
-        }
 #pragma unroll
         for (int e = 0; e < ND; ++e) {
             const Eight a = W::codes(v[e].x, v[e].y, widen_by), b = W::codes(v[e].z, v[e].w, widen_by);
@@ -490,6 +482,30 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
             load_values(v_next);
         }
         k_place = k_next, v_place = v_next, k_next = k_then, v_next = v_then;
+    }
+
+    if (poisoned) {  // a NaN among the values reaches the rows that see it, and no others
+        for (t = first + (int)wave; t < end; t += NW) {
+            const int key0 = range.tile(t) * kTile;
+            look(t, k_place, v_place);
+            if (!is_edge(x, key0, p_min, p_max) && __ballot(v_place < 0) == 0) continue;
+            load_values(v_place);
+#pragma unroll
+            for (int fr = 0; fr < F; ++fr) {
+                Eight seen[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    seen[i / 8][i % 8] = ((v_place >= 0) & sees(x, pos[fr], from[fr], key0 + 16 * (int)g + i)) ? (T)1.0f : (T)0.0f;
+#pragma unroll
+                for (int e = 0; e < ND; ++e) {
+                    float4x hits = {0, 0, 0, 0};
+                    hits = W::mul16(W::codes(ones_at_nan(v[e].x), ones_at_nan(v[e].y), 1.0f), seen[0], hits);
+                    hits = W::mul16(W::codes(ones_at_nan(v[e].z), ones_at_nan(v[e].w), 1.0f), seen[1], hits);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[fr][e][r] = hits[r] > 0 ? __builtin_nanf("") : o[fr][e][r];
+                }
+            }
+        }
     }
 
     // the waves' sums, to their common maximum
@@ -555,22 +571,31 @@ constexpr int kManyRows = 128;  // of a workgroup: four waves of 32
 
 // Where LDS has the 16-byte chunk of a key's row: an order in which eight lanes with neighbouring rows read
 // from different banks.
-template <int DP>
+template <int CP>
 __device__ __forceinline__ uint32_t chunk_place(uint32_t row, uint32_t chunk) {
-    return DP % 128 == 0 ? chunk ^ (row & 7) : chunk ^ (row >> 1 & 3);
+    return CP % 8 == 0 ? chunk ^ (row & 7) : chunk ^ (row >> 1 & 3);
+}
+
+template <typename P>
+__device__ __forceinline__ const P __attribute__((address_space(4))) * constant(const P* p) {
+    return (const P __attribute__((address_space(4)))*)(uintptr_t)p;
 }
 
 // Lane (row n = lane % 32, half h = lane / 32) of a wave has the weights of the blocks h and 2 + h of a tile.  For
 // that, fragment f of two has as its key m the token 4 (m / 8) + m % 4 of block 2 f + m / 4 % 2, and LDS holds the keys in
-// that order.
+// that order.  Each of the four waves brings one of a tile's blocks.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(AttentionArgs x) {
-    constexpr int R = kManyRows, NC = DP / 32, CP = DP / 16;
-    constexpr int KL = 64 * CP / 256, VL = 4 * DP / 256;  // 16-byte loads of a thread
+    constexpr int R = kManyRows, NC = DP / 32, NO = DP / 32;
+    constexpr int CP = DP / 16;  // 16-byte chunks of a key
+    constexpr int L = 16 * CP / 64;  // loads of a lane, of its wave's block of keys, and of values
     using W = Wide<T>;
     using Eight = typename W::Eight;
     __shared__ uint4 keys[2][64 * CP];
     __shared__ uint4 vals[2][4 * DP];
+    // a block's key scale in the softmax's exponents, or -1 where it is not in the cache, and its value scale
+    __shared__ float2 scales[2][4];
+    __shared__ int poisoned;  // whether a tile that some row does not see all of had a NaN among its values
     const Job job = find_job<R, false>(x, item_of_block());
     if (!job.found) return;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -585,221 +610,226 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
     for (int c = 0; c < NC; ++c) load_query<T>(x, job, my_row0 + n, row0 + rows, 32 * c + 16 * h, q[c]);
     const int base = job.sequence.position;
     const int pos = base + (int)(min(my_row0 + n, row0 + rows - 1) / x.share);
-    const int p_min = base + (int)(min(my_row0, row0 + rows - 1) / x.share);
-    const int p_max = base + (int)(min(my_row0 + my_rows - 1, row0 + rows - 1) / x.share);
-    const Range range = range_of(x, base + (int)(row0 / x.share), base + (int)((row0 + rows - 1) / x.share));
+    const int from = window_from(x, pos);
+    const int p_min = uniform(base + (int)(min(my_row0, row0 + rows - 1) / x.share));
+    const int p_max = uniform(idle ? -1 : base + (int)(min(my_row0 + my_rows - 1, row0 + rows - 1) / x.share));
+    const int all_min = uniform(base + (int)(row0 / x.share)), all_max = uniform(base + (int)((row0 + rows - 1) / x.share));
+    const Range range = range_of(x, all_min, all_max);
     const int first = (int)((int64_t)range.count * job.segment / job.segments);
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
 
-    const Places places(x, job.index);
+    const auto table = constant(x.batch.table + job.index * x.batch.ld_table);
+    const auto k_scales = constant(x.cache.k_scales), v_scales = constant(x.cache.v_scales);
     const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head;
     const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head;
-    const uint32_t block_bytes = 16 * dims;
 
-    float16x o[DP / 32];
+    // what a lane brings of its wave's block: chunks of keys, and dimensions of values
+    uint32_t k_from[L], k_to[L], v_from[L];
+    bool k_there[L], v_there[L];
 #pragma unroll
-    for (int e = 0; e < DP / 32; ++e)
+    for (int i = 0; i < L; ++i) {
+        const uint32_t id = 64 * i + lane, token = id / CP, chunk = id % CP;
+        const uint32_t row = 32 * (wave / 2) + token / 4 * 8 + wave % 2 * 4 + token % 4;
+        k_there[i] = 16 * chunk < dims;
+        k_from[i] = token * dims + 16 * chunk;
+        k_to[i] = row * CP + chunk_place<CP>(row, chunk);
+        v_there[i] = id < dims;
+        v_from[i] = 16 * id;
+    }
+    uint4 k_in[L], v_in[L];
+    float2 scale_in = {0, 0};
+    int page = 0;           // of the wave's block of the next tile to be loaded, negative for none
+    uint32_t in_page = 0;
+    auto look = [&](int t) {
+        const uint32_t block = (uint32_t)range.tile(t) * 4 + wave, column = page_column(block, x.cache.divide);
+        page = block < (uint32_t)x.batch.capacity / kCacheBlock ? table[column] : -1;
+        in_page = block - column * x.cache.page_blocks;
+    };
+    auto load = [&]() {
+        const bool here = (uint32_t)page < x.cache.pages;
+        const uint64_t place = here ? (uint32_t)page : 0, block = here ? in_page : 0;
+        const uint8_t* const k = k_head + place * x.cache.k_page + block * 16 * dims;
+        const uint8_t* const v = v_head + place * x.cache.v_page + block * 16 * dims;
+        scale_in = float2{-1.0f, 0.0f};
+        if (here) {
+            const uint64_t at = (place * x.cache.heads + job.head) * x.cache.page_blocks + block;
+            scale_in = float2{k_scales[at], v_scales[at]};
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                k_in[i] = uint4{0, 0, 0, 0};
+                if (k_there[i]) k_in[i] = *(const uint4*)(k + k_from[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                v_in[i] = uint4{0, 0, 0, 0};
+                if (v_there[i]) v_in[i] = *(const uint4*)(v + v_from[i]);
+            }
+            scale_in.x = fmaxf(cache_scale(scale_in.x) * x.scale, 0x1p-126f);
+            scale_in.y = cache_scale(scale_in.y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < L; ++i) k_in[i] = v_in[i] = uint4{0, 0, 0, 0};
+        }
+    };
+    auto hand_over = [&](int t) {
+        const int stage = (t - first) & 1;
+        if (is_edge(x, range.tile(t) * kTile, all_min, all_max)) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < L; ++i) any |= take_nan(v_in[i]);
+            if (any != 0) poisoned = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            keys[stage][k_to[i]] = k_in[i];
+            vals[stage][wave * DP + 64 * i + lane] = v_in[i];
+        }
+        if (lane == 0) scales[stage][wave] = scale_in;
+    };
+
+    float16x o[NO];
+#pragma unroll
+    for (int e = 0; e < NO; ++e)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[e][i] = 0.0f;
     float m = kNothing, l = 0.0f;
     int v_most = -126;
 
-    // of the tile that loads are under way for
-    uint4 k_in[KL], v_in[VL];
-    float k_scale[2], v_scale[2];
-    int64_t place[4];
-    auto look = [&](int t) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) place[j] = places.of((uint32_t)range.tile(t) * 4 + j);
-    };
-    auto load = [&]() {
-#pragma unroll
-        for (int i = 0; i < KL; ++i) {
-            const uint32_t id = i * 256 + threadIdx.x, row = id / CP, chunk = chunk_place<DP>(row, id % CP);
-            const uint32_t km = row % 32, token = 4 * (km / 8) + km % 4, j = 2 * (row / 32) + km / 4 % 2;
-            const int64_t p = j == 0 ? place[0] : j == 1 ? place[1] : j == 2 ? place[2] : place[3];
-            k_in[i] = uint4{0, 0, 0, 0};
-            if (p >= 0 && 16 * chunk < dims)
-                k_in[i] = *(const uint4*)(k_head + (p >> 32) * x.cache.k_page + (uint64_t)(uint32_t)p * block_bytes +
-                                          token * dims + 16 * chunk);
-        }
-#pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const uint32_t id = i * 256 + threadIdx.x, j = id / DP, d = id % DP;
-            const int64_t p = j == 0 ? place[0] : j == 1 ? place[1] : j == 2 ? place[2] : place[3];
-            v_in[i] = uint4{0, 0, 0, 0};
-            if (p >= 0 && d < dims)
-                v_in[i] = *(const uint4*)(v_head + (p >> 32) * x.cache.v_page + (uint64_t)(uint32_t)p * block_bytes + 16 * d);
-        }
+    // One tile for the wave's rows.
+    auto step = [&](int stage, int key0) {
+        const float2 scale[2] = {scales[stage][h], scales[stage][2 + h]};
+        const bool edge = is_edge(x, key0, p_min, p_max) || __ballot(fminf(scale[0].x, scale[1].x) < 0.0f) != 0;
+        const float to_log2[2] = {__builtin_fabsf(scale[0].x), __builtin_fabsf(scale[1].x)};
+        float16x s[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-            const int64_t p = h == 0 ? place[2 * f] : place[2 * f + 1];
-            k_scale[f] = v_scale[f] = 0.0f;
-            if (p >= 0) {
-                const uint64_t at = ((p >> 32) * x.cache.heads + job.head) * x.cache.page_blocks + (uint32_t)p;
-                k_scale[f] = x.cache.k_scales[at];
-                v_scale[f] = x.cache.v_scales[at];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[f][i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const uint4 w = keys[stage][(32 * f + n) * CP + chunk_place<CP>(n, 2 * c + h)];
+                s[f] = W::mul32(W::codes(w.x, w.y, 1.0f), q[c][0], s[f]);
+                s[f] = W::mul32(W::codes(w.z, w.w, 1.0f), q[c][1], s[f]);
             }
         }
-    };
-    auto hand_over = [&](int stage) {
-#pragma unroll
-        for (int i = 0; i < KL; ++i) keys[stage][i * 256 + threadIdx.x] = k_in[i];
-#pragma unroll
-        for (int i = 0; i < VL; ++i) vals[stage][i * 256 + threadIdx.x] = v_in[i];
-    };
-
-    if (first < end) {
-        look(first);
-        load();
-        hand_over(0);
-    }
-    __syncthreads();
-    for (int t = first; t < end; ++t) {
-        const int stage = (t - first) & 1, key0 = range.tile(t) * kTile;
-        float to_log2[2], v_power[2];
-        bool here[2];
-        bool gaps = false;
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            to_log2[f] = fmaxf(cache_scale(k_scale[f]) * x.scale, 0x1p-126f);
-            v_power[f] = cache_scale(v_scale[f]);
-            here[f] = (h == 0 ? place[2 * f] : place[2 * f + 1]) >= 0;
-            gaps |= place[2 * f] < 0 || place[2 * f + 1] < 0;
-        }
-        if (t + 1 < end) {
-            look(t + 1);
-            load();
-        }
-        if (!idle && key0 <= p_max) {
-            float16x s[2];
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[f][i] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const uint4 w = keys[stage][(32 * f + n) * CP + chunk_place<DP>(n, 2 * c + h)];
-                    s[f] = W::mul32(W::codes(w.x, w.y, 1.0f), q[c][0], s[f]);
-                    s[f] = W::mul32(W::codes(w.z, w.w, 1.0f), q[c][1], s[f]);
-                }
-            }
-            const bool edge = key0 + kTile - 1 > p_min || gaps ||
-                              (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
-            uint32_t seen[2];
-            if (edge) {
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    seen[f] = 0;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = key0 + 32 * f + 16 * (int)h + i;
-                        const bool sees = here[f] && key <= pos && (!x.window || pos - key < x.window || key < x.sinks);
-                        seen[f] |= (uint32_t)sees << i;
-                        s[f][i] = sees ? s[f][i] : -__builtin_inff();
-                    }
-                }
-            }
-            float widen_by[2] = {v_power[0], v_power[1]};
-            if constexpr (W::kRelative) {
-                int e[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f)
-                    e[f] = here[f] && block_seen(x, key0 + 32 * f + 16 * (int)h, p_min, p_max) ? exponent_of(v_power[f]) : -126;
-                int most = max(e[0], e[1]);
-                most = __builtin_amdgcn_readfirstlane(max(most, __shfl_xor(most, 32)));
-                if (most > v_most) {
-                    const float down = exp2_fast((float)(v_most - most));
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) o[d] *= down;
-                    v_most = most;
-                }
-                widen_by[0] = power_of(e[0] - v_most);
-                widen_by[1] = power_of(e[1] - v_most);
-            }
-            float top[2];
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                top[f] = s[f][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top[f] = fmaxf(top[f], s[f][i]);
-            }
-            float most = fmaxf(top[0] * to_log2[0], top[1] * to_log2[1]);
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (__ballot(most > m + kLazy) != 0) {
-                const float grown = fmaxf(m, most), down = exp2_fast(m - grown);
-                m = grown;
-                l *= down;
-#pragma unroll
-                for (int e = 0; e < DP / 32; ++e) o[e] *= down;
-            }
-            Eight p[2][2];
+        if (edge) {
+            asm volatile("");  // a branch: the comparisons are not made for other tiles
 #pragma unroll
             for (int f = 0; f < 2; ++f)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
-                    l += w;
-                    p[f][i / 8][i % 8] = (T)w;
-                }
-            bool mend = false;
-            if (edge) {  // a NaN among the values reaches the rows that see it, and no others
-                uint32_t any = 0;
+                for (int i = 0; i < 16; ++i)
+                    s[f][i] = ((scale[f].x > 0.0f) & sees(x, pos, from, key0 + 32 * f + 16 * (int)h + i)) ? s[f][i] : -__builtin_inff();
+        }
+        float top[2];
 #pragma unroll
-                for (int e = 0; e < DP / 32; ++e)
+        for (int f = 0; f < 2; ++f) {
+            top[f] = s[f][0];
 #pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
-                        any |= nan_bytes(w.x) | nan_bytes(w.y) | nan_bytes(w.z) | nan_bytes(w.w);
-                    }
-                mend = __ballot(any != 0) != 0;
-                if (mend) {
-                    Eight sees[2][2];
+            for (int i = 1; i < 16; ++i) top[f] = fmaxf(top[f], s[f][i]);
+        }
+        float most = fmaxf(top[0] * to_log2[0], top[1] * to_log2[1]);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (__ballot(most > m + kLazy) != 0) {
+            const float grown = fmaxf(m, most), down = exp2_fast(m - grown);
+            m = grown;
+            l *= down;
 #pragma unroll
-                    for (int f = 0; f < 2; ++f)
+            for (int e = 0; e < NO; ++e) o[e] *= down;
+        }
+        float widen_by[2] = {scale[0].y, scale[1].y};
+        if constexpr (W::kRelative) {
+            int e[2], largest = -126;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sees[f][i / 8][i % 8] = (T)(float)(seen[f] >> i & 1);
+            for (int f = 0; f < 2; ++f) {
+                const bool counts = scale[f].x > 0.0f && block_seen(x, key0 + 32 * f + 16 * (int)h, p_min, p_max);
+                e[f] = counts ? exponent_of(scale[f].y) : -126;
+                largest = max(largest, e[f]);
+            }
+            largest = __builtin_amdgcn_readfirstlane(max(largest, __shfl_xor(largest, 32)));
+            if (largest > v_most) {
+                const float down = exp2_fast((float)(v_most - largest));
 #pragma unroll
-                    for (int e = 0; e < DP / 32; ++e) {
-                        float16x hits;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) hits[i] = 0.0f;
-#pragma unroll
-                        for (int f = 0; f < 2; ++f) {
-                            const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
-                            hits = W::mul32(W::codes(ones_at_nan(w.x), ones_at_nan(w.y), 1.0f), sees[f][0], hits);
-                            hits = W::mul32(W::codes(ones_at_nan(w.z), ones_at_nan(w.w), 1.0f), sees[f][1], hits);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[e][i] = hits[i] > 0 ? __builtin_nanf("") : o[e][i];
-                    }
-                }
+                for (int d = 0; d < NO; ++d) o[d] *= down;
+                v_most = largest;
             }
 #pragma unroll
-            for (int e = 0; e < DP / 32; ++e)
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
-                    if (mend) w = uint4{without_nan(w.x), without_nan(w.y), without_nan(w.z), without_nan(w.w)};
-                    o[e] = W::mul32(W::codes(w.x, w.y, widen_by[f]), p[f][0], o[e]);
-                    o[e] = W::mul32(W::codes(w.z, w.w, widen_by[f]), p[f][1], o[e]);
-                }
+            for (int f = 0; f < 2; ++f) widen_by[f] = power_of(e[f] - v_most);
         }
-        if (t + 1 < end) hand_over(stage ^ 1);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            Eight p[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
+                l += w;
+                p[i / 8][i % 8] = (T)w;
+            }
+#pragma unroll
+            for (int e = 0; e < NO; ++e) {
+                const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
+                o[e] = W::mul32(W::codes(w.x, w.y, widen_by[f]), p[0], o[e]);
+                o[e] = W::mul32(W::codes(w.z, w.w, widen_by[f]), p[1], o[e]);
+            }
+        }
+    };
+
+    if (threadIdx.x == 0) poisoned = 0;
+    __syncthreads();
+    if (first < end) {
+        look(first);
+        load();
+        hand_over(first);
+        if (first + 1 < end) look(first + 1);
+    }
+    __syncthreads();
+    for (int t = first; t < end; ++t) {
+        const int key0 = range.tile(t) * kTile;
+        if (t + 1 < end) load();
+        if (t + 2 < end) look(t + 2);
+        if (key0 <= p_max) step((t - first) & 1, key0);
+        if (t + 1 < end) hand_over(t + 1);
         __syncthreads();
+    }
+    if (poisoned && !idle) {  // a NaN among the values reaches the rows that see it, and no others
+        const Places places(x, job.index);
+        for (int t = first; t < end; ++t) {
+            const int key0 = range.tile(t) * kTile;
+            if (!is_edge(x, key0, all_min, all_max)) continue;
+            for (int f = 0; f < 2; ++f) {
+                const int64_t place = places.of((uint32_t)key0 / kCacheBlock + 2 * f + h);
+                Eight seen[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    seen[i / 8][i % 8] = ((place >= 0) & sees(x, pos, from, key0 + 32 * f + 16 * (int)h + i)) ? (T)1.0f : (T)0.0f;
+                const uint8_t* const block = v_head + (place < 0 ? 0 : (place >> 32) * x.cache.v_page +
+                                                                          (uint64_t)(uint32_t)place * 16 * dims);
+#pragma unroll
+                for (int e = 0; e < NO; ++e) {
+                    uint4 w = {0, 0, 0, 0};
+                    if (place >= 0 && 32 * e + n < dims) w = *(const uint4*)(block + 16 * (32 * e + n));
+                    float16x hits;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) hits[i] = 0.0f;
+                    hits = W::mul32(W::codes(ones_at_nan(w.x), ones_at_nan(w.y), 1.0f), seen[0], hits);
+                    hits = W::mul32(W::codes(ones_at_nan(w.z), ones_at_nan(w.w), 1.0f), seen[1], hits);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[e][i] = hits[i] > 0 ? __builtin_nanf("") : o[e][i];
+                }
+            }
+        }
     }
 
     l += __shfl_xor(l, 32);
     if constexpr (W::kRelative) {
 #pragma unroll
-        for (int e = 0; e < DP / 32; ++e) o[e] *= power_of(v_most);
+        for (int e = 0; e < NO; ++e) o[e] *= power_of(v_most);
     }
     if (idle || n >= my_rows) return;
     const uint32_t row = wave * 32 + n;
     if (job.segments > 1 && h == 0) part_weights<R, DP>(x, job.part)[row] = float2{m, l};
     const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int e = 0; e < DP / 32; ++e)
+    for (int e = 0; e < NO; ++e)
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
             const uint32_t d = 32 * e + 8 * a + 4 * h;
