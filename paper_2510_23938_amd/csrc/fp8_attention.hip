@@ -38,6 +38,8 @@ using float4x = __attribute__((ext_vector_type(4))) float;
 using float16x = __attribute__((ext_vector_type(16))) float;
 
 constexpr int kTile = 64;         // keys of a step
+constexpr int kMatrix = 0x8, kDsRead = 0x100;  // instruction groups of the scheduler
+constexpr int kWaitAll = 0;       // s_waitcnt: nothing outstanding
 constexpr float kLazy = 8.0f;     // binary orders that a row's weights may grow before its sums are scaled
 constexpr float kNothing = -FLT_MAX;  // the maximum of a row that has seen nothing
 
@@ -60,6 +62,13 @@ struct Wide<__bf16> {
         const bf16x2 a = two<false>(lo, scale), b = two<true>(lo, scale), c = two<false>(hi, scale), d = two<true>(hi, scale);
         return Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
+    // sum and the weights of eight, as they are after their rounding
+    static __device__ __forceinline__ float add(Eight p, float sum) {
+        const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[i], p[i + 1]}, one, sum, false);
+        return sum;
+    }
     static __device__ __forceinline__ float4x mul16(Eight a, Eight b, float4x c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
@@ -80,6 +89,12 @@ struct Wide<_Float16> {
     static __device__ __forceinline__ Eight codes(uint32_t lo, uint32_t hi, float scale) {
         const f16x2 a = two<false>(lo, scale), b = two<true>(lo, scale), c = two<false>(hi, scale), d = two<true>(hi, scale);
         return Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+    static __device__ __forceinline__ float add(Eight p, float sum) {
+        const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2(f16x2{p[i], p[i + 1]}, one, sum, false);
+        return sum;
     }
     static __device__ __forceinline__ float4x mul16(Eight a, Eight b, float4x c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -569,16 +584,11 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
 
 constexpr int kManyRows = 128;  // of a workgroup: four waves of 32
 
-// Where LDS has the 16-byte chunk of a key's row: an order in which eight lanes with neighbouring rows read
-// from different banks.
+// Where LDS has the chunk of 8 elements of a key's row, of CP of them: 16 lanes that read the same chunk of
+// neighbouring rows find them in different banks (16 times 16 bytes before banks repeat).
 template <int CP>
 __device__ __forceinline__ uint32_t chunk_place(uint32_t row, uint32_t chunk) {
-    return CP % 8 == 0 ? chunk ^ (row & 7) : chunk ^ (row >> 1 & 3);
-}
-
-template <typename P>
-__device__ __forceinline__ const P __attribute__((address_space(4))) * constant(const P* p) {
-    return (const P __attribute__((address_space(4)))*)(uintptr_t)p;
+    return CP % 16 == 0 ? chunk ^ (row & 15) : CP % 8 == 0 ? chunk ^ (row >> 1 & 7) : chunk ^ (row >> 2 & 3);
 }
 
 // Lane (row n = lane % 32, half h = lane / 32) of a wave has the weights of the blocks h and 2 + h of a tile.  For
@@ -587,12 +597,12 @@ __device__ __forceinline__ const P __attribute__((address_space(4))) * constant(
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(AttentionArgs x) {
     constexpr int R = kManyRows, NC = DP / 32, NO = DP / 32;
-    constexpr int CP = DP / 16;  // 16-byte chunks of a key
-    constexpr int L = 16 * CP / 64;  // loads of a lane, of its wave's block of keys, and of values
+    constexpr int CP = DP / 8;  // chunks of 8 elements of a key
+    constexpr int L = (DP + 63) / 64;  // loads of a lane, of its wave's block of keys, and of values
     using W = Wide<T>;
     using Eight = typename W::Eight;
-    __shared__ uint4 keys[2][64 * CP];
-    __shared__ uint4 vals[2][4 * DP];
+    __shared__ Eight keys[2][64 * CP];
+    __shared__ Eight vals[2][4 * 2 * DP];  // [block][its halves of 8 tokens][dimension]
     // a block's key scale in the softmax's exponents, or -1 where it is not in the cache, and its value scale
     __shared__ float2 scales[2][4];
     __shared__ int poisoned;  // whether a tile that some row does not see all of had a NaN among its values
@@ -618,58 +628,66 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
     const int first = (int)((int64_t)range.count * job.segment / job.segments);
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
 
-    const auto table = constant(x.batch.table + job.index * x.batch.ld_table);
-    const auto k_scales = constant(x.cache.k_scales), v_scales = constant(x.cache.v_scales);
+    // Loads at an address that is the same for all lanes go by the vector unit all the same: one by the scalar unit
+    // comes back out of order with LDS reads, which would all wait for it.
+    uint32_t nothing = 0;
+    asm volatile("" : "+v"(nothing));
+    const int32_t* const table = x.batch.table + job.index * x.batch.ld_table + nothing;
+    const float* const k_scales = x.cache.k_scales + nothing;
+    const float* const v_scales = x.cache.v_scales + nothing;
     const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head;
     const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head;
 
     // what a lane brings of its wave's block: chunks of keys, and dimensions of values
-    uint32_t k_from[L], k_to[L], v_from[L];
+    uint32_t k_from[L], k_to[L][2];
     bool k_there[L], v_there[L];
+    uint4 k_in[L], v_in[L];  // zeros stay where no dimensions are
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-        const uint32_t id = 64 * i + lane, token = id / CP, chunk = id % CP;
+        const uint32_t id = 64 * i + lane, token = id / (DP / 16), d = id % (DP / 16) * 16;
         const uint32_t row = 32 * (wave / 2) + token / 4 * 8 + wave % 2 * 4 + token % 4;
-        k_there[i] = 16 * chunk < dims;
-        k_from[i] = token * dims + 16 * chunk;
-        k_to[i] = row * CP + chunk_place<CP>(row, chunk);
+        k_there[i] = id < DP && d < dims;
+        k_from[i] = token * dims + d;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) k_to[i][e] = row * CP + chunk_place<CP>(row, d / 8 + e);
         v_there[i] = id < dims;
-        v_from[i] = 16 * id;
+        k_in[i] = v_in[i] = uint4{0, 0, 0, 0};
     }
-    uint4 k_in[L], v_in[L];
     float2 scale_in = {0, 0};
-    int page = 0;           // of the wave's block of the next tile to be loaded, negative for none
+    // The wave's block of the next tile to be loaded: its page, negative for none, and its place there.  The table's
+    // last column stands in for those behind it, so that nothing has to be decided before the load.
+    int next_page = -1;
     uint32_t in_page = 0;
+    bool listed = false;
+    bool here = false;      // whether the block under way is in the cache
+    const uint32_t last_block = (uint32_t)x.batch.capacity / kCacheBlock - 1;
     auto look = [&](int t) {
-        const uint32_t block = (uint32_t)range.tile(t) * 4 + wave, column = page_column(block, x.cache.divide);
-        page = block < (uint32_t)x.batch.capacity / kCacheBlock ? table[column] : -1;
-        in_page = block - column * x.cache.page_blocks;
+        const uint32_t block = (uint32_t)range.tile(t) * 4 + wave, inside = min(block, last_block);
+        const uint32_t column = page_column(inside, x.cache.divide);
+        listed = block == inside;
+        in_page = inside - column * x.cache.page_blocks;
+        next_page = table[column];
     };
-    auto load = [&]() {
-        const bool here = (uint32_t)page < x.cache.pages;
-        const uint64_t place = here ? (uint32_t)page : 0, block = here ? in_page : 0;
-        const uint8_t* const k = k_head + place * x.cache.k_page + block * 16 * dims;
-        const uint8_t* const v = v_head + place * x.cache.v_page + block * 16 * dims;
-        scale_in = float2{-1.0f, 0.0f};
-        if (here) {
-            const uint64_t at = (place * x.cache.heads + job.head) * x.cache.page_blocks + block;
-            scale_in = float2{k_scales[at], v_scales[at]};
+    // Loads tile t - 1, whose place is known by now, and looks for that of tile t.
+    auto load = [&](int t) {
+        const uint32_t page = (uint32_t)uniform(next_page), in_page_now = in_page;
+        here = listed & (page < x.cache.pages);
+        if (t < end) look(t);
+        if (!here) {  // its keys are not seen; no NaN stays among its values
 #pragma unroll
-            for (int i = 0; i < L; ++i) {
-                k_in[i] = uint4{0, 0, 0, 0};
-                if (k_there[i]) k_in[i] = *(const uint4*)(k + k_from[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                v_in[i] = uint4{0, 0, 0, 0};
-                if (v_there[i]) v_in[i] = *(const uint4*)(v + v_from[i]);
-            }
-            scale_in.x = fmaxf(cache_scale(scale_in.x) * x.scale, 0x1p-126f);
-            scale_in.y = cache_scale(scale_in.y);
-        } else {
-#pragma unroll
-            for (int i = 0; i < L; ++i) k_in[i] = v_in[i] = uint4{0, 0, 0, 0};
+            for (int i = 0; i < L; ++i) v_in[i] = uint4{0, 0, 0, 0};
+            return;
         }
+        const uint8_t* const k = k_head + page * x.cache.k_page + in_page_now * (16 * dims);
+        const uint8_t* const v = v_head + page * x.cache.v_page + in_page_now * (16 * dims);
+        const uint64_t at = ((uint64_t)page * x.cache.heads + job.head) * x.cache.page_blocks + in_page_now;
+        scale_in = float2{k_scales[at], v_scales[at]};
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            if (k_there[i]) k_in[i] = *(const uint4*)(k + k_from[i]);
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            if (v_there[i]) v_in[i] = *(const uint4*)(v + (64 * i + lane) * 16);
     };
     auto hand_over = [&](int t) {
         const int stage = (t - first) & 1;
@@ -679,12 +697,18 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
             for (int i = 0; i < L; ++i) any |= take_nan(v_in[i]);
             if (any != 0) poisoned = 1;
         }
+        const float widen_by = W::kRelative ? 1.0f : cache_scale(scale_in.y);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            keys[stage][k_to[i]] = k_in[i];
-            vals[stage][wave * DP + 64 * i + lane] = v_in[i];
+            if (64 * (i + 1) > DP && 64 * i + lane >= DP) break;
+            keys[stage][k_to[i][0]] = W::codes(k_in[i].x, k_in[i].y, 1.0f);
+            keys[stage][k_to[i][1]] = W::codes(k_in[i].z, k_in[i].w, 1.0f);
+            vals[stage][(2 * wave) * DP + 64 * i + lane] = W::codes(v_in[i].x, v_in[i].y, widen_by);
+            vals[stage][(2 * wave + 1) * DP + 64 * i + lane] = W::codes(v_in[i].z, v_in[i].w, widen_by);
         }
-        if (lane == 0) scales[stage][wave] = scale_in;
+        if (lane == 0)
+            scales[stage][wave] = float2{here ? fmaxf(cache_scale(scale_in.x) * x.scale, 0x1p-126f) : -1.0f,
+                                         cache_scale(scale_in.y)};
     };
 
     float16x o[NO];
@@ -702,16 +726,34 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
         const float to_log2[2] = {__builtin_fabsf(scale[0].x), __builtin_fabsf(scale[1].x)};
         float16x s[2];
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
+        for (int f = 0; f < 2; ++f)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[f][i] = 0.0f;
+        Eight k[2 * NC][2];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const uint4 w = keys[stage][(32 * f + n) * CP + chunk_place<CP>(n, 2 * c + h)];
-                s[f] = W::mul32(W::codes(w.x, w.y, 1.0f), q[c][0], s[f]);
-                s[f] = W::mul32(W::codes(w.z, w.w, 1.0f), q[c][1], s[f]);
-            }
+        for (int c = 0; c < 2 * NC; ++c)
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+                k[c][f] = keys[stage][(32 * f + n) * CP + chunk_place<CP>(n, 4 * (c / 2) + 2 * h + c % 2)];
+#pragma unroll
+        for (int c = 0; c < 2 * NC; ++c)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) s[f] = W::mul32(k[c][f], q[c / 2][c % 2], s[f]);
+        // eight reads ahead of the products, which the compiler would make two at a time
+        constexpr int kAhead = std::min(8, 4 * NC);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < (4 * NC - kAhead) / 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead, 0);
+        Eight v[2][NO];  // of the half block at work, and the next one
+        auto read_values = [&](int i) {  // half a of the wave's block f, i = 2 f + a
+#pragma unroll
+            for (int e = 0; e < NO; ++e) v[i % 2][e] = vals[stage][(4 * (i / 2) + 2 * h + i % 2) * DP + 32 * e + n];
+        };
+        read_values(0);
         if (edge) {
             asm volatile("");  // a branch: the comparisons are not made for other tiles
 #pragma unroll
@@ -736,7 +778,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
 #pragma unroll
             for (int e = 0; e < NO; ++e) o[e] *= down;
         }
-        float widen_by[2] = {scale[0].y, scale[1].y};
+        float down[2] = {1.0f, 1.0f};  // of values, relative to the largest scale
         if constexpr (W::kRelative) {
             int e[2], largest = -126;
 #pragma unroll
@@ -747,28 +789,32 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
             }
             largest = __builtin_amdgcn_readfirstlane(max(largest, __shfl_xor(largest, 32)));
             if (largest > v_most) {
-                const float down = exp2_fast((float)(v_most - largest));
+                const float by = exp2_fast((float)(v_most - largest));
 #pragma unroll
-                for (int d = 0; d < NO; ++d) o[d] *= down;
+                for (int d = 0; d < NO; ++d) o[d] *= by;
                 v_most = largest;
             }
 #pragma unroll
-            for (int f = 0; f < 2; ++f) widen_by[f] = power_of(e[f] - v_most);
+            for (int f = 0; f < 2; ++f) down[f] = power_of(e[f] - v_most);
         }
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             Eight p[2];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
-                l += w;
+                float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
+                if constexpr (W::kRelative) {
+                    l += w;
+                    w *= down[f];
+                }
                 p[i / 8][i % 8] = (T)w;
             }
 #pragma unroll
-            for (int e = 0; e < NO; ++e) {
-                const uint4 w = vals[stage][(2 * f + h) * DP + 32 * e + n];
-                o[e] = W::mul32(W::codes(w.x, w.y, widen_by[f]), p[0], o[e]);
-                o[e] = W::mul32(W::codes(w.z, w.w, widen_by[f]), p[1], o[e]);
+            for (int a = 0; a < 2; ++a) {
+                if (2 * f + a < 3) read_values(2 * f + a + 1);
+                if constexpr (!W::kRelative) l = W::add(p[a], l);
+#pragma unroll
+                for (int e = 0; e < NO; ++e) o[e] = W::mul32(v[a][e], p[a], o[e]);
             }
         }
     };
@@ -777,15 +823,16 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
     __syncthreads();
     if (first < end) {
         look(first);
-        load();
+        load(first + 1);
         hand_over(first);
-        if (first + 1 < end) look(first + 1);
     }
+    // The queries have arrived, as far as the compiler knows too: it would wait for them within the loop, and by that
+    // for the tile that was asked for last.
+    __builtin_amdgcn_s_waitcnt(kWaitAll);
     __syncthreads();
     for (int t = first; t < end; ++t) {
         const int key0 = range.tile(t) * kTile;
-        if (t + 1 < end) load();
-        if (t + 2 < end) look(t + 2);
+        if (t + 1 < end) load(t + 2);
         if (key0 <= p_max) step((t - first) & 1, key0);
         if (t + 1 < end) hand_over(t + 1);
         __syncthreads();
@@ -846,7 +893,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
 // the parts' sums joined, in order: workgroups of 16 rows of each unit that is cut
 
 template <typename T, int DP, int R>
-__global__ void __launch_bounds__(4 * DP) join_attention(AttentionArgs x) {
+__global__ void __launch_bounds__(16 * (DP / 4)) join_attention(AttentionArgs x) {
     constexpr uint32_t kLanes = DP / 4;
     const Job job = find_job<R, true>(x, blockIdx.x);
     if (!job.found) return;
@@ -876,7 +923,7 @@ template <typename T, int DP, int R, typename Main>
 hipError_t run(const AttentionArgs& a, const AttentionPlan& plan, uint32_t threads, Main main, hipStream_t s) {
     main<<<item_grid(plan.jobs), threads, 0, s>>>(a);
     if (plan.join == 0) return hipGetLastError();
-    join_attention<T, DP, R><<<dim3(plan.join, R / 16), 4 * DP, 0, s>>>(a);
+    join_attention<T, DP, R><<<dim3(plan.join, R / 16), 16 * (DP / 4), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -899,6 +946,7 @@ template <typename T>
 hipError_t launch(const AttentionArgs& a, const AttentionPlan& plan, hipStream_t s) {
     switch (plan.dims) {
         case 64: return launch<T, 64>(a, plan, s);
+        case 96: return run<T, 96, kManyRows>(a, plan, 256, tile_attention<T, 96>, s);
         case 128: return launch<T, 128>(a, plan, s);
         case 192: return launch<T, 192>(a, plan, s);
         default: return launch<T, 256>(a, plan, s);
@@ -914,6 +962,7 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     const uint64_t share = heads / kv_heads;
     const uint64_t rows = (tokens + sequences - 1) / sequences * share;  // of a sequence, on the average
     plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && plan.dims <= 128 ? 64 : kManyRows;
+    if (plan.rows == kManyRows && head_dim > 64 && head_dim <= 96) plan.dims = 96;
     const uint64_t units = kv_heads * (tokens * share / plan.rows + std::min(sequences, tokens));
     // tiles that one row tile may see at most
     const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
