@@ -27,6 +27,18 @@ __device__ __forceinline__ uint32_t page_column(uint32_t block, uint64_t divide)
     return (uint32_t)(block * divide >> 40);
 }
 
+// With l the bits of d - 1, mul = floor(2^(31 + l) / d) + 1 is off by at most 2^l / 2^(31 + l) of itself: too little to
+// change the quotient of a number below 2^31.
+inline Divider divider(uint32_t d) {
+    if (d <= 1) return {0, 0};
+    uint32_t l = 1;
+    while (((uint64_t)1 << l) < d) ++l;
+    return {(uint32_t)(((uint64_t)1 << (31 + l)) / d + 1), l - 1};
+}
+__device__ __forceinline__ uint32_t divided(uint32_t n, Divider d) {
+    return d.mul != 0 ? __umulhi(n, d.mul) >> d.shift : n;
+}
+
 // Sum of x over this lane and those before it, by DPP: within rows of 16, then across them.
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
     auto moved = [](uint32_t v, auto ctrl, auto rows) {

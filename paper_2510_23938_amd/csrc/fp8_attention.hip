@@ -145,16 +145,6 @@ __device__ __forceinline__ Range range_of(const AttentionArgs& x, int p_min, int
     return {lo_tile, sinks, sinks + max(hi_tile - lo_tile + 1, 0)};
 }
 
-// How a sequence's work is cut: row tiles of R rows, and the segments of each one's keys.
-struct Cut {
-    uint32_t units, segments;  // row tiles times key heads
-};
-
-template <int R>
-__device__ __forceinline__ uint32_t units_of(const AttentionArgs& x, const Sequence& s) {
-    return ((uint32_t)s.rows * x.share + R - 1) / R * x.cache.heads;
-}
-
 // A workgroup's work.
 struct Job {
     bool found;
@@ -162,28 +152,33 @@ struct Job {
     uint32_t index, row_tile, head, segment, segments, part;
 };
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) v += __shfl_xor((unsigned long long)v, step);
-    return v;
-}
+// A sequence's work: row tiles of R rows for each key head, and the key tiles that each of them may see.
+struct Work {
+    Sequence sequence;
+    uint32_t row_tiles, units, tiles;
+};
 
-// Tiles of a segment: an even share of all for each of `slots` workgroups, at least `least`.
 template <int R>
-__device__ __forceinline__ uint32_t segment_tiles(const AttentionArgs& x, uint32_t lane) {
-    if (x.slots == 0) return ~0u;
-    uint64_t total = 0;
-    for (uint32_t i = lane; i < x.batch.count; i += 64) {
-        const Sequence s = sequence_at(x.batch, i);
-        if (s.rows > 0)
-            total += (uint64_t)units_of<R>(x, s) * range_of(x, s.position, s.position + s.rows - 1).count;
-    }
-    const uint64_t share = (wave_sum(total) + x.slots - 1) / x.slots;
-    return (uint32_t)min(max(share, (uint64_t)x.least), (uint64_t)1 << 30);
+__device__ __forceinline__ Work work_at(const AttentionArgs& x, uint32_t i) {
+    Work w = {{0, 0, 0}, 0, 0, 0};
+    if (i >= x.batch.count) return w;
+    w.sequence = sequence_at(x.batch, i);
+    if (w.sequence.rows == 0) return w;
+    w.row_tiles = ((uint32_t)w.sequence.rows * x.share + R - 1) / R;
+    w.units = w.row_tiles * x.cache.heads;
+    w.tiles = (uint32_t)range_of(x, w.sequence.position, w.sequence.position + w.sequence.rows - 1).count;
+    return w;
 }
 
-// Segments of a sequence's row tiles.  A quarter of a segment more does not cost another, so the tiles of all that are
-// cut in two or more take fewer than 2 * slots: s < c / share + 3/4 with c / share > 5/4.
+// All lanes' units times tiles; each is cut at 2^40, which is more than any call has.
+__device__ __forceinline__ uint64_t total_tiles(const Work& w) {
+    const uint64_t mine = min((uint64_t)w.units * w.tiles, (uint64_t)1 << 40);
+    const uint32_t low = wave_scan((uint32_t)mine & 0xffff), high = wave_scan((uint32_t)(mine >> 16));
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, 63) << 16) + (uint32_t)__builtin_amdgcn_readlane(low, 63);
+}
+
+// Segments of a unit's tiles, `share` of them each.  A quarter of a segment more does not cost another, so the
+// segments of all units that are cut in two or more are fewer than 2 * slots: s < c / share + 3/4 with c / share > 5/4.
 __device__ __forceinline__ uint32_t segments_of(uint32_t tiles, uint32_t share) {
     const uint32_t slack = share / 4;
     return tiles <= share + slack ? 1 : (tiles - slack + share - 1) / share;
@@ -193,36 +188,43 @@ __device__ __forceinline__ uint32_t segments_of(uint32_t tiles, uint32_t share) 
 template <int R, bool kJoin>
 __device__ __forceinline__ Job find_job(const AttentionArgs& x, uint32_t item) {
     const uint32_t lane = lane_id();
-    const uint32_t share = segment_tiles<R>(x, lane);
+    Work w = work_at<R>(x, lane);
+    // tiles of a segment: an even share of all for each of the slots, at least `least`
+    uint32_t share = ~0u;
+    if (x.log2_slots != 0) {
+        uint64_t total = total_tiles(w);
+        for (uint32_t base = 64; base < x.batch.count; base += 64) total += total_tiles(work_at<R>(x, base + lane));
+        const uint64_t even = (total + ((uint64_t)1 << x.log2_slots) - 1) >> x.log2_slots;
+        share = (uint32_t)min(max(even, (uint64_t)x.least), (uint64_t)1 << 30);
+    }
     uint32_t part = 0;
-    for (uint32_t base = 0; base < x.batch.count; base += 64) {
-        const Sequence s = base + lane < x.batch.count ? sequence_at(x.batch, base + lane) : Sequence{0, 0, 0};
-        uint32_t units = 0, segments = 1;
-        if (s.rows > 0) {
-            units = units_of<R>(x, s);
-            segments = segments_of(range_of(x, s.position, s.position + s.rows - 1).count, share);
-        }
-        const uint32_t parts = segments > 1 ? units * segments : 0;
-        const uint32_t items = kJoin ? (segments > 1 ? units : 0) : units * segments;
+    for (uint32_t base = 0;;) {
+        const bool cut = w.tiles > share + share / 4 && share != ~0u;
+        uint32_t segments = 1;
+        if (__ballot(cut) != 0) segments = cut ? segments_of(w.tiles, share) : 1;
+        const uint32_t parts = cut ? w.units * segments : 0;
+        const uint32_t items = kJoin ? (cut ? w.units : 0) : w.units * segments;
         const uint32_t upto = wave_scan(items), parts_upto = wave_scan(parts);
         const uint64_t at = __ballot(upto > item);
         if (at != 0) {
             const uint32_t l = __builtin_ctzll(at);
             const uint32_t within = item - __builtin_amdgcn_readlane(upto - items, l);
             const uint32_t n = __builtin_amdgcn_readlane(segments, l), all = __builtin_amdgcn_readlane(items, l);
-            const uint32_t unit = kJoin ? within : within / n, segment = kJoin ? 0 : within - unit * n;
-            const uint32_t row_tiles = __builtin_amdgcn_readlane(units, l) / x.cache.heads;
-            const uint32_t row_tile = unit / x.cache.heads;
+            const uint32_t unit = kJoin || n == 1 ? within : within / n, segment = kJoin ? 0 : within - unit * n;
+            const uint32_t row_tiles = __builtin_amdgcn_readlane(w.row_tiles, l);
+            const uint32_t row_tile = divided(unit, x.by_heads);
             part += __builtin_amdgcn_readlane(parts_upto - parts, l) + unit * n + segment;
             // the last rows, which see the most, first; what a batch without order may ask for stays in bounds
             const bool ok = within < all && (n == 1 || part < x.parts_limit);
-            return {ok, sequence_in_lane(s, l), base + l, row_tiles - 1 - row_tile, unit - row_tile * x.cache.heads,
+            return {ok, sequence_in_lane(w.sequence, l), base + l, row_tiles - 1 - row_tile, unit - row_tile * x.cache.heads,
                     segment, n, part};
         }
         item -= __builtin_amdgcn_readlane(upto, 63);
         part += __builtin_amdgcn_readlane(parts_upto, 63);
+        base += 64;
+        if (base >= x.batch.count) return {};
+        w = work_at<R>(x, base + lane);
     }
-    return {};
 }
 
 // Whether some of the positions p_min to p_max sees some of the block's 16 tokens from `key` on.
@@ -283,7 +285,7 @@ __device__ __forceinline__ void store_four(T* p, float4x v) {
 
 template <typename T>
 __device__ __forceinline__ T* out_at(const AttentionArgs& x, const Job& job, uint32_t row) {
-    const uint32_t token = row / x.share;
+    const uint32_t token = divided(row, x.by_share);
     return (T*)x.out + (uint64_t)(job.sequence.row + token) * x.out_token +
            (uint64_t)(job.head * x.share + (row - token * x.share)) * x.out_head;
 }
@@ -294,7 +296,7 @@ __device__ __forceinline__ void load_query(const AttentionArgs& x, const Job& jo
                                            typename Wide<T>::Eight (&q)[2]) {
     uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < rows && d < x.cache.head_dim) {
-        const uint32_t token = row / x.share;
+        const uint32_t token = divided(row, x.by_share);
         const T* const p = (const T*)x.q + (uint64_t)(job.sequence.row + token) * x.q_token +
                            (uint64_t)(job.head * x.share + (row - token * x.share)) * x.q_head + d;
         __builtin_memcpy(zero, p, 32);
@@ -331,11 +333,11 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
         const uint32_t row = 16 * fr + n;
 #pragma unroll
         for (int c = 0; c < NC; ++c) load_query<T>(x, job, row0 + row, row0 + rows, 64 * c + 16 * g, q[fr][c]);
-        pos[fr] = job.sequence.position + (int)((row0 + min(row, rows - 1)) / x.share);
+        pos[fr] = job.sequence.position + (int)divided(row0 + min(row, rows - 1), x.by_share);
         from[fr] = window_from(x, pos[fr]);
     }
-    const int p_min = uniform(job.sequence.position + (int)(row0 / x.share));
-    const int p_max = uniform(job.sequence.position + (int)((row0 + rows - 1) / x.share));
+    const int p_min = uniform(job.sequence.position + (int)divided(row0, x.by_share));
+    const int p_max = uniform(job.sequence.position + (int)divided(row0 + rows - 1, x.by_share));
     const Range range = range_of(x, p_min, p_max);
     const int first = (int)((int64_t)range.count * job.segment / job.segments);
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
@@ -619,11 +621,11 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
 #pragma unroll
     for (int c = 0; c < NC; ++c) load_query<T>(x, job, my_row0 + n, row0 + rows, 32 * c + 16 * h, q[c]);
     const int base = job.sequence.position;
-    const int pos = base + (int)(min(my_row0 + n, row0 + rows - 1) / x.share);
+    const int pos = base + (int)divided(min(my_row0 + n, row0 + rows - 1), x.by_share);
     const int from = window_from(x, pos);
-    const int p_min = uniform(base + (int)(min(my_row0, row0 + rows - 1) / x.share));
-    const int p_max = uniform(idle ? -1 : base + (int)(min(my_row0 + my_rows - 1, row0 + rows - 1) / x.share));
-    const int all_min = uniform(base + (int)(row0 / x.share)), all_max = uniform(base + (int)((row0 + rows - 1) / x.share));
+    const int p_min = uniform(base + (int)divided(min(my_row0, row0 + rows - 1), x.by_share));
+    const int p_max = uniform(idle ? -1 : base + (int)divided(min(my_row0 + my_rows - 1, row0 + rows - 1), x.by_share));
+    const int all_min = uniform(base + (int)divided(row0, x.by_share)), all_max = uniform(base + (int)divided(row0 + rows - 1, x.by_share));
     const Range range = range_of(x, all_min, all_max);
     const int first = (int)((int64_t)range.count * job.segment / job.segments);
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
@@ -901,17 +903,34 @@ __global__ void __launch_bounds__(16 * (DP / 4)) join_attention(AttentionArgs x)
     const uint32_t row = blockIdx.y * 16 + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
     if (row >= rows || d >= x.cache.head_dim) return;
     const float2* const weights = part_weights<R, DP>(x, job.part) + row;
-    float most = kNothing;
-    for (uint32_t i = 0; i < job.segments; ++i) most = fmaxf(most, weights[i * R].x);
-    float total = 0.0f;
-    float4x sum = {0, 0, 0, 0};
     const float* const from = part_rows<R, DP>(x, job.part) + row * DP + d;
-#pragma unroll 4
-    for (uint32_t i = 0; i < job.segments; ++i) {
-        const float2 w = weights[i * R];
-        const float up = exp2_fast(w.x - most);
-        total += up * w.y;
-        sum += up * *(const float4x*)(from + (uint64_t)i * R * DP);
+    // Eight parts at a time are on their way; the maximum of those so far scales the sums, as in a segment.
+    constexpr uint32_t kStep = 8;
+    float most = kNothing, total = 0.0f;
+    float4x sum = {0, 0, 0, 0};
+    for (uint32_t i = 0; i < job.segments; i += kStep) {
+        float2 w[kStep];
+        float4x part[kStep];
+#pragma unroll
+        for (uint32_t k = 0; k < kStep; ++k) {
+            const uint32_t at = min(i + k, job.segments - 1);
+            w[k] = weights[at * R];
+            part[k] = *(const float4x*)(from + (uint64_t)at * R * DP);
+            if (i + k >= job.segments) w[k] = float2{kNothing, 0.0f};
+        }
+        float top = most;
+#pragma unroll
+        for (uint32_t k = 0; k < kStep; ++k) top = fmaxf(top, w[k].x);
+        const float down = exp2_fast(most - top);
+        total *= down;
+        sum *= down;
+        most = top;
+#pragma unroll
+        for (uint32_t k = 0; k < kStep; ++k) {
+            const float up = i + k < job.segments ? exp2_fast(w[k].x - top) : 0.0f;
+            total += up * w[k].y;
+            sum += i + k < job.segments ? up * part[k] : float4x{0, 0, 0, 0};
+        }
     }
     store_four(out_at<T>(x, job, job.row_tile * R + row) + d, total == 0.0f ? float4x{0, 0, 0, 0} : sum / total);
 }
@@ -968,17 +987,20 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
     const uint64_t tiles = (reach + kTile - 1) / kTile;
     plan.least = 8;
-    plan.slots = 512;
-    if (tiles <= plan.least + plan.least / 4) plan.slots = 0;  // segments_of gives one
-    plan.jobs = (uint32_t)(units + 2 * plan.slots);
-    plan.join = (uint32_t)std::min<uint64_t>(units, plan.slots);
-    plan.parts = 2 * plan.slots;
+    plan.log2_slots = 9;
+    if (tiles <= plan.least + plan.least / 4) plan.log2_slots = 0;  // no unit is cut
+    const uint32_t slots = plan.log2_slots ? 1u << plan.log2_slots : 0;
+    plan.jobs = (uint32_t)(units + 2 * slots);
+    plan.join = (uint32_t)std::min<uint64_t>(units, slots);
+    plan.parts = 2 * slots;
     plan.workspace = (uint64_t)plan.parts * plan.rows * (plan.dims + 2) * sizeof(float);
     return plan;
 }
 
 hipError_t launch_fp8_attention(int type, AttentionArgs a, const AttentionPlan& plan, hipStream_t s) {
-    a.slots = plan.slots;
+    a.log2_slots = plan.log2_slots;
+    a.by_share = divider(a.share);
+    a.by_heads = divider(a.cache.heads);
     a.least = plan.least;
     a.parts_limit = plan.parts;
     return type == kTypeBf16 ? launch<__bf16>(a, plan, s) : launch<_Float16>(a, plan, s);

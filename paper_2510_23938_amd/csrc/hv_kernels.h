@@ -345,6 +345,10 @@ struct WriteArgs {
 };
 hipError_t launch_fp8_cache_write(int type, const WriteArgs& a, hipStream_t s);
 
+// n / d for n below 2^31 as (n * mul >> 32) >> shift; mul 0: n.
+struct Divider {
+    uint32_t mul, shift;
+};
 struct AttentionArgs {
     CacheArgs cache;
     BatchArgs batch;
@@ -356,14 +360,15 @@ struct AttentionArgs {
     float scale;        // of scores, times log2(e)
     int window, sinks;  // window 0: none
     float* parts;       // workspace
-    uint32_t slots, least, parts_limit;  // of the plan, set by the launcher
+    uint32_t log2_slots, least, parts_limit;  // of the plan, set by the launcher as the next are
+    Divider by_share, by_heads;
 };
 // What a call is made by, from sizes alone; the kernels cut the keys by the lengths that they find.
 struct AttentionPlan {
     uint32_t dims;   // of a head, rounded up to what the kernels are made for
     uint32_t rows;   // of a workgroup: 16, 32 or 64 straight from memory, 128 through LDS
     uint32_t jobs;   // workgroups, at most
-    uint32_t slots;  // shares that the keys' tiles are cut into where there are few rows; 0 where they never are
+    uint32_t log2_slots;  // of the shares that the keys' tiles are cut into; 0 where they never are
     uint32_t least;  // tiles of a share, at least
     uint32_t join;   // units that are cut, at most
     uint32_t parts;  // that have sums to be joined, at most
