@@ -288,6 +288,10 @@ int fp8_matmul_parts(bool wide, bool aligned, bool tiles, uint64_t m, uint64_t n
 uint64_t fp8_matmul_workspace(bool wide, bool aligned, uint64_t m, uint64_t n, uint64_t k);
 hipError_t launch_fp8_matmul(int type, const MatmulArgs& a, hipStream_t s);
 
+// n / d for n below 2^31 as (n * mul >> 32) >> shift; mul 0: n.
+struct Divider {
+    uint32_t mul, shift;
+};
 // Adapters beside a product (fp8_adapters.hip); as in hv_fp8.h, checked.
 struct AdapterArgs {
     const void* y;
@@ -303,12 +307,15 @@ struct AdapterArgs {
     void* out;
     uint64_t ld_out;
     float* inner;  // workspace
-    uint32_t distinct, splits, split_groups, tiles, inner_ld, token_rows;  // of the plan, set by the launcher
+    uint32_t distinct, splits, split_groups, inner_ld, token_rows;  // of the plan, set by the launcher as the next are
+    uint32_t column_blocks;  // of the second kernel's workgroups
+    Divider by_column_blocks, by_vectors;
 };
 struct AdapterPlan {
     uint32_t distinct;              // adapters among 16 tokens, at most
     uint32_t splits, split_groups;  // parts of x's columns, and groups of 128 of each
-    uint32_t tiles;                 // of 16 tokens that a workgroup makes outputs of
+    uint32_t down_waves;            // of a workgroup of the first kernel
+    bool many;                      // tokens: a wave of the second kernel takes 16 of them, not one of their adapters
     uint32_t inner_ld;              // ranks, rounded up to whole vectors
     uint32_t token_rows;            // of a launch's third dimension
     uint64_t workspace;             // [splits][m][inner_ld] inner rows
@@ -345,10 +352,6 @@ struct WriteArgs {
 };
 hipError_t launch_fp8_cache_write(int type, const WriteArgs& a, hipStream_t s);
 
-// n / d for n below 2^31 as (n * mul >> 32) >> shift; mul 0: n.
-struct Divider {
-    uint32_t mul, shift;
-};
 struct AttentionArgs {
     CacheArgs cache;
     BatchArgs batch;
