@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) up_kernel(AdapterArgs x) {
     const uint64_t col = col0 + 16 * g;  // of the lane's 16 outputs
     const int there = col < x.n ? (int)min(x.n - col, (uint64_t)16) : 0;
     const uint32_t vectors = x.inner_ld / 4;  // of an inner row
-    if constexpr (kInLds) {
+    auto stage = [&]() {
         const uint32_t rows = (uint32_t)min(x.m - tile * kTokens, (uint64_t)kTokens);
         for (uint32_t i = threadIdx.x; i < rows * vectors; i += blockDim.x) {
             const uint32_t row = divided(i, x.by_vectors), r = (i - row * vectors) * 4;
@@ -270,31 +270,40 @@ __global__ void __launch_bounds__(kMostWaves * 64) up_kernel(AdapterArgs x) {
             *(float4x*)&staged[row * pitch + r] = t;
         }
         __syncthreads();
-    }
-    uint32_t job = 0;
-    uint64_t left = __ballot(token < x.m);
-    while (left != 0) {
-        const uint32_t a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-        left &= ~__ballot(mine == a);
-        const bool my_turn = job == wave;
-        job = job + 1 == waves ? 0 : job + 1;
-        if (!my_turn) continue;
-        const bool keep = mine == a && token < x.m;
-        auto make = [&](auto all) {
-            constexpr bool kAll = decltype(all)::value;
+    };
+    auto make = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        bool to_stage = kInLds;  // every wave does it once, the loads of its first product under way
+        uint32_t job = 0;
+        uint64_t left = __ballot(token < x.m);
+        while (left != 0) {
+            const uint32_t a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+            left &= ~__ballot(mine == a);
+            const bool my_turn = job == wave;
+            job = job + 1 == waves ? 0 : job + 1;
+            if (!my_turn) continue;
+            const bool keep = mine == a && token < x.m;
+            const W* const up = (const W*)x.up + (a == kNone ? 0 : (uint64_t)a * x.n * x.rank);
             T y[16];
+            W w[4][4];
             const T* const row = (const T*)x.y + min(token, x.m - 1) * x.ld_y;
             load_some<kAll>(row + col, there, row + x.n - 1, y);
+            if (a != kNone) {
+#pragma unroll
+                for (int f = 0; f < 4; ++f) load_up<kQuads>(x, up, column_of(col0, n, f), 4 * g, w[f]);
+            }
+            if (to_stage) stage();
+            to_stage = false;
             float4x out[4];
 #pragma unroll
             for (int f = 0; f < 4; ++f) out[f] = float4x{0, 0, 0, 0};
             if (a != kNone) {
-                const W* const up = (const W*)x.up + (uint64_t)a * x.n * x.rank;
                 for (uint32_t r0 = 0; r0 < x.rank; r0 += 16) {
                     const uint32_t r = r0 + 4 * g;
-                    W w[4][4];
+                    if (r0 > 0) {
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) load_up<kQuads>(x, up, column_of(col0, n, f), r, w[f]);
+                        for (int f = 0; f < 4; ++f) load_up<kQuads>(x, up, column_of(col0, n, f), r, w[f]);
+                    }
                     float4x t = {0, 0, 0, 0};
                     if (keep && r < x.rank)
                         t = kInLds ? *(const float4x*)&staged[n * pitch + r] : inner_row(x, token, r, a);
@@ -302,12 +311,13 @@ __global__ void __launch_bounds__(kMostWaves * 64) up_kernel(AdapterArgs x) {
                 }
             }
             if (keep) add_and_store<kAll>(y, out, (T*)x.out + token * x.ld_out + col, there);
-        };
-        if (col0 + 64 <= x.n)
-            make(std::true_type{});
-        else
-            make(std::false_type{});
-    }
+        }
+        if (to_stage) stage();
+    };
+    if (col0 + 64 <= x.n)
+        make(std::true_type{});
+    else
+        make(std::false_type{});
 }
 
 // The same for many tokens: a wave takes one tile of 16 tokens and 128 columns, all the adapters among them in turn.
