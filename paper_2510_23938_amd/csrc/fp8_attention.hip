@@ -138,7 +138,7 @@ struct Range {
 
 __device__ __forceinline__ Range range_of(const AttentionArgs& x, int p_min, int p_max) {
     const int hi = min(p_max, x.batch.capacity - 1);
-    if (hi < 0) return {0, 0, 0};
+    if (hi < 0 || x.cache.pages == 0) return {0, 0, 0};
     const int lo = x.window ? max(p_min - x.window + 1, 0) : 0;
     const int lo_tile = lo / kTile, hi_tile = hi / kTile;
     const int sinks = x.window ? min(lo_tile, (min(x.sinks, hi + 1) + kTile - 1) / kTile) : 0;
@@ -246,21 +246,27 @@ __device__ __forceinline__ bool is_edge(const AttentionArgs& x, int key0, int p_
     return key0 + kTile - 1 > p_min || (x.window && p_max - key0 >= x.window && key0 + kTile > x.sinks);
 }
 
-// The pages of a sequence's blocks of 16 tokens: a page and a block in it, or none.
+// The pages of a sequence's blocks of 16 tokens.  The table's last column stands in for those behind it, so that
+// nothing has to be decided before it is read.
 struct Places {
     const int32_t* table;
-    uint32_t columns_end;  // blocks that the table has columns for
-    uint32_t pages, page_blocks;
+    uint32_t last, pages, page_blocks;  // last: block that the table has a column for
     uint64_t divide;
+    struct Block {
+        uint32_t page, block;  // and the number in the page
+        bool listed;
+        uint32_t pages;        // of the cache
+        __device__ __forceinline__ bool there() const { return listed & (page < pages); }
+    };
     __device__ __forceinline__ Places(const AttentionArgs& x, uint32_t sequence)
-        : table(x.batch.table + sequence * x.batch.ld_table), columns_end((uint32_t)x.batch.capacity / kCacheBlock),
+        : table(x.batch.table + sequence * x.batch.ld_table), last((uint32_t)x.batch.capacity / kCacheBlock - 1),
           pages(x.cache.pages), page_blocks(x.cache.page_blocks), divide(x.cache.divide) {}
-    // page << 32 | block in it; -1 for none
-    __device__ __forceinline__ int64_t of(uint32_t block) const {
-        if (block >= columns_end) return -1;
-        const uint32_t column = page_column(block, divide);
-        const int32_t page = table[column];
-        return (uint32_t)page < pages ? (int64_t)page << 32 | (block - column * page_blocks) : -1;
+    __device__ __forceinline__ Block of(uint32_t block, bool wanted = true) const {
+        const uint32_t inside = min(block, last), column = page_column(inside, divide);
+        return {(uint32_t)table[column], inside - column * page_blocks, wanted && block == inside, pages};
+    }
+    __device__ __forceinline__ Block first_if_none(const Block& b) const {
+        return {b.there() ? b.page : 0, b.there() ? b.block : 0, b.listed, pages};
     }
 };
 
@@ -326,13 +332,10 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
     const uint32_t n = lane % 16, g = lane / 16, dims = x.cache.head_dim;
     const uint32_t rows_all = job.sequence.rows * x.share, row0 = job.row_tile * R, rows = min(rows_all - row0, (uint32_t)R);
 
-    Eight q[F][NC][2];
     int pos[F], from[F];
 #pragma unroll
     for (int fr = 0; fr < F; ++fr) {
         const uint32_t row = 16 * fr + n;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) load_query<T>(x, job, row0 + row, row0 + rows, 64 * c + 16 * g, q[fr][c]);
         pos[fr] = job.sequence.position + (int)divided(row0 + min(row, rows - 1), x.by_share);
         from[fr] = window_from(x, pos[fr]);
     }
@@ -343,9 +346,15 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
     const int end = (int)((int64_t)range.count * (job.segment + 1) / job.segments);
 
     const Places places(x, job.index);
-    const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head + (n % 4) * dims + 16 * g;
-    const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head + n * 16;
-    const uint64_t block_bytes = 16 * dims;
+    const uint8_t* const k_head = x.cache.k_codes + job.head * x.cache.k_head + (n % 4) * dims;
+    const uint8_t* const v_head = x.cache.v_codes + job.head * x.cache.v_head;
+    // Dimensions past the last are read as others of the same key, against zeros of the query, and of the values
+    // into rows of sums that nobody stores.
+    uint32_t k_from[NC], v_from[ND];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) k_from[c] = 64 * c + 16 * g < dims ? 64 * c + 16 * g : 0;
+#pragma unroll
+    for (int e = 0; e < ND; ++e) v_from[e] = 16 * e + n < dims ? 16 * (16 * e + n) : 0;
 
     float4x o[F][ND];
     float m[F], l[F];
@@ -359,55 +368,64 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
     int v_most = -126;      // kRelative: the exponent of the largest value scale met
     bool poisoned = false;  // whether a tile that some row does not see all of had a NaN among its values
 
+    // Nothing is decided around these loads, so that the compiler knows which are under way and waits for no others:
+    // what has no place is read at the cache's first block, and hidden afterwards.
     uint4 k[4][NC], v[ND];
     float k_scale = 0.0f, v_scale = 0.0f;
     // a tile's places: of the block that a lane reads keys of, and of the one that it has values and weights of
-    int64_t k_place = -1, v_place = -1, k_next = -1, v_next = -1;
-    auto look = [&](int t, int64_t& kp, int64_t& vp) {
-        const uint32_t block = (uint32_t)range.tile(t) * 4;
-        kp = places.of(block + n / 4);
-        vp = places.of(block + g);
+    Places::Block k_next = {0, 0, false, 0}, v_next = {0, 0, false, 0};
+    auto look = [&](int t, Places::Block& k_place, Places::Block& v_place) {
+        const uint32_t block = (uint32_t)range.tile(min(t, end - 1)) * 4;
+        k_place = places.of(block + n / 4, t < end);
+        v_place = places.of(block + g, t < end);
     };
-    auto load_keys = [&](int64_t place) {
-        const uint8_t* const p = k_head + (place < 0 ? 0 : (place >> 32) * x.cache.k_page + (uint32_t)place * block_bytes);
+    auto load_keys = [&](const Places::Block& b) {
+        const Places::Block at = places.first_if_none(b);
+        const uint8_t* const p = k_head + at.page * x.cache.k_page + at.block * (16 * dims);
 #pragma unroll
         for (int f = 0; f < 4; ++f)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                k[f][c] = uint4{0, 0, 0, 0};
-                if (place >= 0 && 64 * c + 16 * g < dims) k[f][c] = *(const uint4*)(p + 4 * f * dims + 64 * c);
-            }
+            for (int c = 0; c < NC; ++c) k[f][c] = *(const uint4*)(p + 4 * f * dims + k_from[c]);
     };
-    auto load_values = [&](int64_t place) {
-        const uint8_t* const p = v_head + (place < 0 ? 0 : (place >> 32) * x.cache.v_page + (uint32_t)place * block_bytes);
+    auto load_values = [&](const Places::Block& b) {
+        const Places::Block at = places.first_if_none(b);
+        const uint8_t* const p = v_head + at.page * x.cache.v_page + at.block * (16 * dims);
 #pragma unroll
-        for (int e = 0; e < ND; ++e) {
-            v[e] = uint4{0, 0, 0, 0};
-            if (place >= 0 && 16 * e + n < dims) v[e] = *(const uint4*)(p + 256 * e);
-        }
+        for (int e = 0; e < ND; ++e) v[e] = *(const uint4*)(p + v_from[e]);
     };
-    auto load_scales = [&](int64_t place) {
-        k_scale = v_scale = 0.0f;
-        if (place < 0) return;
-        const uint64_t at = ((place >> 32) * x.cache.heads + job.head) * x.cache.page_blocks + (uint32_t)place;
-        k_scale = x.cache.k_scales[at];
-        v_scale = x.cache.v_scales[at];
+    auto load_scales = [&](const Places::Block& b) {
+        const Places::Block at = places.first_if_none(b);
+        const uint64_t i = ((uint64_t)at.page * x.cache.heads + job.head) * x.cache.page_blocks + at.block;
+        k_scale = x.cache.k_scales[i];
+        v_scale = x.cache.v_scales[i];
     };
 
     int t = first + (int)wave;
+    bool here = false;  // whether the block that a lane has weights of is in the cache
     if (t < end) {
-        look(t, k_place, v_place);
-        if (t + NW < end) look(t + NW, k_next, v_next);
-        load_keys(k_place);
-        load_scales(v_place);
-        load_values(v_place);
+        look(t, k_next, v_next);
+        here = v_next.there();
+        load_keys(k_next);
+        load_scales(v_next);
+        load_values(v_next);
+        look(t + NW, k_next, v_next);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    Eight q[F][NC][2];
+#pragma unroll
+    for (int fr = 0; fr < F; ++fr)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            load_query<T>(x, job, row0 + 16 * fr + n, row0 + rows, 64 * c + 16 * g, q[fr][c]);
+    // The queries are here before the loop, as far as the compiler knows too, which would wait for them in it, and by
+    // that for what was asked for after them.
+    __builtin_amdgcn_s_waitcnt(kWaitAll);
     for (; t < end; t += NW) {
         const int tile = range.tile(t), key0 = tile * kTile;
-        const bool more = t + NW < end;
-        int64_t k_then = -1, v_then = -1;
-        if (t + 2 * NW < end) look(t + 2 * NW, k_then, v_then);
-
+        // asked for before the next tile's codes, so that it is there a tile later without waiting for them
+        Places::Block k_then, v_then;
+        look(t + 2 * NW, k_then, v_then);
+        __builtin_amdgcn_sched_barrier(0);
         float4x s[F][4];
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
@@ -425,8 +443,7 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
         }
         const float to_log2 = fmaxf(cache_scale(k_scale) * x.scale, 0x1p-126f);
         const float v_power = cache_scale(v_scale);
-        const bool here = v_place >= 0;
-        if (more) load_keys(k_next);
+        load_keys(k_next);
 
         const bool edge = is_edge(x, key0, p_min, p_max) || __ballot(!here) != 0;
         if (edge) {
@@ -494,25 +511,26 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                 o[fr][e] = W::mul16(b, p[fr][1], o[fr][e]);
             }
         }
-        if (more) {
-            load_scales(v_next);
-            load_values(v_next);
-        }
-        k_place = k_next, v_place = v_next, k_next = k_then, v_next = v_then;
+        here = v_next.there();
+        load_scales(v_next);
+        load_values(v_next);
+        k_next = k_then;
+        v_next = v_then;
     }
 
     if (poisoned) {  // a NaN among the values reaches the rows that see it, and no others
         for (t = first + (int)wave; t < end; t += NW) {
             const int key0 = range.tile(t) * kTile;
-            look(t, k_place, v_place);
-            if (!is_edge(x, key0, p_min, p_max) && __ballot(v_place < 0) == 0) continue;
-            load_values(v_place);
+            look(t, k_next, v_next);
+            here = v_next.there();
+            if (!is_edge(x, key0, p_min, p_max) && __ballot(!here) == 0) continue;
+            load_values(v_next);
 #pragma unroll
             for (int fr = 0; fr < F; ++fr) {
                 Eight seen[2];
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    seen[i / 8][i % 8] = ((v_place >= 0) & sees(x, pos[fr], from[fr], key0 + 16 * (int)g + i)) ? (T)1.0f : (T)0.0f;
+                    seen[i / 8][i % 8] = (here & sees(x, pos[fr], from[fr], key0 + 16 * (int)g + i)) ? (T)1.0f : (T)0.0f;
 #pragma unroll
                 for (int e = 0; e < ND; ++e) {
                     float4x hits = {0, 0, 0, 0};
@@ -845,17 +863,17 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
             const int key0 = range.tile(t) * kTile;
             if (!is_edge(x, key0, all_min, all_max)) continue;
             for (int f = 0; f < 2; ++f) {
-                const int64_t place = places.of((uint32_t)key0 / kCacheBlock + 2 * f + h);
+                const Places::Block place = places.of((uint32_t)key0 / kCacheBlock + 2 * f + h);
+                const bool here = place.there();
                 Eight seen[2];
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    seen[i / 8][i % 8] = ((place >= 0) & sees(x, pos, from, key0 + 32 * f + 16 * (int)h + i)) ? (T)1.0f : (T)0.0f;
-                const uint8_t* const block = v_head + (place < 0 ? 0 : (place >> 32) * x.cache.v_page +
-                                                                          (uint64_t)(uint32_t)place * 16 * dims);
+                    seen[i / 8][i % 8] = (here & sees(x, pos, from, key0 + 32 * f + 16 * (int)h + i)) ? (T)1.0f : (T)0.0f;
+                const uint8_t* const block = v_head + (here ? place.page * x.cache.v_page + place.block * (16 * dims) : 0);
 #pragma unroll
                 for (int e = 0; e < NO; ++e) {
                     uint4 w = {0, 0, 0, 0};
-                    if (place >= 0 && 32 * e + n < dims) w = *(const uint4*)(block + 16 * (32 * e + n));
+                    if (here && 32 * e + n < dims) w = *(const uint4*)(block + 16 * (32 * e + n));
                     float16x hits;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) hits[i] = 0.0f;
@@ -987,8 +1005,8 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
     const uint64_t tiles = (reach + kTile - 1) / kTile;
     plan.least = 8;
-    plan.log2_slots = 9;
-    if (tiles <= plan.least + plan.least / 4) plan.log2_slots = 0;  // no unit is cut
+    // Up to 1536 tokens a workgroup's eight waves take three tiles each, which costs less than the join's launch.
+    plan.log2_slots = tiles <= 24 ? 0 : 9;
     const uint32_t slots = plan.log2_slots ? 1u << plan.log2_slots : 0;
     plan.jobs = (uint32_t)(units + 2 * slots);
     plan.join = (uint32_t)std::min<uint64_t>(units, slots);
