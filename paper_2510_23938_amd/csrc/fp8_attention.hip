@@ -966,15 +966,12 @@ hipError_t run(const AttentionArgs& a, const AttentionPlan& plan, uint32_t threa
 
 template <typename T, int DP>
 hipError_t launch(const AttentionArgs& a, const AttentionPlan& plan, hipStream_t s) {
+    // Eight waves as long as they have the registers; with 256 of them a lane (8 sequences of 8000 tokens): 16 rows of 256
+    // dimensions took 153 us by eight waves and 54 by four, 32 of 128 45 and 33.
+    constexpr int NW = DP <= 128 ? 8 : 4, NW2 = DP <= 64 ? 8 : 4;
     switch (plan.rows) {
-        case 16: return run<T, DP, 16>(a, plan, 512, stream_attention<T, DP, 1, 8>, s);
-        case 32: {
-            constexpr int NW = DP <= 128 ? 8 : 4;
-            return run<T, DP, 32>(a, plan, NW * 64, stream_attention<T, DP, 2, NW>, s);
-        }
-        case 64:
-            if constexpr (DP <= 128) return run<T, DP, 64>(a, plan, 256, stream_attention<T, DP, 4, 4>, s);
-            [[fallthrough]];
+        case 16: return run<T, DP, 16>(a, plan, NW * 64, stream_attention<T, DP, 1, NW>, s);
+        case 32: return run<T, DP, 32>(a, plan, NW2 * 64, stream_attention<T, DP, 2, NW2>, s);
         default: return run<T, DP, kManyRows>(a, plan, 256, tile_attention<T, DP>, s);
     }
 }
@@ -998,15 +995,15 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     plan.dims = (uint32_t)((head_dim + 63) / 64 * 64);
     const uint64_t share = heads / kv_heads;
     const uint64_t rows = (tokens + sequences - 1) / sequences * share;  // of a sequence, on the average
-    plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && plan.dims <= 128 ? 64 : kManyRows;
+    plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kManyRows;
     if (plan.rows == kManyRows && head_dim > 64 && head_dim <= 96) plan.dims = 96;
     const uint64_t units = kv_heads * (tokens * share / plan.rows + std::min(sequences, tokens));
     // tiles that one row tile may see at most
     const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
     const uint64_t tiles = (reach + kTile - 1) / kTile;
-    plan.least = 8;
+    plan.least = 4;
     // Up to 1536 tokens a workgroup's eight waves take three tiles each, which costs less than the join's launch.
-    plan.log2_slots = tiles <= 24 ? 0 : 9;
+    plan.log2_slots = tiles <= 24 ? 0 : plan.rows == kManyRows ? 9 : 8;
     const uint32_t slots = plan.log2_slots ? 1u << plan.log2_slots : 0;
     plan.jobs = (uint32_t)(units + 2 * slots);
     plan.join = (uint32_t)std::min<uint64_t>(units, slots);

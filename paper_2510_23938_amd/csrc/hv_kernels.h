@@ -369,7 +369,7 @@ struct AttentionArgs {
 // What a call is made by, from sizes alone; the kernels cut the keys by the lengths that they find.
 struct AttentionPlan {
     uint32_t dims;   // of a head, rounded up to what the kernels are made for
-    uint32_t rows;   // of a workgroup: 16, 32 or 64 straight from memory, 128 through LDS
+    uint32_t rows;   // of a workgroup: 16 or 32 straight from memory, 128 through LDS
     uint32_t jobs;   // workgroups, at most
     uint32_t log2_slots;  // of the shares that the keys' tiles are cut into; 0 where they never are
     uint32_t least;  // tiles of a share, at least
