@@ -913,13 +913,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
 // the parts' sums joined, in order: workgroups of 16 rows of each unit that is cut
 
 template <typename T, int DP, int R>
-__global__ void __launch_bounds__(16 * (DP / 4)) join_attention(AttentionArgs x) {
-    constexpr uint32_t kLanes = DP / 4;
-    const Job job = find_job<R, true>(x, blockIdx.x);
-    if (!job.found) return;
-    const uint32_t rows = min(job.sequence.rows * x.share - job.row_tile * R, (uint32_t)R);
-    const uint32_t row = blockIdx.y * 16 + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
-    if (row >= rows || d >= x.cache.head_dim) return;
+__device__ __forceinline__ void join_row(const AttentionArgs& x, const Job& job, uint32_t row, uint32_t d) {
     const float2* const weights = part_weights<R, DP>(x, job.part) + row;
     const float* const from = part_rows<R, DP>(x, job.part) + row * DP + d;
     // Eight parts at a time are on their way; the maximum of those so far scales the sums, as in a segment.
@@ -953,14 +947,27 @@ __global__ void __launch_bounds__(16 * (DP / 4)) join_attention(AttentionArgs x)
     store_four(out_at<T>(x, job, job.row_tile * R + row) + d, total == 0.0f ? float4x{0, 0, 0, 0} : sum / total);
 }
 
-// ---------------------------------------------------------------------------
+template <typename T, int DP, int R>
+__global__ void __launch_bounds__(16 * (DP / 4)) join_attention(AttentionArgs x) {
+    constexpr uint32_t kLanes = DP / 4;
+    const Job job = find_job<R, true>(x, blockIdx.x);
+    if (!job.found) return;
+    const uint32_t rows = min(job.sequence.rows * x.share - job.row_tile * R, (uint32_t)R);
+    const uint32_t d = threadIdx.x % kLanes * 4;
+    if (d >= x.cache.head_dim) return;
+    for (uint32_t row = blockIdx.y * 16 + threadIdx.x / kLanes; row < rows; row += gridDim.y * 16)
+        join_row<T, DP, R>(x, job, row, d);
+}
+
+ // ---------------------------------------------------------------------------
 // launches
 
 template <typename T, int DP, int R, typename Main>
 hipError_t run(const AttentionArgs& a, const AttentionPlan& plan, uint32_t threads, Main main, hipStream_t s) {
     main<<<item_grid(plan.jobs), threads, 0, s>>>(a);
     if (plan.join == 0) return hipGetLastError();
-    join_attention<T, DP, R><<<dim3(plan.join, R / 16), 16 * (DP / 4), 0, s>>>(a);
+    // where there are many units few of them are cut
+    join_attention<T, DP, R><<<dim3(plan.join, plan.join >= 256 ? 1 : R / 16), 16 * (DP / 4), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -82,20 +82,14 @@ __global__ void __launch_bounds__(kWaves * 64) write_kernel(WriteArgs x) {
     const int p0 = first_written(s), p1 = end_written(s);
     const uint32_t block = p0 / 16 + place.within, column = page_column(block, x.cache.divide);
     const int32_t page = x.batch.table[place.index * x.batch.ld_table + column];
-    if (page < 0 || (uint32_t)page >= x.cache.pages) return;
     const uint32_t in_page = block - column * x.cache.page_blocks;
     // slots [a, b) of the block get new tokens, those before a hold earlier ones
     const int a = max(p0 - (int)block * 16, 0), b = min(p1 - (int)block * 16, 16);
     const int64_t row0 = s.row + ((int)block * 16 - s.position);  // of slot 0
 
     const uint32_t dims = x.cache.head_dim;
-    const uint64_t scale_at = ((uint64_t)page * x.cache.heads + head) * x.cache.page_blocks + in_page;
-    uint8_t* const k_to = x.cache.k_codes + page * x.cache.k_page + head * x.cache.k_head + (uint64_t)in_page * 16 * dims;
-    uint8_t* const v_to = x.cache.v_codes + page * x.cache.v_page + head * x.cache.v_head + (uint64_t)in_page * 16 * dims;
     const T* const k_from = (const T*)x.k + head * x.k_head;
     const T* const v_from = (const T*)x.v + head * x.v_head;
-
-    const float k_old = cache_scale(x.cache.k_scales[scale_at]), v_old = cache_scale(x.cache.v_scales[scale_at]);
 
     // keys: eights of the block's elements, token by token
     float k[KI][8];
@@ -128,8 +122,23 @@ __global__ void __launch_bounds__(kWaves * 64) write_kernel(WriteArgs x) {
             v[i][t][0] = (float)two.x;
             v[i][t][1] = (float)two.y;
         }
+    }
+
+    // the page and what the block holds, with those loads under way
+    if (page < 0 || (uint32_t)page >= x.cache.pages) return;
+    const uint64_t scale_at = ((uint64_t)page * x.cache.heads + head) * x.cache.page_blocks + in_page;
+    uint8_t* const k_to = x.cache.k_codes + page * x.cache.k_page + head * x.cache.k_head + (uint64_t)in_page * 16 * dims;
+    uint8_t* const v_to = x.cache.v_codes + page * x.cache.v_page + head * x.cache.v_head + (uint64_t)in_page * 16 * dims;
+    float k_old = 0.0f, v_old = 0.0f;
+    if (a > 0) {
+        k_old = cache_scale(x.cache.k_scales[scale_at]);
+        v_old = cache_scale(x.cache.v_scales[scale_at]);
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+        const uint32_t d = (i * 64 + lane) * 2;
         held[i][0] = held[i][1] = uint4{0, 0, 0, 0};
-        if ((a > 0 || b < 16) && inside) __builtin_memcpy(held[i], v_to + d * 16, 32);
+        if ((a > 0 || b < 16) && d < dims) __builtin_memcpy(held[i], v_to + d * 16, 32);
     }
 
     float k_most = 0.0f, v_most = 0.0f;
