@@ -29,15 +29,22 @@ hv_status check_head_dim(uint64_t head_dim) {
     return HV_OK;
 }
 
+// Whether `outer` things, each of `inner` things of `size`, lie apart by these strides without overlap, all of them
+// within what can be addressed.
+bool nested(uint64_t size, uint64_t inner, uint64_t inner_stride, uint64_t outer, uint64_t outer_stride) {
+    using Wide = unsigned __int128;
+    const Wide span = (Wide)(inner - 1) * inner_stride + size;
+    return (inner <= 1 || inner_stride >= size) && (outer <= 1 || outer_stride >= span) &&
+           (Wide)(outer - 1) * outer_stride + span <= (Wide)1 << 62;
+}
+
 // Pages and heads of `bytes` bytes each, apart by the two strides: one nested in the other.
 hv_status check_places(const char* what, uint64_t bytes, uint64_t pages, uint64_t page, uint64_t heads, uint64_t head) {
     if (page % 16 != 0 || head % 16 != 0)
         return fail(HV_ERR_INVALID_ARG, "%s: pages or heads are not a multiple of 16 bytes apart", what);
     HV_LIMIT(what, page, kMaxStride);
     HV_LIMIT(what, head, kMaxStride);
-    const bool heads_in_pages = (heads == 1 || head >= bytes) && (pages <= 1 || page >= (heads - 1) * head + bytes);
-    const bool pages_in_heads = (pages <= 1 || page >= bytes) && (heads == 1 || head >= (pages - 1) * page + bytes);
-    if (!heads_in_pages && !pages_in_heads)
+    if (!nested(bytes, heads, head, pages, page) && !nested(bytes, pages, page, heads, head))
         return fail(HV_ERR_INVALID_ARG, "%s: pages or heads overlap (%llu and %llu bytes apart, %llu each)", what,
                     (unsigned long long)page, (unsigned long long)head, (unsigned long long)bytes);
     return HV_OK;
@@ -79,15 +86,13 @@ hv_status check_batch(const hv_fp8_batch* b, uint64_t page_tokens) {
     return HV_OK;
 }
 
-// [tokens][heads][dim] with the dimensions adjacent: tokens and heads nested either way, or not read twice at least.
+// [tokens][heads][dim] with the dimensions adjacent: tokens and heads nested either way.
 hv_status check_rows(const char* what, const void* p, size_t element, uint64_t tokens, uint64_t token, uint64_t heads,
                      uint64_t head, uint64_t dim) {
     HV_TRY(check_pointer(what, p, element));
     HV_LIMIT(what, token, kMaxStride);
     HV_LIMIT(what, head, kMaxStride);
-    const bool heads_in_tokens = (heads == 1 || head >= dim) && (tokens == 1 || token >= (heads - 1) * head + dim);
-    const bool tokens_in_heads = (tokens == 1 || token >= dim) && (heads == 1 || head >= (tokens - 1) * token + dim);
-    if (!heads_in_tokens && !tokens_in_heads)
+    if (!nested(dim, heads, head, tokens, token) && !nested(dim, tokens, token, heads, head))
         return fail(HV_ERR_INVALID_ARG, "%s: rows overlap (tokens %llu and heads %llu elements apart, %llu each)", what,
                     (unsigned long long)token, (unsigned long long)head, (unsigned long long)dim);
     return HV_OK;
