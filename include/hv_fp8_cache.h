@@ -20,7 +20,7 @@
  *
  * Batches.  A call serves `count` sequences.  Sequence i has, with this call's new
  * tokens, lengths[i] tokens; the new ones are the last of them and take the rows
- * starts[i] to starts[i + 1] - 1 of the call's matrices, so a token in row t has
+ * starts[i] to starts[i + 1] - 1 of the call's matrices, no row of two sequences, so a token in row t has
  * the position lengths[i] - starts[i + 1] + t.  The token at position p of sequence
  * i lies in page pages[i][p / page_tokens].  All three are device memory that the
  * call's kernels read, so a captured call takes what they hold when it is replayed.
@@ -44,7 +44,7 @@
  * strides that overlap, a head_dim that is no multiple of 16 from 16 to 256, a
  * page_tokens that is no multiple of 16 from 16 to 65536, or sizes past the limits (pages
  * 2^31 - 1, kv_heads 65535, sequences 65536, columns * page_tokens 2^30, tokens * heads
- * 2^30, strides 2^40); HV_ERR_HIP.
+ * 2^30, strides 2^40, all of an operand 2^62); HV_ERR_HIP.
  */
 #ifndef HV_FP8_CACHE_H
 #define HV_FP8_CACHE_H
@@ -108,12 +108,12 @@ size_t hv_fp8_attention_workspace_bytes(uint64_t sequences, uint64_t capacity, u
  * of a token's are minus infinity, zeros.
  *   type: HV_BF16 or HV_F16, of q and out.
  *   q, out: [tokens][heads][head_dim], the dimensions of a head adjacent; kv_heads divides heads.
- *   scale: positive and finite.
+ *   scale: positive and finite, at least 2^-126.
  *   window: 0 for none; sinks count only beside a window.
  *   workspace: >= hv_fp8_attention_workspace_bytes(...), 256-byte aligned; NULL where that is 0.
  *              Scratch: calls that share one must share a stream.
  * For HV_F16, value codes are widened relative to the largest value scale met: a block whose scale
- * is 2^-14 of it loses bits, and from 2^-24 on all of them.
+ * is 2^-12 of it begins to lose bits, and from 2^-24 on all of them.
  * Errors: HV_ERR_INVALID_ARG also for another type, heads that are no multiple of kv_heads, or another
  * scale; HV_ERR_WORKSPACE for a missing, short or misaligned workspace. */
 hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* q,

@@ -20,11 +20,11 @@ __device__ __forceinline__ float cache_scale(float s) {
     return __uint_as_float(min(max(e, 0x00800000u), 0x7f000000u));
 }
 
-// b / blocks_per_page of a block number below 2^26 and up to 2^12 blocks a page: with divide = ceil(2^40 /
-// blocks_per_page) the quotient is off by less than b * 2^12 / 2^40 < 2^-2 / 2^12 (above it), which no
-// fraction of a whole number by 2^12 reaches.
+// b / blocks_per_page of a block number below 2^26 and up to 2^12 blocks a page: with divide = ceil(2^38 /
+// blocks_per_page) the product stays below 2^64, and its quotient is above the true one by less than 2^26 / 2^38,
+// which is less than a whole number's fraction by 2^12 lacks to the next.
 __device__ __forceinline__ uint32_t page_column(uint32_t block, uint64_t divide) {
-    return (uint32_t)(block * divide >> 40);
+    return (uint32_t)(block * divide >> 38);
 }
 
 // With l the bits of d - 1, mul = floor(2^(31 + l) / d) + 1 is off by at most 2^l / 2^(31 + l) of itself: too little to

@@ -116,7 +116,7 @@ hv::CacheArgs cache_args(const hv_fp8_cache& c) {
     const uint64_t blocks = c.page_tokens / 16;
     return {c.k_codes, c.k_scales, c.v_codes, c.v_scales, c.k_page, c.k_head, c.v_page, c.v_head,
             (uint32_t)c.pages, (uint32_t)c.kv_heads, (uint32_t)blocks, (uint32_t)c.head_dim,
-            (((uint64_t)1 << 40) + blocks - 1) / blocks};
+            (((uint64_t)1 << 38) + blocks - 1) / blocks};
 }
 
 hv::BatchArgs batch_args(const hv_fp8_batch& b, uint64_t page_tokens, uint64_t tokens) {

@@ -331,7 +331,7 @@ struct CacheArgs {
     float* v_scales;
     uint64_t k_page, k_head, v_page, v_head;  // bytes
     uint32_t pages, heads, page_blocks, head_dim;
-    uint64_t divide;  // ceil(2^40 / page_blocks)
+    uint64_t divide;  // ceil(2^38 / page_blocks)
 };
 struct BatchArgs {
     const int32_t* starts;

@@ -118,7 +118,7 @@ def test_mixed_prompts_and_tokens():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("steep", [0.0, 1e-4, 8.0, 60.0])
+@pytest.mark.parametrize("steep", [0.0, 1e-4, 0.1, 8.0, 60.0])
 def test_flat_and_steep_scores(dtype, steep):
     rng = rng_of(steep * 10)
     check(rng, [(1, 600), (1, 40)], 8, 2, 128, 64, dtype, steep=steep)
