@@ -8,7 +8,8 @@
  * them: codes and scales, with no second copy in another layout.  (That goes for
  * weights whose rows are 16-byte aligned.  Rows at other addresses hv_fp8_matmul may
  * copy to its workspace, anew in each call, and multiply from there.)
- * Held in 8 bits, a weight set also takes half the time to hash.
+ * Held in 8 bits, a weight set also takes half the time to hash.  Low-rank adapters of many requests go beside
+ * the products on one verified base.
  *
  * Format.  A code is an 8-bit floating-point number, OCP E4M3 (1 sign, 4
  * exponent and 3 mantissa bits, largest value 448, NaN 0x7f and 0xff, no

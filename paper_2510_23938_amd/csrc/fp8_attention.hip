@@ -17,10 +17,14 @@
 // which the conversion of codes applies; and values lie in the cache by dimensions so that
 // their 16 bytes are those 16 tokens.
 //
-// Two kernels: few rows (a token or a few each of many sequences), bound by reading
-// the cache, take it from memory to registers; many rows, bound by the matrix and vector
-// units, share it in LDS.  In both, a sequence's keys are cut into segments where
-// there are too few rows to fill the chip; the parts' sums are joined by another kernel.
+// Two kernels: up to 32 rows (a token or a few each of many sequences), bound by reading
+// the cache, take it from memory to registers (666 MB of 64 sequences 133 us, 5.0 TB/s; one of 131072 tokens 56 us, 4.8,
+// where a copy reaches 4.75); more rows, bound by the matrix and vector units, which
+// take turns more than they overlap (33% and 44% of the cycles), share it in LDS (4 prompts of 2048 tokens, 64 heads
+// on 8 of 128 dimensions, 344 us, 0.80 PFLOP/s; one of 16384 tokens 1.0, where a library's product reaches 1.3 to 1.5).
+// In both, a sequence's keys are cut into segments where there are too few rows to fill the
+// chip; the parts' sums are joined by another kernel, in order.  A call whose sequences can have no more than 1536
+// tokens is never cut: its one launch (777 tokens: 11 us, of which the host's part is 10) is shorter than two.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -314,7 +318,9 @@ __device__ __forceinline__ void load_query(const AttentionArgs& x, const Job& jo
 // ---------------------------------------------------------------------------
 // few rows: the cache from memory to registers
 
-// A workgroup takes 16 * F rows and one segment of their keys, its NW waves a tile of 64 keys in turn.  In a
+// A workgroup takes 16 * F rows and one segment of their keys, its NW waves a tile of 64 keys in turn: a tile's 16 KB (of
+// 128 dimensions) are asked for a tile ahead, 128 KB for each unit, which is what its share of HBM's rate
+// times its latency asks for.  In a
 // tile, a lane (row n = lane % 16, group g = lane / 16) has the weights of block g.  For that, fragment f of four has
 // as its key m the token 4 f + m % 4 of block m / 4.
 template <typename T, int DP, int F, int NW>
@@ -613,7 +619,9 @@ __device__ __forceinline__ uint32_t chunk_place(uint32_t row, uint32_t chunk) {
 
 // Lane (row n = lane % 32, half h = lane / 32) of a wave has the weights of the blocks h and 2 + h of a tile.  For
 // that, fragment f of two has as its key m the token 4 (m / 8) + m % 4 of block 2 f + m / 4 % 2, and LDS holds the keys in
-// that order.  Each of the four waves brings one of a tile's blocks.
+// that order.  Each of the four waves brings one of a tile's blocks and widens it once for all: LDS holds what the
+// matrix unit reads, two tiles of keys and values (64 KB for 128 dimensions), so that two workgroups share a unit and one
+// computes while the other waits.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(AttentionArgs x) {
     constexpr int R = kManyRows, NC = DP / 32, NO = DP / 32;
@@ -1002,14 +1010,18 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     plan.dims = (uint32_t)((head_dim + 63) / 64 * 64);
     const uint64_t share = heads / kv_heads;
     const uint64_t rows = (tokens + sequences - 1) / sequences * share;  // of a sequence, on the average
+    // (8 sequences of 8000 tokens, 64 rows of 128 dimensions: straight from memory 79 us, by tiles 47; 32 rows 33 and 41)
     plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kManyRows;
-    if (plan.rows == kManyRows && head_dim > 64 && head_dim <= 96) plan.dims = 96;
+    if (plan.rows == kManyRows && head_dim > 64 && head_dim <= 96) plan.dims = 96;  // products and LDS of three quarters
     const uint64_t units = kv_heads * (tokens * share / plan.rows + std::min(sequences, tokens));
     // tiles that one row tile may see at most
     const uint64_t reach = window == 0 ? capacity : std::min(capacity, window + sinks + tokens + 2 * kTile);
     const uint64_t tiles = (reach + kTile - 1) / kTile;
     plan.least = 4;
-    // Up to 1536 tokens a workgroup's eight waves take three tiles each, which costs less than the join's launch.
+    // Up to 1536 tokens a workgroup's eight waves take three tiles each, which costs less than the join's launch.  Shares:
+    // as many as run at a time, one workgroup a unit of few rows (131072 tokens: 256 shares 56 us, 512 65, 1024 84; 64
+    // sequences 136, 140, 137), two of many (777 tokens after 30,000 with a window of 4095: 256 63 us, 512 55, 1024 63).
+    // At least four tiles (one sequence of 2000 tokens: 13.2 us, at least eight 14.3, sixteen 15.7).
     plan.log2_slots = tiles <= 24 ? 0 : plan.rows == kManyRows ? 9 : 8;
     const uint32_t slots = plan.log2_slots ? 1u << plan.log2_slots : 0;
     plan.jobs = (uint32_t)(units + 2 * slots);

@@ -9,6 +9,10 @@
 // neighbouring dimensions of all 16 tokens, which in the cache lie side by side
 // for each dimension: 16 loads of two elements a lane turn the block without LDS or
 // exchanges between lanes, and the stores are whole lines.
+//
+// Bound by memory: 16384 tokens of 8 heads of 128 dimensions in bfloat16 (101 MB) 25 us, 4.0 TB/s, where a copy
+// reaches 4.75: 1.6 rounds of the waves that the chip holds, each with three trips to memory (the sequences,
+// the page beside the elements, the stores).  A token of each of 8 sequences takes 6 us, those trips and a launch.
 #include <algorithm>
 #include <type_traits>
 
