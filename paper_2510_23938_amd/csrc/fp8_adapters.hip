@@ -442,7 +442,7 @@ AdapterPlan fp8_adapter_plan(uint64_t m, uint64_t k, uint64_t rank, uint64_t ada
     p.split_groups = (uint32_t)std::max<uint64_t>(1, (groups + splits - 1) / splits);
     p.splits = (uint32_t)std::max<uint64_t>(1, (groups + p.split_groups - 1) / p.split_groups);
     // More than 1024 tokens fill the chip by themselves (2048 x 28672 of rank 16: 68 us, and 94 by a wave for each adapter);
-    // of fewer, each adapter has a wave (32 x 8192 with 16 in each 16 tokens: 6 us, all by one wave 27).
+    // of fewer, each adapter has a wave (32 x 8192 with 16 in each 16 tokens: 6 us, by four waves in turn 27).
     p.many = m > 1024;
     p.token_rows = (uint32_t)((tiles + kRowOfItems - 1) / kRowOfItems);
     p.workspace = adapters > 0 && k > 0 ? (uint64_t)p.splits * m * p.inner_ld * sizeof(float) : 0;
