@@ -1433,9 +1433,13 @@ def _heads(t, dtypes, what: str, index: int, shape=None) -> tuple:
                          f"{'[tokens, heads, head_dim]' if shape is None else tuple(shape)}")
     if t.is_contiguous():
         return t.data_ptr(), t.shape[1] * t.shape[2], t.shape[2]
-    token, head, one = _strides(t)
-    if one != 1:
+    (tokens, heads, dim), (token, head, one) = t.shape, t.stride()
+    if one != 1 and dim > 1:
         raise ValueError(f"{what}: the elements of a head must be adjacent")
+    if heads <= 1:  # the stride of a dimension of one element means nothing
+        head = dim
+    if tokens <= 1:
+        token = head * heads
     return t.data_ptr(), token, head
 
 
