@@ -83,7 +83,7 @@ typedef struct {
  * A new value's code is value / scale rounded to the nearest E4M3 number, ties to
  * even; a NaN or an infinity becomes a NaN code and leaves the rest of its block alone.
  * Slots of a block behind its last new token stay as they are and hold nothing.
- * No page may be written by two sequences in one call.
+ * No page may be written by two sequences in one call, nor by two columns of one.
  *   k, v: [tokens][kv_heads][head_dim] of the type, the dimensions of a head adjacent. */
 hv_status hv_fp8_cache_write(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* k,
                              uint64_t k_token, uint64_t k_head, const void* v, uint64_t v_token, uint64_t v_head,
@@ -105,15 +105,15 @@ size_t hv_fp8_attention_workspace_bytes(uint64_t sequences, uint64_t capacity, u
  * Products of q and codes and of weights and codes are added in 32 bits, the softmax
  * is in 32 bits; a weight is rounded to the type before its product, relative to its row's
  * largest, and the result once.  Scores beyond 32 bits give NaN or, where all
- * of a token's are minus infinity, zeros.
+ * of a token's are minus infinity, zeros; values whose sums are beyond 32 bits give infinities or NaN.
  *   type: HV_BF16 or HV_F16, of q and out.
  *   q, out: [tokens][heads][head_dim], the dimensions of a head adjacent; kv_heads divides heads.
  *   scale: positive and finite, at least 2^-126.
  *   window: 0 for none; sinks count only beside a window.
  *   workspace: >= hv_fp8_attention_workspace_bytes(...), 256-byte aligned; NULL where that is 0.
  *              Scratch: calls that share one must share a stream.
- * For HV_F16, value codes are widened relative to the largest value scale met: a block whose scale
- * is 2^-12 of it begins to lose bits, and from 2^-24 on all of them.
+ * For HV_F16, a weight is rounded together with its block's value scale, relative to the largest weight
+ * and the largest scale of what the token sees: products of the two below 2^-18 begin to lose bits, below 2^-29 all.
  * Errors: HV_ERR_INVALID_ARG also for another type, heads that are no multiple of kv_heads, or another
  * scale; HV_ERR_WORKSPACE for a missing, short or misaligned workspace. */
 hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch, hv_type type, const void* q,

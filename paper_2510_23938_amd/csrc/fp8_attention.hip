@@ -46,6 +46,9 @@ constexpr int kMatrix = 0x8, kDsRead = 0x100;  // instruction groups of the sche
 constexpr int kWaitAll = 0;       // s_waitcnt: nothing outstanding
 constexpr float kLazy = 8.0f;     // binary orders that a row's weights may grow before its sums are scaled
 constexpr float kNothing = -FLT_MAX;  // the maximum of a row that has seen nothing
+// Half precision: binary orders that weights are raised by, so that those of blocks with small scales lose less.  With
+// kLazy they reach 2^12, and 2^16 where a score's last place is worth four.
+constexpr int kRaised = 4;
 
 // ---------------------------------------------------------------------------
 // the 16-bit types
@@ -84,7 +87,8 @@ struct Wide<__bf16> {
 template <>
 struct Wide<_Float16> {
     using Eight = f16x8;
-    // Values times their scale may leave the type: they are taken relative to the largest scale met.
+    // Values times their scale may leave the type: the scale goes into the weights, relative to the largest scale of
+    // what the row sees.
     static constexpr bool kRelative = true;
     template <bool kHigh>
     static __device__ __forceinline__ f16x2 two(uint32_t w, float scale) {
@@ -114,20 +118,28 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)max(e + 127, 1) << 23); }
 __device__ __forceinline__ int exponent_of(float power) { return (int)(__float_as_uint(power) >> 23) - 127; }
 
-// The high bit of each byte that is a NaN code.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7f) + 0x01010101) & 0x80808080; }
+// Codes that a weight of zero does not hide: NaN, and in bfloat16 those whose value under the block's scale is 2^128 or
+// more, an infinity.  Such a code's magnitude, as a byte, is the limit or more: 0x7f, or that of 2^(128 - e).  What is
+// added to a byte's low seven bits makes its high bit of that.
+template <typename T>
+__device__ __forceinline__ uint32_t lost_codes(float power) {
+    const int e = Wide<T>::kRelative ? 0 : exponent_of(power), limit = e < 120 ? 0x7f : (135 - e) << 3;
+    return (0x80 - limit) * 0x01010101u;
+}
+// The high bit of each byte that is one of them.
+__device__ __forceinline__ uint32_t lost_bytes(uint32_t w, uint32_t lost) { return ((w & 0x7f7f7f7f) + lost) & 0x80808080; }
 // Zero codes in their place; whether there were any.
-__device__ __forceinline__ uint32_t take_nan(uint32_t& w) {
-    const uint32_t m = nan_bytes(w);
+__device__ __forceinline__ uint32_t take_lost(uint32_t& w, uint32_t lost) {
+    const uint32_t m = lost_bytes(w, lost);
     w &= ~(m | (m - (m >> 7)));
     return m;
 }
-__device__ __forceinline__ uint32_t take_nan(uint4& w) {
-    return take_nan(w.x) | take_nan(w.y) | take_nan(w.z) | take_nan(w.w);
+__device__ __forceinline__ uint32_t take_lost(uint4& w, uint32_t lost) {
+    return take_lost(w.x, lost) | take_lost(w.y, lost) | take_lost(w.z, lost) | take_lost(w.w, lost);
 }
 // The code of 1 in their place, and of zero elsewhere.
-__device__ __forceinline__ uint32_t ones_at_nan(uint32_t w) {
-    const uint32_t m = nan_bytes(w);
+__device__ __forceinline__ uint32_t ones_at_lost(uint32_t w, uint32_t lost) {
+    const uint32_t m = lost_bytes(w, lost);
     return m >> 2 | m >> 3 | m >> 4;
 }
 
@@ -231,9 +243,9 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& x, uint32_t item) {
     }
 }
 
-// Whether some of the positions p_min to p_max sees some of the block's 16 tokens from `key` on.
-__device__ __forceinline__ bool block_seen(const AttentionArgs& x, int key, int p_min, int p_max) {
-    return key <= p_max && (!x.window || key + (int)kCacheBlock > p_min - x.window + 1 || key < x.sinks);
+// Whether a position sees some of the block's 16 tokens from `key` on.
+__device__ __forceinline__ bool block_seen(const AttentionArgs& x, int key, int position) {
+    return key <= position && (!x.window || key + (int)kCacheBlock > position - x.window + 1 || key < x.sinks);
 }
 
 // `from`: the first key that a position's window has.
@@ -364,15 +376,16 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
 
     float4x o[F][ND];
     float m[F], l[F];
+    int v_most[F];  // kRelative: the exponent of the largest value scale that the row has met
 #pragma unroll
     for (int fr = 0; fr < F; ++fr) {
+        v_most[fr] = -126;
         m[fr] = kNothing;
         l[fr] = 0.0f;
 #pragma unroll
         for (int e = 0; e < ND; ++e) o[fr][e] = float4x{0, 0, 0, 0};
     }
-    int v_most = -126;      // kRelative: the exponent of the largest value scale met
-    bool poisoned = false;  // whether a tile that some row does not see all of had a NaN among its values
+    bool poisoned = false;  // whether a tile that some row does not see all of had a lost code among its values
 
     // Nothing is decided around these loads, so that the compiler knows which are under way and waits for no others:
     // what has no place is read at the cache's first block, and hidden afterwards.
@@ -462,25 +475,12 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                     for (int r = 0; r < 4; ++r)
                         s[fr][f][r] = (here & sees(x, pos[fr], from[fr], key0 + 16 * (int)g + 4 * f + r)) ? s[fr][f][r] : -__builtin_inff();
             uint32_t any = 0;
+            const uint32_t lost = lost_codes<T>(v_power);
 #pragma unroll
-            for (int e = 0; e < ND; ++e) any |= take_nan(v[e]);
+            for (int e = 0; e < ND; ++e) any |= take_lost(v[e], lost);
             poisoned |= __ballot(any != 0) != 0;
         }
-        float widen_by = v_power;
-        if constexpr (W::kRelative) {
-            const int e = here && block_seen(x, key0 + 16 * (int)g, p_min, p_max) ? exponent_of(v_power) : -126;
-            int most = max(e, __shfl_xor(e, 16));
-            most = __builtin_amdgcn_readfirstlane(max(most, __shfl_xor(most, 32)));
-            if (most > v_most) {
-                const float down = exp2_fast((float)(v_most - most));
-#pragma unroll
-                for (int fr = 0; fr < F; ++fr)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) o[fr][d] *= down;
-                v_most = most;
-            }
-            widen_by = power_of(e - v_most);
-        }
+        const float widen_by = W::kRelative ? 1.0f : v_power;
         Eight p[F][2];
 #pragma unroll
         for (int fr = 0; fr < F; ++fr) {
@@ -492,12 +492,26 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
             top *= to_log2;
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (__ballot(top > m[fr] + kLazy) != 0) {
-                const float grown = fmaxf(m[fr], top), down = exp2_fast(m[fr] - grown);
+            if (__ballot(top > m[fr] + kLazy) != 0) {  // for those rows: no row's rounding depends on another
+                const float grown = top > m[fr] + kLazy ? top : m[fr], down = exp2_fast(m[fr] - grown);
                 m[fr] = grown;
                 l[fr] *= down;
 #pragma unroll
                 for (int e = 0; e < ND; ++e) o[fr][e] *= down;
+            }
+            float by = 1.0f;
+            if constexpr (W::kRelative) {
+                const int e = here && block_seen(x, key0 + 16 * (int)g, pos[fr]) ? exponent_of(v_power) : -126;
+                int most = max(e, __shfl_xor(e, 16));
+                most = max(most, __shfl_xor(most, 32));
+                if (__ballot(most > v_most[fr]) != 0) {
+                    const int grown = max(most, v_most[fr]);
+                    const float down = exp2_fast((float)(v_most[fr] - grown));
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) o[fr][d] *= down;
+                    v_most[fr] = grown;
+                }
+                by = power_of(e - v_most[fr] + kRaised);
             }
 #pragma unroll
             for (int f = 0; f < 4; ++f)
@@ -505,7 +519,7 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                 for (int r = 0; r < 4; ++r) {
                     const float w = exp2_fast(fmaf(s[fr][f][r], to_log2, -m[fr]));
                     l[fr] += w;
-                    p[fr][f / 2][f % 2 * 4 + r] = (T)w;
+                    p[fr][f / 2][f % 2 * 4 + r] = (T)(W::kRelative ? w * by : w);
                 }
         }
 #pragma unroll
@@ -524,13 +538,15 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
         v_next = v_then;
     }
 
-    if (poisoned) {  // a NaN among the values reaches the rows that see it, and no others
+    if (poisoned) {  // such a value makes NaN of the rows that see it, and of no others
         for (t = first + (int)wave; t < end; t += NW) {
             const int key0 = range.tile(t) * kTile;
             look(t, k_next, v_next);
             here = v_next.there();
             if (!is_edge(x, key0, p_min, p_max) && __ballot(!here) == 0) continue;
+            load_scales(v_next);
             load_values(v_next);
+            const uint32_t lost = lost_codes<T>(cache_scale(v_scale));
 #pragma unroll
             for (int fr = 0; fr < F; ++fr) {
                 Eight seen[2];
@@ -540,8 +556,8 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
 #pragma unroll
                 for (int e = 0; e < ND; ++e) {
                     float4x hits = {0, 0, 0, 0};
-                    hits = W::mul16(W::codes(ones_at_nan(v[e].x), ones_at_nan(v[e].y), 1.0f), seen[0], hits);
-                    hits = W::mul16(W::codes(ones_at_nan(v[e].z), ones_at_nan(v[e].w), 1.0f), seen[1], hits);
+                    hits = W::mul16(W::codes(ones_at_lost(v[e].x, lost), ones_at_lost(v[e].y, lost), 1.0f), seen[0], hits);
+                    hits = W::mul16(W::codes(ones_at_lost(v[e].z, lost), ones_at_lost(v[e].w, lost), 1.0f), seen[1], hits);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[fr][e][r] = hits[r] > 0 ? __builtin_nanf("") : o[fr][e][r];
                 }
@@ -567,7 +583,7 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
 #pragma unroll
         for (int w = 0; w < NW; ++w) l[fr] += exp2_fast(weights[w][16 * fr + n].x - most) * weights[w][16 * fr + n].y;
         down[fr] = exp2_fast(m[fr] - most);
-        if constexpr (W::kRelative) down[fr] *= power_of(v_most);
+        if constexpr (W::kRelative) down[fr] *= power_of(v_most[fr] - kRaised);
         m[fr] = most;
     }
     const bool whole = job.segments == 1;
@@ -633,7 +649,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
     __shared__ Eight vals[2][4 * 2 * DP];  // [block][its halves of 8 tokens][dimension]
     // a block's key scale in the softmax's exponents, or -1 where it is not in the cache, and its value scale
     __shared__ float2 scales[2][4];
-    __shared__ int poisoned;  // whether a tile that some row does not see all of had a NaN among its values
+    __shared__ int poisoned;  // whether a tile that some row does not see all of had a lost code among its values
     const Job job = find_job<R, false>(x, item_of_block());
     if (!job.found) return;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -721,8 +737,9 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
         const int stage = (t - first) & 1;
         if (is_edge(x, range.tile(t) * kTile, all_min, all_max)) {
             uint32_t any = 0;
+            const uint32_t lost = lost_codes<T>(cache_scale(scale_in.y));
 #pragma unroll
-            for (int i = 0; i < L; ++i) any |= take_nan(v_in[i]);
+            for (int i = 0; i < L; ++i) any |= take_lost(v_in[i], lost);
             if (any != 0) poisoned = 1;
         }
         const float widen_by = W::kRelative ? 1.0f : cache_scale(scale_in.y);
@@ -799,31 +816,32 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
         }
         float most = fmaxf(top[0] * to_log2[0], top[1] * to_log2[1]);
         most = fmaxf(most, __shfl_xor(most, 32));
-        if (__ballot(most > m + kLazy) != 0) {
-            const float grown = fmaxf(m, most), down = exp2_fast(m - grown);
+        if (__ballot(most > m + kLazy) != 0) {  // for those rows: no row's rounding depends on another
+            const float grown = most > m + kLazy ? most : m, down = exp2_fast(m - grown);
             m = grown;
             l *= down;
 #pragma unroll
             for (int e = 0; e < NO; ++e) o[e] *= down;
         }
-        float down[2] = {1.0f, 1.0f};  // of values, relative to the largest scale
+        float raise[2] = {1.0f, 1.0f};  // by the values' scales, relative to the largest that the row has met
         if constexpr (W::kRelative) {
-            int e[2], largest = -126;
+            int e[2];
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
-                const bool counts = scale[f].x > 0.0f && block_seen(x, key0 + 32 * f + 16 * (int)h, p_min, p_max);
+                const bool counts = scale[f].x > 0.0f && block_seen(x, key0 + 32 * f + 16 * (int)h, pos);
                 e[f] = counts ? exponent_of(scale[f].y) : -126;
-                largest = max(largest, e[f]);
             }
-            largest = __builtin_amdgcn_readfirstlane(max(largest, __shfl_xor(largest, 32)));
-            if (largest > v_most) {
-                const float by = exp2_fast((float)(v_most - largest));
+            int largest = max(e[0], e[1]);
+            largest = max(largest, __shfl_xor(largest, 32));
+            if (__ballot(largest > v_most) != 0) {
+                const int grown = max(largest, v_most);
+                const float by = exp2_fast((float)(v_most - grown));
 #pragma unroll
                 for (int d = 0; d < NO; ++d) o[d] *= by;
-                v_most = largest;
+                v_most = grown;
             }
 #pragma unroll
-            for (int f = 0; f < 2; ++f) down[f] = power_of(e[f] - v_most);
+            for (int f = 0; f < 2; ++f) raise[f] = power_of(e[f] - v_most + kRaised);
         }
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
@@ -833,7 +851,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
                 float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
                 if constexpr (W::kRelative) {
                     l += w;
-                    w *= down[f];
+                    w *= raise[f];
                 }
                 p[i / 8][i % 8] = (T)w;
             }
@@ -865,7 +883,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
         if (t + 1 < end) hand_over(t + 1);
         __syncthreads();
     }
-    if (poisoned && !idle) {  // a NaN among the values reaches the rows that see it, and no others
+    if (poisoned && !idle) {  // such a value makes NaN of the rows that see it, and of no others
         const Places places(x, job.index);
         for (int t = first; t < end; ++t) {
             const int key0 = range.tile(t) * kTile;
@@ -878,6 +896,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
                 for (int i = 0; i < 16; ++i)
                     seen[i / 8][i % 8] = (here & sees(x, pos, from, key0 + 32 * f + 16 * (int)h + i)) ? (T)1.0f : (T)0.0f;
                 const uint8_t* const block = v_head + (here ? place.page * x.cache.v_page + place.block * (16 * dims) : 0);
+                const uint64_t at = ((uint64_t)place.page * x.cache.heads + job.head) * x.cache.page_blocks + place.block;
+                const uint32_t lost = lost_codes<T>(cache_scale(here ? x.cache.v_scales[at] : 1.0f));
 #pragma unroll
                 for (int e = 0; e < NO; ++e) {
                     uint4 w = {0, 0, 0, 0};
@@ -885,8 +905,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
                     float16x hits;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) hits[i] = 0.0f;
-                    hits = W::mul32(W::codes(ones_at_nan(w.x), ones_at_nan(w.y), 1.0f), seen[0], hits);
-                    hits = W::mul32(W::codes(ones_at_nan(w.z), ones_at_nan(w.w), 1.0f), seen[1], hits);
+                    hits = W::mul32(W::codes(ones_at_lost(w.x, lost), ones_at_lost(w.y, lost), 1.0f), seen[0], hits);
+                    hits = W::mul32(W::codes(ones_at_lost(w.z, lost), ones_at_lost(w.w, lost), 1.0f), seen[1], hits);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[e][i] = hits[i] > 0 ? __builtin_nanf("") : o[e][i];
                 }
@@ -897,7 +917,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
     l += __shfl_xor(l, 32);
     if constexpr (W::kRelative) {
 #pragma unroll
-        for (int e = 0; e < NO; ++e) o[e] *= power_of(v_most);
+        for (int e = 0; e < NO; ++e) o[e] *= power_of(v_most - kRaised);
     }
     if (idle || n >= my_rows) return;
     const uint32_t row = wave * 32 + n;

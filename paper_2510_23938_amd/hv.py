@@ -1525,7 +1525,7 @@ def hv_fp8_cache_write(cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, starts
     """Writes new tokens' keys and values [tokens, kv_heads, head_dim] (bfloat16, float16 or float32) to the cache.
     Sequence i's new tokens are the rows ``starts[i]`` to ``starts[i + 1]`` and the last of its ``lengths[i]`` tokens;
     its token at position p goes to page ``pages[i, p // page_tokens]``.  All three are int32 tensors on the GPU.
-    No page may be written by two sequences of one call."""
+    No page may be written by two sequences of one call, nor by two columns of one."""
     index = cache.device.index
     if index != _current_device():  # a stream's handle of zero is the current device's default stream
         with torch.cuda.device(cache.device):

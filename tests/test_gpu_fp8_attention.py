@@ -216,3 +216,55 @@ def test_an_empty_cache_gives_zeros():
         args = [torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([0, 1, 3], [1, 2])]
         out = hv.hv_fp8_attention(q, cache, *args, torch.zeros(2, columns, dtype=torch.int32, device=DEV))
         assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,heads", [(8, 4), (8, 8), (30, 2), (100, 4), (100, 16)])
+@pytest.mark.parametrize("window,late", [(0, True), (40, True), (40, False)])
+def test_finite_extremes_that_others_see_change_nothing(dtype, new, heads, window, late):
+    """Blocks that only some of the tokens of a call see, the latest or (with a window) the oldest, get the largest
+    codes and scales, and the tokens that see them large queries: the others' outputs are the same bit for bit, and right."""
+    rng = rng_of(new, heads, window, late)
+    total = 310 if new > 8 else 308 if late else 316
+    batch = Batch(rng, [(new, total)], 32)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    q = torch.from_numpy(rng.standard_normal((new, heads, 64))).to(TYPES[dtype])
+    pos = np.arange(total - new, total)
+    cut = (total - new // 2) // 16 * 16
+    if late:
+        wild, untouched = range(cut, total, 16), pos < cut
+    else:
+        first = max(total - new - window + 1, 0) // 16 * 16  # the first token's oldest block, or half of it
+        wild, untouched = [first], pos - window >= first + 15
+    assert 0 < untouched.sum() < new
+    other, loud = host.copy(), q.clone()
+    for p in wild:
+        page, block = batch.table[0, p // 32], p % 32 // 16
+        other.k[page, :, block * 16:block * 16 + 16], other.ks[page, :, block] = 0x7e, 2.0 ** 100
+        other.v[page, :, block], other.vs[page, :, block] = 0x7e, 2.0 ** 127
+    loud[torch.from_numpy(~untouched)] *= 50
+    outs = [hv.hv_fp8_attention(x.to(DEV), on_gpu(c), *batch.gpu(), window=window).cpu() for c, x in ((host, q), (other, loud))]
+    keep = torch.from_numpy(untouched)
+    want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table, 0.125, window)
+    for part in want[:3]:
+        part[~untouched] = np.nan
+    for out in outs:
+        cache_bounds.check(out.double().numpy(), want, dtype, total)
+    assert torch.equal(outs[0][keep].view(torch.int16), outs[1][keep].view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,heads", [(8, 4), (8, 8), (100, 4)])
+def test_finite_extremes_in_the_rest_of_a_block_change_nothing(dtype, new, heads):
+    """The last token's value is 448 * 2^127, in a block of zeros otherwise: the tokens before it see zeros."""
+    rng = rng_of(new, heads)
+    batch = Batch(rng, [(new, 312)], 32)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    page, block, slot = fp8_cache.place(host, batch.table, 0, 311)
+    host.v[page, :, block], host.vs[page, :, block] = 0, 2.0 ** 127
+    other = host.copy()
+    other.v[page, :, block, :, slot] = 0x7e
+    q = torch.from_numpy(rng.standard_normal((new, heads, 64))).to(TYPES[dtype]).to(DEV)
+    plain, changed = (hv.hv_fp8_attention(q, on_gpu(c), *batch.gpu()).cpu() for c in (host, other))
+    assert bool(torch.isfinite(plain).all()) and not bool(torch.isfinite(changed[-1]).any())
+    assert torch.equal(plain[:-1].view(torch.int16), changed[:-1].view(torch.int16))
