@@ -21,7 +21,7 @@
 // the cache, take it from memory to registers (666 MB of 64 sequences 133 us, 5.0 TB/s; one of 131072 tokens 56 us, 4.8,
 // where a copy reaches 4.75); more rows, bound by the matrix and vector units, which
 // take turns more than they overlap (33% and 44% of the cycles), share it in LDS (4 prompts of 2048 tokens, 64 heads
-// on 8 of 128 dimensions, 344 us, 0.80 PFLOP/s; one of 16384 tokens 1.0, where a library's product reaches 1.3 to 1.5).
+// on 8 of 128 dimensions, 342 us, 0.80 PFLOP/s; one of 16384 tokens 1.0, where a library's product reaches 1.3 to 1.5).
 // In both, a sequence's keys are cut into segments where there are too few rows to fill the
 // chip; the parts' sums are joined by another kernel, in order.  A call whose sequences can have no more than 1536
 // tokens is never cut: its one launch (777 tokens: 11 us, of which the host's part is 10) is shorter than two.
