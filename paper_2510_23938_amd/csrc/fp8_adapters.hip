@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) up_kernel(AdapterArgs x) {
     const uint32_t item = item_of_block(), group = divided(item, x.by_column_blocks);
     const uint64_t col0 = (uint64_t)(item - group * x.column_blocks) * 64;
     const uint64_t tile = group, token = tile * kTokens + n;
+    if (tile * kTokens >= x.m) return;  // a workgroup past the last item
     const uint32_t mine = adapter_of(x, tile);
     const uint64_t col = col0 + 16 * g;  // of the lane's 16 outputs
     const int there = col < x.n ? (int)min(x.n - col, (uint64_t)16) : 0;
