@@ -51,22 +51,22 @@ def test_cache_write():
     assert bool((cache.k_codes.view(torch.uint8).view(257, -1)[0, 16 * (first + 10):] == 0).all())
 
 
-@pytest.mark.parametrize("new", [1, 32])
+@pytest.mark.parametrize("new", [1, 32, 40])
 def test_attention(new):
     """A key head's values of a sequence are all the same, so each output is that value, up to a weight's rounding and
     the result's: 1024 sequences of 1100 key heads."""
     gen = torch.Generator(device=DEV).manual_seed(new)
     count, heads, dim = 1024, 1100, 16
-    cache = hv.Fp8Cache.empty(2 * count, heads, 16, dim, DEV)
-    cache.k_codes.copy_(whole(gen, -3, 3, 2 * count, heads, 16, dim, dtype=torch.float16).to(E4M3))
+    cache = hv.Fp8Cache.empty(3 * count, heads, 16, dim, DEV)
+    cache.k_codes.copy_(whole(gen, -3, 3, 3 * count, heads, 16, dim, dtype=torch.float16).to(E4M3))
     value = whole(gen, -15, 15, count, heads, 1, 1, 1, dtype=torch.float16)
-    cache.v_codes.copy_(value.repeat_interleave(2, 0).expand(-1, -1, 1, dim, 16).to(E4M3))
+    cache.v_codes.copy_(value.repeat_interleave(3, 0).expand(-1, -1, 1, dim, 16).to(E4M3))
     cache.k_scales.fill_(1.0)
     cache.v_scales.fill_(0.5)
     q = torch.randn(count * new, heads, dim, generator=gen, device=DEV, dtype=torch.bfloat16)
     batch = [torch.arange(count + 1, dtype=torch.int32, device=DEV) * new,
-             torch.full((count,), 32, dtype=torch.int32, device=DEV),
-             torch.arange(2 * count, dtype=torch.int32, device=DEV).view(count, 2)]
+             torch.full((count,), 41, dtype=torch.int32, device=DEV),
+             torch.arange(3 * count, dtype=torch.int32, device=DEV).view(count, 3)]
     out = hv.hv_fp8_attention(q, cache, *batch).float()
     want = (value.float() * 0.5).view(count, 1, heads, 1)
     off = (out.view(count, new, heads, dim) - want).abs()
