@@ -47,7 +47,7 @@ constexpr int kWaitAll = 0;       // s_waitcnt: nothing outstanding
 constexpr float kLazy = 8.0f;     // binary orders that a row's weights may grow before its sums are scaled
 constexpr float kNothing = -FLT_MAX;  // the maximum of a row that has seen nothing
 // Half precision: binary orders that weights are raised by, so that those of blocks with small scales lose less.  With
-// kLazy they reach 2^12, and 2^16 where a score's last place is worth four.
+// kLazy and half of a score's last place, which is worth less than one there (kCoarse), they stay below 2^13.
 constexpr int kRaised = 4;
 
 // ---------------------------------------------------------------------------
@@ -113,6 +113,17 @@ struct Wide<_Float16> {
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A weight's exponent is s * by - m, by one instruction that rounds once, while m is a rounded product: of the largest score
+// that leaves m's rounding error, half of its last place, which all of a row's weights have in common.  Where m's last place
+// is worth one or more the product is rounded before the subtraction, as m was, so that the largest weight stays what it
+// has to be: at 2^31 half of a last place is 2^7 binary orders, which no sum would hold.
+constexpr float kCoarse = 0x1p23f;
+__device__ __forceinline__ float coarse_exponent(float s, float by, float m) {
+#pragma clang fp contract(off)
+    const float scaled = s * by;
+    return scaled - m;
+}
 
 // 2^e as the conversions' scale, at least 2^-126.
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)max(e + 127, 1) << 23); }
@@ -513,11 +524,20 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                 }
                 by = power_of(e - v_most[fr] + kRaised);
             }
+            float score_by = to_log2, less = m[fr];
+            if (__builtin_fabsf(less) >= kCoarse) {  // for those rows alone
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[fr][f][r] = coarse_exponent(s[fr][f][r], to_log2, less);
+                score_by = 1.0f;
+                less = 0.0f;
+            }
 #pragma unroll
             for (int f = 0; f < 4; ++f)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float w = exp2_fast(fmaf(s[fr][f][r], to_log2, -m[fr]));
+                    const float w = exp2_fast(fmaf(s[fr][f][r], score_by, -less));
                     l[fr] += w;
                     p[fr][f / 2][f % 2 * 4 + r] = (T)(W::kRelative ? w * by : w);
                 }
@@ -843,12 +863,22 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
 #pragma unroll
             for (int f = 0; f < 2; ++f) raise[f] = power_of(e[f] - v_most + kRaised);
         }
+        float score_by[2] = {to_log2[0], to_log2[1]}, less = m;
+        if (__builtin_fabsf(less) >= kCoarse) {  // for those rows alone
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[f][i] = coarse_exponent(s[f][i], to_log2[f], less);
+                score_by[f] = 1.0f;
+            }
+            less = 0.0f;
+        }
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             Eight p[2];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float w = exp2_fast(fmaf(s[f][i], to_log2[f], -m));
+                float w = exp2_fast(fmaf(s[f][i], score_by[f], -less));
                 if constexpr (W::kRelative) {
                     l += w;
                     w *= raise[f];

@@ -1,0 +1,65 @@
+"""Attention over the 8-bit cache far from ordinary numbers: scores whose last place is worth more than one."""
+import numpy as np
+import pytest
+import torch
+
+import cache_bounds
+from cache_cases import TYPES, Batch, on_gpu, random_cache
+from oracle import fp8, fp8_cache
+from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda")
+
+
+def rng_of(*numbers):
+    return np.random.default_rng([abs(int(n)) for n in numbers])
+
+
+def best_keys(cache, q, batch, scale):
+    """(value of each row's best key [tokens, heads, dim], by how much its score is ahead, the largest sum of
+    |q k| * scale among those that the row sees), in 64 bits."""
+    tokens, heads, dim = q.shape
+    value, ahead, steep = np.zeros(q.shape), np.full((tokens, heads), np.inf), np.zeros((tokens, heads))
+    share = heads // cache.heads
+    for i, rows, position in fp8_cache.sequences(batch.starts, batch.lengths, tokens):
+        j = np.arange(position + len(rows))
+        page, block, slot = np.array([fp8_cache.place(cache, batch.table, i, p) for p in j]).T
+        for h in range(heads):
+            g = h // share
+            keys = fp8.VALUES[cache.k[page, g, block * 16 + slot]] * cache.ks[page, g, block].astype(np.float64)[:, None]
+            vals = fp8.VALUES[cache.v[page, g, block, :, slot]] * cache.vs[page, g, block].astype(np.float64)[:, None]
+            for n, row in enumerate(rows):
+                seen = position + n + 1
+                s = keys[:seen] @ q[row, h] * scale
+                order = np.argsort(s)
+                value[row, h] = vals[order[-1]]
+                if seen > 1:
+                    ahead[row, h] = s[order[-1]] - s[order[-2]]
+                steep[row, h] = (np.abs(keys[:seen]) @ np.abs(q[row, h])).max() * scale
+    return value, ahead, steep
+
+
+# 4, 24 and 160 rows of a sequence's key head: each kernel; the long one is cut into segments
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,total", [(1, 300), (1, 3000), (6, 300), (40, 300)])
+@pytest.mark.parametrize("power", [14, 17, 19, 20, 21, 22, 23, 24, 25, 26, 27, 28, 30, 40, 64, 100])
+def test_large_scores(new, total, dtype, power):
+    """Finite scores of up to about 2^(power + 5): where the best key's is ahead by more than 100 and what 32 bits lose
+    (the bound of cache_bounds.py, and the product's and the subtraction's last places), its value is the output, up to the
+    roundings of its weight and of the result.  Every output is finite and no larger than the values."""
+    rng = rng_of(power, new, total)
+    batch = Batch(rng, [(new, total), (new, new), (1, 1), (new, new + 20)], 32)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    host.ks *= np.float32(2.0 ** power)
+    q = torch.from_numpy(rng.standard_normal((batch.tokens, 8, 64))).to(TYPES[dtype])
+    out = hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *batch.gpu()).double().cpu().numpy()
+    value, ahead, steep = best_keys(host, q.double().numpy(), batch, 0.125)
+    assert np.isfinite(out).all()
+    largest = np.abs(fp8.VALUES[host.v[np.isin(np.arange(host.pages), batch.table)] & 0x7f]).max() * host.vs.max()
+    assert (np.abs(out) <= largest).all()
+    clear = ahead > 100 + (200 * 2.0 ** -24 + 2.0 ** -21) * steep
+    assert clear.mean() > 0.5
+    half = cache_bounds.HALF_STEP[dtype]
+    off = np.abs(out - value)
+    assert (off[clear] <= (2 * half + 2.0 ** -20) * np.abs(value[clear]) + (2.0 ** -25 if dtype == "f16" else 2.0 ** -134)).all()
