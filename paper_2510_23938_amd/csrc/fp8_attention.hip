@@ -45,6 +45,9 @@ constexpr int kTile = 64;         // keys of a step
 constexpr int kMatrix = 0x8, kDsRead = 0x100;  // instruction groups of the scheduler
 constexpr int kWaitAll = 0;       // s_waitcnt: nothing outstanding
 constexpr float kLazy = 8.0f;     // binary orders that a row's weights may grow before its sums are scaled
+// What turns scores into exponents, at least: the smallest positive number, as what is not seen is minus infinity times it.
+// Sums of a query and codes are below 2^128, so what this changes is less than 2^-21 of an exponent.
+constexpr float kLeastBy = 0x1p-149f;
 constexpr float kNothing = -FLT_MAX;  // the maximum of a row that has seen nothing
 // Half precision: binary orders that weights are raised by, so that those of blocks with small scales lose less.  With
 // kLazy and half of a score's last place, which is worth less than one there (kCoarse), they stay below 2^13.
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(NW * 64) stream_attention(AttentionArgs x) {
                 }
             }
         }
-        const float to_log2 = fmaxf(cache_scale(k_scale) * x.scale, 0x1p-126f);
+        const float to_log2 = fmaxf(cache_scale(k_scale) * x.scale, kLeastBy);
         const float v_power = cache_scale(v_scale);
         load_keys(k_next);
 
@@ -772,7 +775,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_attention(Attenti
             vals[stage][(2 * wave + 1) * DP + 64 * i + lane] = W::codes(v_in[i].z, v_in[i].w, widen_by);
         }
         if (lane == 0)
-            scales[stage][wave] = float2{here ? fmaxf(cache_scale(scale_in.x) * x.scale, 0x1p-126f) : -1.0f,
+            scales[stage][wave] = float2{here ? fmaxf(cache_scale(scale_in.x) * x.scale, kLeastBy) : -1.0f,
                                          cache_scale(scale_in.y)};
     };
 

@@ -1,4 +1,5 @@
-"""Attention over the 8-bit cache far from ordinary numbers: scores whose last place is worth more than one."""
+"""Attention over the 8-bit cache far from ordinary numbers: scores whose last place is worth more than one, scales at
+the ends of 32 bits."""
 import numpy as np
 import pytest
 import torch
@@ -63,3 +64,17 @@ def test_large_scores(new, total, dtype, power):
     half = cache_bounds.HALF_STEP[dtype]
     off = np.abs(out - value)
     assert (off[clear] <= (2 * half + 2.0 ** -20) * np.abs(value[clear]) + (2.0 ** -25 if dtype == "f16" else 2.0 ** -134)).all()
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_small_key_scales_under_large_queries(new):
+    """Key scales of 2^-126 times the softmax's scale are below the smallest normal number; queries of 2^115 make scores
+    of ordinary size of them."""
+    rng = rng_of(new)
+    batch = Batch(rng, [(new, 300), (new, 41)], 32)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    host.ks[:] = 2.0 ** -126
+    q = torch.from_numpy(rng.standard_normal((batch.tokens, 8, 64)) * 2.0 ** 115).to(torch.bfloat16)
+    out = hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *batch.gpu())
+    want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table, 0.125)
+    cache_bounds.check(out.double().cpu().numpy(), want, "bf16", 300)
