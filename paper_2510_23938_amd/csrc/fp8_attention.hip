@@ -160,6 +160,12 @@ __device__ __forceinline__ uint32_t ones_at_lost(uint32_t w, uint32_t lost) {
 // ---------------------------------------------------------------------------
 // which keys, and who takes them
 
+// The first key that a position's window has, if not negative.  A position before the first, which sees nothing, is taken
+// for the first: its distance to a window's start may not fit.
+__device__ __forceinline__ int window_from(const AttentionArgs& x, int position) {
+    return x.window ? max(position, 0) - x.window + 1 : 0;
+}
+
 // Tiles of 64 keys that the positions p_min to p_max see: the first `sinks` of them from 0 on, the others from `first`.
 struct Range {
     int first, sinks, count;
@@ -169,7 +175,7 @@ struct Range {
 __device__ __forceinline__ Range range_of(const AttentionArgs& x, int p_min, int p_max) {
     const int hi = min(p_max, x.batch.capacity - 1);
     if (hi < 0 || x.cache.pages == 0) return {0, 0, 0};
-    const int lo = x.window ? max(p_min - x.window + 1, 0) : 0;
+    const int lo = max(window_from(x, p_min), 0);
     const int lo_tile = lo / kTile, hi_tile = hi / kTile;
     const int sinks = x.window ? min(lo_tile, (min(x.sinks, hi + 1) + kTile - 1) / kTile) : 0;
     return {lo_tile, sinks, sinks + max(hi_tile - lo_tile + 1, 0)};
@@ -259,15 +265,12 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& x, uint32_t item) {
 
 // Whether a position sees some of the block's 16 tokens from `key` on.
 __device__ __forceinline__ bool block_seen(const AttentionArgs& x, int key, int position) {
-    return key <= position && (!x.window || key + (int)kCacheBlock > position - x.window + 1 || key < x.sinks);
+    return key <= position && (key + (int)kCacheBlock > window_from(x, position) || key < x.sinks);
 }
 
 // `from`: the first key that a position's window has.
 __device__ __forceinline__ bool sees(const AttentionArgs& x, int position, int from, int key) {
     return (key <= position) & ((key >= from) | (key < x.sinks));
-}
-__device__ __forceinline__ int window_from(const AttentionArgs& x, int position) {
-    return x.window ? position - x.window + 1 : 0;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 

@@ -170,7 +170,8 @@ hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch,
     const hv::AttentionPlan plan = hv::fp8_attention_plan(batch->count, capacity, tokens, heads, cache->kv_heads,
                                                           cache->head_dim, window, sinks);
     HV_TRY(check_workspace(workspace, workspace_bytes, round_up(plan.workspace)));
-    constexpr uint32_t kFar = 1u << 30;  // more than any position
+    // Positions are below 2^31, so a longer window leaves nothing out; those that the table has, below kMaxCapacity.
+    const bool windowed = window < 1u << 31;
     hv::AttentionArgs args = {};
     args.cache = cache_args(*cache);
     args.batch = batch_args(*batch, cache->page_tokens, tokens);
@@ -178,8 +179,8 @@ hv_status hv_fp8_attention(const hv_fp8_cache* cache, const hv_fp8_batch* batch,
     args.out = out, args.out_token = out_token, args.out_head = out_head;
     args.share = (uint32_t)(heads / cache->kv_heads);
     args.scale = log2_scale;
-    args.window = (int)std::min(window, kFar);
-    args.sinks = (int)std::min(sinks, kFar);
+    args.window = windowed ? (int)window : 0;
+    args.sinks = (int)std::min<uint64_t>(sinks, kMaxCapacity);
     args.parts = static_cast<float*>(workspace);
     return done(hv::launch_fp8_attention(type, args, plan, stream), "attention kernels");
 }

@@ -1,5 +1,5 @@
 """Attention over the 8-bit cache far from ordinary numbers: scores whose last place is worth more than one, scales at
-the ends of 32 bits."""
+the ends of 32 bits, positions and windows near 2^31."""
 import numpy as np
 import pytest
 import torch
@@ -78,3 +78,22 @@ def test_small_key_scales_under_large_queries(new):
     out = hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *batch.gpu())
     want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table, 0.125)
     cache_bounds.check(out.double().cpu().numpy(), want, "bf16", 300)
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+@pytest.mark.parametrize("length,window,same_length,same_window", [
+    ((1 << 31) - 1, 0, 1000, 0), ((1 << 31) - 1, (1 << 31) - 1, 1000, 0), ((1 << 31) - 1, 1 << 31, 1000, 0),
+    ((1 << 31) - 1, (1 << 32) - 1, 1000, 0), ((1 << 30) + 300, (1 << 30) + 200, 300, 200), (250, (1 << 31) - 1, 250, 0),
+    ((1 << 31) - 1, (1 << 31) - 1 - 150, 300, 150), (3, (1 << 31) - 1, 3, 0), (3, (1 << 30) + 5, 3, 0)])
+def test_far_positions(new, length, window, same_length, same_window):
+    """Tokens behind the table's last column see what is in the cache: as much as nearer ones with a window that reaches
+    as far, bit for bit.  Tokens ahead of the first see nothing."""
+    rng = rng_of(new, length, window)
+    batch = Batch(rng, [(new, 240)], 48)
+    host = on_gpu(random_cache(rng, batch.pool, 2, 48, 64))
+    starts, _, table = batch.gpu()
+    q = torch.from_numpy(rng.standard_normal((new, 8, 64))).to(torch.bfloat16).to(DEV)
+    far, near = (hv.hv_fp8_attention(q, host, starts, torch.tensor([n], dtype=torch.int32, device=DEV), table, window=w)
+                 for n, w in ((length, window), (same_length, same_window)))
+    assert bool(near[-1].any())
+    assert torch.equal(far.view(torch.int16), near.view(torch.int16))
