@@ -206,7 +206,8 @@ __device__ __forceinline__ Work work_at(const AttentionArgs& x, uint32_t i) {
     return w;
 }
 
-// All lanes' units times tiles; each is cut at 2^40, which is more than any call has.
+// All lanes' units times tiles.  Each is cut at 2^40, so that 64 of them add in two pieces: one of those is enough for a share
+// of 2^30 tiles (2^9 slots), and no sequence has more than 2^24.
 __device__ __forceinline__ uint64_t total_tiles(const Work& w) {
     const uint64_t mine = min((uint64_t)w.units * w.tiles, (uint64_t)1 << 40);
     const uint32_t low = wave_scan((uint32_t)mine & 0xffff), high = wave_scan((uint32_t)(mine >> 16));
@@ -251,7 +252,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& x, uint32_t item) {
             const uint32_t row_tile = divided(unit, x.by_heads);
             part += __builtin_amdgcn_readlane(parts_upto - parts, l) + unit * n + segment;
             // the last rows, which see the most, first; what a batch without order may ask for stays in bounds
-            const bool ok = within < all && (n == 1 || part < x.parts_limit);
+            const bool ok = within < all && (n == 1 || part + (kJoin ? n - 1 : 0) < x.parts_limit);
             return {ok, sequence_in_lane(w.sequence, l), base + l, row_tiles - 1 - row_tile, unit - row_tile * x.cache.heads,
                     segment, n, part};
         }
