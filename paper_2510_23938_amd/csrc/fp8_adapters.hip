@@ -35,6 +35,7 @@ constexpr int kRanks = 64;     // of a workgroup of the first kernel
 constexpr int kMostWaves = 16; // of a workgroup
 constexpr int kStaged = 128;   // ranks of inner rows that the second kernel has in LDS
 constexpr uint32_t kNone = ~0u;
+constexpr float kNothingAdded = -0.0f;  // leaves zeros of either sign as they are
 
 template <typename W>
 struct Inner;
@@ -300,8 +301,9 @@ __global__ void __launch_bounds__(kMostWaves * 64) up_kernel(AdapterArgs x) {
             if (to_stage) stage();
             to_stage = false;
             float4x out[4];
+            const float start = a != kNone ? 0.0f : kNothingAdded;
 #pragma unroll
-            for (int f = 0; f < 4; ++f) out[f] = float4x{0, 0, 0, 0};
+            for (int f = 0; f < 4; ++f) out[f] = float4x{start, start, start, start};
             if (a != kNone) {
                 for (uint32_t r0 = 0; r0 < x.rank; r0 += 16) {
                     const uint32_t r = r0 + 4 * g;
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(256) up_tiles_kernel(AdapterArgs x) {
 #pragma unroll
         for (int b = 0; b < CB; ++b)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) out[b][f] = float4x{0, 0, 0, 0};
+            for (int f = 0; f < 4; ++f) out[b][f] = float4x{kNothingAdded, kNothingAdded, kNothingAdded, kNothingAdded};
         uint64_t left = __ballot(mine != kNone);
         while (left != 0) {
             const uint32_t a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));

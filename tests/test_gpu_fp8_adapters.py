@@ -167,3 +167,22 @@ def test_offsets_past_32_bits():
     index = torch.full((5,), adapters - 1, dtype=torch.int32, device=DEV)
     out = hv.hv_fp8_adapters(*c.args[:3], down, up, index, c.args[6].expand(adapters).contiguous())
     c.check(out)
+
+
+@pytest.mark.parametrize("m", [1, 40, 1100])
+@pytest.mark.parametrize("kind", TYPES)
+def test_tokens_without_an_adapter_keep_their_bits(m, kind):
+    """Zeros of either sign, the smallest numbers, infinities and NaN among them: out[t] is y[t]."""
+    rng = rng_of(m)
+    c = Case(rng, m, 90, 300, 16, 3, "bf16", kind, index=np.where(np.arange(m) % 3 == 0, -1, np.arange(m) % 3))
+    y, x, s, down, up, index, factors = c.args
+    tiny = torch.finfo(y.dtype).smallest_normal
+    special = torch.tensor([0.0, -0.0, tiny / 4, -tiny / 4, float("inf"), -float("inf"), 1.0], device=DEV).to(y.dtype)
+    y[:, ::2] = special.repeat(7)[:45]
+    bits = {2: torch.int16, 4: torch.int32}[y.element_size()]
+    none = index < 0
+    for args in ((y, x, s, down, up, index, factors), (y, x, s, down[:0], up[:0], index, factors[:0]),
+                 (y, x[:, :0], s[:, :0], down[:, :, :0].contiguous(), up, index, factors)):
+        out = hv.hv_fp8_adapters(*args)
+        kept = none if args[3].numel() else torch.ones_like(none)
+        assert torch.equal(out[kept].view(bits), y[kept].view(bits))
