@@ -35,6 +35,7 @@ import weakref
 
 import numpy as np
 import torch  # loads the HIP runtime libhv.so binds to
+from torch.autograd import forward_ad as _forward
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhv.so")
@@ -1172,7 +1173,7 @@ def verify(named_tensors, expected: bytes, chunk_bytes: int, alg: str = "sha256"
 # ([..., ceil(cols / 128)]) or for every block of 128 x 128
 # ([ceil(rows / 128), ceil(cols / 128)]).  There is no backward pass: what is
 # verified is a constant, and codes have no gradient.  A call that autograd
-# would record is refused.
+# would record is refused, and one on tensors with a tangent.
 
 def _device_of(t, what: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -1189,6 +1190,9 @@ def _on(t, dtypes, what: str, index: int):
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient, and the 8-bit operators have no backward pass: call them "
                          "under torch.no_grad(), or on detached tensors")
+    # the level is asked first: unpacking costs a third of a microsecond, and there is nothing to unpack outside of one
+    if _forward._current_level >= 0 and _forward.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{what} carries a tangent, and the 8-bit operators have no derivative: give them the primal")
     return t
 
 
@@ -1196,7 +1200,10 @@ def _matrix(t, dtypes, what: str, index: int, shape=None) -> tuple:
     """(data pointer, leading dimension, rows, cols) of a device tensor whose last dimension
     lies in one piece: two-dimensional with any row stride, or contiguous.  The library trusts
     what it is given, so anything it would overrun or misread is refused here."""
-    s = _on(t, dtypes, what, index).shape
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype not in dtypes or t.requires_grad or \
+            _forward._current_level >= 0:  # here, as a call costs 0.1 us
+        _on(t, dtypes, what, index)
+    s = t.shape
     if shape is not None and s != shape:
         raise ValueError(f"{what} has shape {tuple(s)}; the call needs {tuple(shape)}")
     if len(s) == 0:

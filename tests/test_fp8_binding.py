@@ -6,6 +6,7 @@ import weakref
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
 
@@ -146,3 +147,20 @@ def test_gradients_are_refused_where_they_would_be_lost(monkeypatch, operator):
             call(**args)
         assert len(library.calls) == 1
         library.calls.clear()
+
+
+@pytest.mark.parametrize("operator", OPERATORS)
+def test_forward_mode_tangents_are_refused(monkeypatch, operator):
+    """They would be dropped without a word, under no_grad too; within a level, tensors without one pass."""
+    library = Library(monkeypatch, 1)
+    call, args = arguments()[operator]
+    wide = [k for k, v in args.items() if isinstance(v, torch.Tensor) and v.dtype in (torch.bfloat16, torch.float32)]
+    with forward_ad.dual_level():
+        call(**args)
+        assert len(library.calls) == 1
+        for name in wide:
+            args = arguments()[operator][1]
+            args[name] = forward_ad.make_dual(args[name], torch.ones_like(args[name])).as_subclass(OnGpu1)
+            with pytest.raises(ValueError, match=f"{name} carries a tangent"), torch.no_grad():
+                call(**args)
+    assert len(library.calls) == 1

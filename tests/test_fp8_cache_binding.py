@@ -2,6 +2,7 @@
 GPU: tensors in host memory say that they are on one, and a recorder stands in for the library."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import test_fp8_binding as base
 from paper_2510_23938_amd import hv  # noqa: E402  (a missing library fails the run, never skips it)
@@ -80,6 +81,23 @@ def test_gradients_are_refused_where_they_would_be_lost(monkeypatch, operator):
             call(**args)
         assert len(library.calls) == 1
         library.calls.clear()
+
+
+@pytest.mark.parametrize("operator", LIBRARY)
+def test_forward_mode_tangents_are_refused(monkeypatch, operator):
+    library = Library(monkeypatch, 1)
+    call, args = arguments()[operator]
+    wide = [k for k, v in args.items() if isinstance(v, torch.Tensor) and v.dtype in (torch.bfloat16, F32)]
+    assert wide
+    with forward_ad.dual_level():
+        call(**args)
+        assert len(library.calls) == 1
+        for name in wide:
+            args = arguments()[operator][1]
+            args[name] = forward_ad.make_dual(args[name], torch.ones_like(args[name])).as_subclass(base.OnGpu1)
+            with pytest.raises(ValueError, match=f"{name} carries a tangent"), torch.no_grad():
+                call(**args)
+    assert len(library.calls) == 1
 
 
 REFUSED = [
