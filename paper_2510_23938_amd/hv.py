@@ -1454,7 +1454,7 @@ class Fp8Cache:
     """Keys and values in 8 bits, by pages: codes ``k_codes`` [pages, kv_heads, page_tokens, head_dim] and ``v_codes``
     [pages, kv_heads, page_tokens // 16, head_dim, 16] (float8_e4m3fn) and a power of two for each 16 tokens of
     a head, ``k_scales`` and ``v_scales`` [pages, kv_heads, page_tokens // 16] (float32).  Pages and heads of the
-    codes may lie apart, a multiple of 16 bytes each; the rest is contiguous."""
+    codes may lie apart, a multiple of 16 bytes each; the rest is contiguous.  Its tensors and sizes stay what they are."""
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
         device = _device_of(k_codes, "k_codes")
@@ -1488,6 +1488,20 @@ class Fp8Cache:
         self._struct = hv_fp8_cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
                                     pages, heads, tokens, dim, k_page, k_head, v_page, v_head)
         self._ref = ctypes.byref(self._struct)
+
+    # what calls go by: its addresses are in _struct
+    _FIXED = frozenset(("k_codes", "k_scales", "v_codes", "v_scales", "pages", "kv_heads", "page_tokens", "head_dim",
+                        "device", "_struct", "_ref"))
+
+    def __setattr__(self, name, value):
+        if name in self._FIXED and "_ref" in self.__dict__:
+            raise AttributeError(f"{name} of a cache stays as it was made: make another Fp8Cache")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self._FIXED:
+            raise AttributeError(f"{name} of a cache stays as it was made: make another Fp8Cache")
+        super().__delattr__(name)
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, page_tokens: int, head_dim: int, device="cuda") -> Fp8Cache:

@@ -174,6 +174,19 @@ def test_caches_refused():
         hv.Fp8Cache.empty(4, 2, 40, 64, device="cpu")
 
 
+@pytest.mark.parametrize("name", ["k_codes", "k_scales", "v_codes", "v_scales", "pages", "kv_heads", "page_tokens", "head_dim", "device"])
+def test_a_caches_parts_stay(name):
+    """Calls go to the addresses and sizes that the cache was made with: another tensor in one's place would be neither
+    checked nor used, and the one before it freed under them."""
+    cache = hv.Fp8Cache(*parts())
+    was = getattr(cache, name)
+    with pytest.raises(AttributeError, match="another Fp8Cache"):
+        setattr(cache, name, was)
+    with pytest.raises(AttributeError, match="another Fp8Cache"):
+        delattr(cache, name)
+    assert getattr(cache, name) is was
+
+
 def test_strides_as_the_library_takes_them(monkeypatch):
     """Keys and values of one product's rows, a table's rows apart, pages of a pool that holds both."""
     seen = {}
