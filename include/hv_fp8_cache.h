@@ -104,8 +104,11 @@ size_t hv_fp8_attention_workspace_bytes(uint64_t sequences, uint64_t capacity, u
  * holds (NaN included).
  * Products of q and codes and of weights and codes are added in 32 bits, the softmax
  * is in 32 bits; a weight is rounded to the type before its product, relative to its row's
- * largest, and the result once.  Scores beyond 32 bits give NaN or, where all
- * of a token's are minus infinity, zeros; values whose sums are beyond 32 bits give infinities or NaN.
+ * largest, and the result once.  Finite scores of any size are kept apart as far as 32 bits do.  Scores beyond 32 bits,
+ * their sums before the key scale, and `scale` times a key scale beyond them give NaN or, where all of a token's scores are
+ * minus infinity, zeros; values whose sums, by weights of up to 2^8 that are divided by theirs at the end,
+ * are beyond 32 bits give infinities or NaN.  For HV_BF16, values (codes times their scale) below 2^-126 are rounded to
+ * multiples of 2^-133.
  *   type: HV_BF16 or HV_F16, of q and out.
  *   q, out: [tokens][heads][head_dim], the dimensions of a head adjacent; kv_heads divides heads.
  *   scale: positive and finite, at least 2^-126.

@@ -97,3 +97,39 @@ def test_far_positions(new, length, window, same_length, same_window):
                  for n, w in ((length, window), (same_length, same_window)))
     assert bool(near[-1].any())
     assert torch.equal(far.view(torch.int16), near.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 3, 20])
+def test_many_sequences(dtype, new):
+    """More than ten times as many as a wave looks at at once, short ones and a few that are cut."""
+    rng = rng_of(new, 700)
+    lengths = rng.integers(0, 60, 700)
+    lengths[[5, 300, 301, 650, 699]] = [2500, 1800, 4000, 3000, 1700]
+    batch = Batch(rng, [(min(int(rng.integers(0, new + 1)) if n < 100 else new, int(n)), int(n)) for n in lengths], 16)
+    host = random_cache(rng, batch.pool, 1, 16, 32)
+    q = torch.from_numpy(rng.standard_normal((batch.tokens, 4, 32))).to(TYPES[dtype])
+    out = hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *batch.gpu())
+    want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table, 32 ** -0.5)
+    cache_bounds.check(out.double().cpu().numpy(), want, dtype, 60)
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_values_near_the_smallest_numbers(new):
+    """Values under a scale of 2^-126, in units of it; half of the dimensions have values below it.  bfloat16 holds those as
+    multiples of 2^-7 units, and codes are multiples of 2^-9: a value is off by up to 2^-8 units, their mean by weights that
+    add up to one by as much, and the result's rounding by as much again."""
+    rng = rng_of(new, 4)
+    batch = Batch(rng, [(new, 300), (new, 41)], 32)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    host.vs[:] = 2.0 ** -126
+    host.v[:, :, :, ::2] = fp8.round_to_code(rng.uniform(-2, 2, host.v[:, :, :, ::2].shape))
+    q = torch.from_numpy(rng.standard_normal((batch.tokens, 8, 64))).to(torch.bfloat16)
+    out = hv.hv_fp8_attention(q.to(DEV), on_gpu(host), *batch.gpu()).double().cpu().numpy() * 2.0 ** 126
+    units = host.copy()
+    units.vs[:] = 1.0
+    want, size, root, steep = fp8_cache.attention(units, q.double().numpy(), batch.starts, batch.lengths, batch.table, 0.125)
+    half = cache_bounds.HALF_STEP["bf16"]
+    weights = 2 * (100 * 2.0 ** -24 * steep + 2.0 ** -21 + 2.0 ** -18)[:, :, None]
+    allowed = weights * size + 6 * half / np.sqrt(3) * root + half * np.abs(want) + 2 * 2.0 ** -8
+    assert (np.abs(out - want) <= allowed).all()
