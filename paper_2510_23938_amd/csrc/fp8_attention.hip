@@ -101,12 +101,6 @@ struct Wide<_Float16> {
         const f16x2 a = two<false>(lo, scale), b = two<true>(lo, scale), c = two<false>(hi, scale), d = two<true>(hi, scale);
         return Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
-    static __device__ __forceinline__ float add(Eight p, float sum) {
-        const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2(f16x2{p[i], p[i + 1]}, one, sum, false);
-        return sum;
-    }
     static __device__ __forceinline__ float4x mul16(Eight a, Eight b, float4x c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
