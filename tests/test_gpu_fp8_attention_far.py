@@ -133,3 +133,67 @@ def test_values_near_the_smallest_numbers(new):
     weights = 2 * (100 * 2.0 ** -24 * steep + 2.0 ** -21 + 2.0 ** -18)[:, :, None]
     allowed = weights * size + 6 * half / np.sqrt(3) * root + half * np.abs(want) + 2 * 2.0 ** -8
     assert (np.abs(out - want) <= allowed).all()
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_offsets_past_32_bits(new):
+    """Pages behind the first 4 GiB of a pool, and tokens' rows behind the first 4 GiB of queries and outputs."""
+    rng = rng_of(new, 32)
+    batch = Batch(rng, [(new, 300)], 32, spare=2)
+    host = random_cache(rng, batch.pool, 2, 32, 64)
+    apart, far = 1 << 29, 1 << 26 if new > 1 else 128
+    codes = []
+    for a in (host.k, host.v):
+        raw = torch.empty(batch.pool * apart, dtype=torch.uint8, device=DEV)
+        inner = (64, 1) if a.ndim == 4 else (1024, 16, 1)
+        t = raw.as_strided(a.shape, (apart, 2048, *inner))
+        t.copy_(torch.from_numpy(a).to(DEV))
+        codes.append(t.view(torch.float8_e4m3fn))
+    assert int(batch.table.max()) * apart > 1 << 32
+    cache = hv.Fp8Cache(codes[0], torch.from_numpy(host.ks).to(DEV), codes[1], torch.from_numpy(host.vs).to(DEV))
+    rows = [torch.empty(far * new, dtype=torch.bfloat16, device=DEV).as_strided((new, 8, 64), (far, 64, 1)) if far > 128 else
+            torch.empty(new, 8, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    q = torch.from_numpy(rng.standard_normal((new, 8, 64))).to(torch.bfloat16)
+    rows[0].copy_(q.to(DEV))
+    hv.hv_fp8_attention(rows[0], cache, *batch.gpu(), out=rows[1])
+    want = fp8_cache.attention(host, q.double().numpy(), batch.starts, batch.lengths, batch.table, 0.125)
+    cache_bounds.check(rows[1].double().cpu().numpy(), want, "bf16", 300)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 12, 40])
+def test_a_very_long_context(dtype, new):
+    """Three million tokens, against a softmax in 64 bits on the GPU."""
+    gen = torch.Generator(device=DEV).manual_seed(new)
+    length, page, dim = 3_000_001, 1024, 16
+    pages = -(-length // page)
+    cache = hv.Fp8Cache.empty(pages, 1, page, dim, DEV)
+    for t in (cache.k_codes, cache.v_codes):
+        t.copy_((torch.randn(t.shape, generator=gen, device=DEV) * 30).to(t.dtype))
+    cache.k_scales.fill_(2.0 ** -5)
+    cache.v_scales.copy_(torch.exp2(torch.randint(-6, 1, cache.v_scales.shape, generator=gen, device=DEV).float()))
+    table = torch.randperm(pages, generator=gen, device=DEV).to(torch.int32).view(1, pages)
+    q = torch.randn(new, 2, dim, generator=gen, device=DEV).to(TYPES[dtype])
+    starts, lengths = (torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([0, new], [length]))
+    out = hv.hv_fp8_attention(q, cache, starts, lengths, table).double()
+    order = table[0].long()
+    k = cache.k_codes[order].float().double().view(-1, dim) * 2.0 ** -5
+    v = cache.v_codes[order].float().double() * cache.v_scales[order].double()[..., None, None]
+    v = v.transpose(3, 4).reshape(-1, dim)
+    half = cache_bounds.HALF_STEP[dtype]
+    for n in range(new):
+        seen = length - new + n + 1
+        for h in range(2):
+            s = (k[:seen] * q[n, h].double()).sum(1) * 0.25
+            w = torch.softmax(s, 0)[:, None]
+            want, size = (w * v[:seen]).sum(0), (w * v[:seen].abs()).sum(0)
+            root = ((w * v[:seen]) ** 2).sum(0).sqrt()
+            steep = float((k[:seen].abs() * q[n, h].double().abs()).sum(1).max()) * 0.25
+            allowed = 2 * (100 * 2.0 ** -24 * steep + 2.0 ** -21 + 2.0 ** -18) * size + 6 * half / 3 ** 0.5 * root + half * want.abs()
+            if dtype == "f16":  # weights that are subnormal numbers (half_bounds.py), and a subnormal result
+                p = torch.exp(s - s.max()) * cache.v_scales[order].double().view(-1, 1).expand(-1, 16).reshape(-1)[:seen] * 16
+                small = p < 2.0 ** -14
+                codes = (v[:seen] / cache.v_scales[order].double().view(-1, 1).expand(-1, 16).reshape(-1, 1)[:seen]).abs()
+                lost = (torch.clamp(p, max=2.0 ** -25) * small)[:, None] * codes
+                allowed += lost.sum(0) / 16 / torch.exp(s - s.max()).sum() + 2.0 ** -25
+            assert bool(((out[n, h] - want).abs() <= allowed).all()), (n, h, ((out[n, h] - want).abs() / allowed).max())
