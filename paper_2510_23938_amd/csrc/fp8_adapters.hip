@@ -11,10 +11,10 @@
 // adapter is read once for 16 tokens; the matrix unit has time for the products thrown away.
 //
 // The inner rows stay in 32 bits: the second product is made by the 32-bit instruction,
-// whose rate is enough beside reading y and writing the output (2048 x 28672 of rank 16: 5 of 68 us go away with
+// whose rate is enough beside reading y and writing the output (2048 x 28672 of rank 16: 5 of 68 us went away with
 // three quarters of it).
 //
-// 2048 tokens of four prompts, 8192 x 28672, rank 16: 16 and 68 us (3.5 TB/s; a copy 4.75: reading `up` anew for each
+// 2048 tokens of four prompts, 8192 x 28672, rank 16: 16 and 67 us (3.6 TB/s; a copy 4.75: reading `up` anew for each
 // 16 tokens costs 12 of them); 32 tokens with 16 adapters in each 16, 8192 x 8192: 6 and 6 us, three trips to memory each.
 #include <algorithm>
 #include <type_traits>
@@ -444,7 +444,7 @@ AdapterPlan fp8_adapter_plan(uint64_t m, uint64_t k, uint64_t rank, uint64_t ada
     const uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>({wanted, (groups + p.down_waves - 1) / p.down_waves, 16}));
     p.split_groups = (uint32_t)std::max<uint64_t>(1, (groups + splits - 1) / splits);
     p.splits = (uint32_t)std::max<uint64_t>(1, (groups + p.split_groups - 1) / p.split_groups);
-    // More than 1024 tokens fill the chip by themselves (2048 x 28672 of rank 16: 68 us, and 94 by a wave for each adapter);
+    // More than 1024 tokens fill the chip by themselves (2048 x 28672 of rank 16: 67 us, and 94 by a wave for each adapter);
     // of fewer, each adapter has a wave (32 x 8192 with 16 in each 16 tokens: 6 us, by four waves in turn 27).
     p.many = m > 1024;
     p.token_rows = (uint32_t)((tiles + kRowOfItems - 1) / kRowOfItems);

@@ -21,10 +21,10 @@
 // the cache, take it from memory to registers (666 MB of 64 sequences 133 us, 5.0 TB/s; one of 131072 tokens 56 us, 4.8,
 // where a copy reaches 4.75); more rows, bound by the matrix and vector units, which
 // take turns more than they overlap (33% and 44% of the cycles), share it in LDS (4 prompts of 2048 tokens, 64 heads
-// on 8 of 128 dimensions, 342 us, 0.80 PFLOP/s; one of 16384 tokens 1.0, where a library's product reaches 1.3 to 1.5).
+// on 8 of 128 dimensions, 350 us, 0.79 PFLOP/s; one of 16384 tokens 1.0, where a library's product reaches 1.3 to 1.5).
 // In both, a sequence's keys are cut into segments where there are too few rows to fill the
 // chip; the parts' sums are joined by another kernel, in order.  A call whose sequences can have no more than 1536
-// tokens is never cut: its one launch (777 tokens: 11 us, of which the host's part is 10) is shorter than two.
+// tokens is never cut: its one launch (777 tokens: 11 us) is shorter than two (13.6, with room for 8192).
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -1061,7 +1061,7 @@ AttentionPlan fp8_attention_plan(uint64_t sequences, uint64_t capacity, uint64_t
     plan.dims = (uint32_t)((head_dim + 63) / 64 * 64);
     const uint64_t share = heads / kv_heads;
     const uint64_t rows = (tokens + sequences - 1) / sequences * share;  // of a sequence, on the average
-    // (8 sequences of 8000 tokens, 64 rows of 128 dimensions: straight from memory 79 us, by tiles 47; 32 rows 33 and 41)
+    // (8 sequences of 8000 tokens, 64 rows of 128 dimensions: straight from memory 79 us, by tiles 46; 32 rows 33 and 41)
     plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kManyRows;
     if (plan.rows == kManyRows && head_dim > 64 && head_dim <= 96) plan.dims = 96;  // products and LDS of three quarters
     const uint64_t units = kv_heads * (tokens * share / plan.rows + std::min(sequences, tokens));

@@ -10,7 +10,7 @@
 // for each dimension: 16 loads of two elements a lane turn the block without LDS or
 // exchanges between lanes, and the stores are whole lines.
 //
-// Bound by memory: 16384 tokens of 8 heads of 128 dimensions in bfloat16 (101 MB) 25 us, 4.0 TB/s, where a copy
+// Bound by memory: 16384 tokens of 8 heads of 128 dimensions in bfloat16 (101 MB) 26 us, 3.8 TB/s, where a copy
 // reaches 4.75: 1.6 rounds of the waves that the chip holds, each with three trips to memory (the sequences,
 // the page beside the elements, the stores).  A token of each of 8 sequences takes 6 us, those trips and a launch.
 #include <algorithm>
